@@ -1,5 +1,5 @@
-"""Binding of libechoattn: same names as include/echoattn.h, include/echodropout.h and
-include/echolstm.h, argument marshalling only.  Device buffers are passed as torch tensors (their
+"""Binding of libechoattn: same names as include/echoattn.h, include/echodropout.h, include/echolstm.h,
+include/echovocab.h and include/echoclip.h, argument marshalling only.  Device buffers are passed as torch tensors (their
 data_ptr() is taken) or as integer addresses; nothing is computed here.
 
 The shared library must have been built (python -m paper_1805_08899_amd.build);
@@ -27,6 +27,17 @@ DTYPES = {"f32": ECHO_F32, "bf16": ECHO_BF16}
 class echo_attn_desc_t(ctypes.Structure):
     _fields_ = [("B", c_int32), ("Tq", c_int32), ("Tk", c_int32), ("H", c_int32), ("Dv", c_int32),
                 ("in_dtype", c_int32)]
+
+
+ECHO_VOCAB_MAX_ROWS, ECHO_VOCAB_MAX_D, ECHO_GRAD_MAX_COUNT = 1 << 24, 16384, 16384
+
+
+class echo_vocab_desc_t(ctypes.Structure):
+    _fields_ = [("N", c_int32), ("V", c_int32), ("D", c_int32), ("in_dtype", c_int32), ("out_dtype", c_int32)]
+
+
+class echo_grad_t(ctypes.Structure):
+    _fields_ = [("grad", c_void_p), ("clipped", c_void_p), ("n", ctypes.c_int64), ("dtype", c_int32), ("reserved", c_int32)]
 
 
 class EchoError(RuntimeError):
@@ -67,6 +78,21 @@ EXPORTS = {
     "echo_lstm_cell_fwd_stash": (c_int, [ctypes.c_int64, ctypes.c_int64] + [c_void_p] * 8),
     "echo_lstm_cell_bwd_stash": (c_int, [ctypes.c_int64, ctypes.c_int64] + [c_void_p] * 8),
     "echo_lstm_cell_kept_bytes": (c_size_t, [ctypes.c_int64, ctypes.c_int64, c_int]),
+    "echo_embed_fwd": (c_int, [POINTER(echo_vocab_desc_t), c_void_p, c_void_p, c_float, c_void_p, c_void_p]),
+    "echo_embed_bwd_workspace_bytes": (c_size_t, [POINTER(echo_vocab_desc_t)]),
+    "echo_embed_bwd": (c_int, [POINTER(echo_vocab_desc_t), c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_size_t,
+                               c_void_p]),
+    "echo_embed_bwd_accumulate": (c_int, [POINTER(echo_vocab_desc_t), c_void_p, c_void_p, c_float, c_void_p, c_void_p,
+                                          c_size_t, c_void_p]),
+    "echo_vocab_loss_fwd_workspace_bytes": (c_size_t, [POINTER(echo_vocab_desc_t)]),
+    "echo_vocab_loss_fwd": (c_int, [POINTER(echo_vocab_desc_t)] + [c_void_p] * 3 + [c_float] + [c_void_p] * 3 +
+                            [c_size_t, c_void_p]),
+    "echo_vocab_loss_bwd_workspace_bytes": (c_size_t, [POINTER(echo_vocab_desc_t)]),
+    "echo_vocab_loss_bwd": (c_int, [POINTER(echo_vocab_desc_t)] + [c_void_p] * 5 + [c_float] + [c_void_p] * 3 +
+                            [c_size_t, c_void_p]),
+    "echo_grad_workspace_bytes": (c_size_t, [POINTER(echo_grad_t), c_int32]),
+    "echo_grad_norm": (c_int, [POINTER(echo_grad_t), c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "echo_grad_clip": (c_int, [POINTER(echo_grad_t), c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]),
     "echo_status_string": (c_char_p, [c_int]),
     "echo_last_error_detail": (c_char_p, []),
     "echo_version": (c_char_p, []),
@@ -107,7 +133,8 @@ def _install_native_calls(L) -> None:
     if not os.path.exists(PY_CALLS_PATH):
         raise FileNotFoundError(f"{PY_CALLS_PATH} is missing: build it with `python -m paper_1805_08899_amd.build`")
     from . import _py_calls
-    _py_calls.bind(echo_attn_desc_t, {name: ctypes.cast(getattr(L, name), c_void_p).value for name in EXPORTS})
+    _py_calls.bind(echo_attn_desc_t, echo_vocab_desc_t, echo_grad_t,
+                   {name: ctypes.cast(getattr(L, name), c_void_p).value for name in EXPORTS})
     for name in EXPORTS:
         native = getattr(_py_calls, name, None)
         if native is not None:
@@ -291,6 +318,89 @@ def echo_lstm_cell_bwd_stash(B, H, dh, dc, acts, tanh_c, c_prev, da, dc_prev, st
 
 def echo_lstm_cell_kept_bytes(B: int, H: int, stash: bool) -> int:
     return lib().echo_lstm_cell_kept_bytes(B, H, 1 if stash else 0)
+
+
+def make_vocab_desc(N, V, D, in_dtype="f32", out_dtype="f32") -> echo_vocab_desc_t:
+    codes = [DTYPES[t] if isinstance(t, str) else int(t) for t in (in_dtype, out_dtype)]
+    return echo_vocab_desc_t(N, V, D, *codes)
+
+
+def echo_embed_fwd(desc, tokens, table, scale, out, stream=None) -> int:
+    return lib().echo_embed_fwd(ctypes.byref(desc), _ptr(tokens), _ptr(table), scale, _ptr(out), _stream(stream))
+
+
+def echo_embed_bwd_workspace_bytes(desc) -> int:
+    return lib().echo_embed_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_embed_bwd(desc, tokens, dout, scale, dtable, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_embed_bwd(ctypes.byref(desc), _ptr(tokens), _ptr(dout), scale, _ptr(dtable), _ptr(workspace),
+                                _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_embed_bwd_accumulate(desc, tokens, dout, scale, dtable, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_embed_bwd_accumulate(ctypes.byref(desc), _ptr(tokens), _ptr(dout), scale, _ptr(dtable),
+                                           _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_vocab_loss_fwd_workspace_bytes(desc) -> int:
+    return lib().echo_vocab_loss_fwd_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_vocab_loss_fwd(desc, h, W, labels, label_smoothing, loss, lse, workspace, workspace_bytes=None,
+                        stream=None) -> int:
+    return lib().echo_vocab_loss_fwd(ctypes.byref(desc), _ptr(h), _ptr(W), _ptr(labels), label_smoothing, _ptr(loss),
+                                     _ptr(lse), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_vocab_loss_bwd_workspace_bytes(desc) -> int:
+    return lib().echo_vocab_loss_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_vocab_loss_bwd(desc, dloss, lse, h, W, labels, label_smoothing, dh, dW, workspace, workspace_bytes=None,
+                        stream=None) -> int:
+    return lib().echo_vocab_loss_bwd(ctypes.byref(desc), _ptr(dloss), _ptr(lse), _ptr(h), _ptr(W), _ptr(labels),
+                                     label_smoothing, _ptr(dh), _ptr(dW), _ptr(workspace),
+                                     _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def make_grads(grads, clipped=None):
+    """The array of echo_grad_t of some fp32 and bf16 torch tensors; clipped: where each goes (None: in place).  The array
+    holds addresses; it keeps the tensors alive as its attribute `tensors`."""
+    grads = list(grads)
+    clipped = grads if clipped is None else list(clipped)
+    if len(clipped) != len(grads):
+        raise ValueError(f"{len(grads)} gradients, {len(clipped)} places for them")
+    codes = {"torch.float32": ECHO_F32, "torch.bfloat16": ECHO_BF16}
+    array = (echo_grad_t * len(grads))()
+    for e, g, c in zip(array, grads, clipped):
+        if g.dtype != c.dtype or g.numel() != c.numel() or str(g.dtype) not in codes:
+            raise ValueError("gradients are fp32 or bf16 tensors, clipped ones of the same type and size")
+        if not (g.is_contiguous() and c.is_contiguous()):
+            raise ValueError("tensor must be contiguous")
+        e.grad, e.clipped, e.n, e.dtype = g.data_ptr(), c.data_ptr(), g.numel(), codes[str(g.dtype)]
+    array.tensors = (grads, clipped)
+    return array
+
+
+def _count(grads, count):
+    if count > len(grads):
+        raise ValueError(f"count {count} of an array of {len(grads)}")
+    return count
+
+
+def echo_grad_workspace_bytes(grads, count) -> int:
+    return lib().echo_grad_workspace_bytes(grads, _count(grads, count))
+
+
+def echo_grad_norm(grads, count, norm, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_grad_norm(grads, _count(grads, count), _ptr(norm), _ptr(workspace),
+                                _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_grad_clip(grads, count, max_norm, norm, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_grad_clip(grads, _count(grads, count), max_norm, _ptr(norm), _ptr(workspace),
+                                _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_status_string(status: int) -> str:

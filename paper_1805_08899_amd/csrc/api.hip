@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "launch.hpp"
 
 namespace {
 
@@ -196,6 +197,31 @@ echo_status_t bwd_impl(const echo_attn_desc_t *desc, const float *dContext, cons
                                        dv_flag, next_launch_number(), dv, st));
     return ECHO_OK;
 }
+
+}  // namespace
+
+namespace echo {
+
+LaunchRecord launch_begin(const char *name, hipStream_t st) {
+    LaunchRecord r{name, st, nullptr, nullptr};
+    (void)hipGetLastError();
+    if (g_prof_on && hipEventCreate(&r.t0) == hipSuccess && hipEventCreate(&r.t1) == hipSuccess) (void)hipEventRecord(r.t0, st);
+    return r;
+}
+echo_status_t launch_end(LaunchRecord &r) {
+    const hipError_t e = hipGetLastError();
+    if (r.t0 && r.t1) {
+        (void)hipEventRecord(r.t1, r.st);
+        g_prof.push_back({r.name, r.t0, r.t1});
+    }
+    if (e == hipSuccess) return ECHO_OK;
+    g_last_error = std::string(r.name) + ": " + hipGetErrorString(e);
+    return ECHO_ERR_HIP;
+}
+
+}  // namespace echo
+
+namespace {
 
 // ---- device memory that belongs to the library: the backward workspace of echo_attn_bwd_static -------------
 // In host code `scratch` is only the handle of the symbol, not an address on the device; the address of each

@@ -1,0 +1,402 @@
+// Token embedding out[n] = s E[t_n] and its gradient dE[v] = s sum_{t_n = v} dout[n], by sorted tokens.
+//
+// Both are bound by HBM: the forward pass reads N rows and writes N rows, the backward pass reads N rows of dout and writes all V
+// rows of dE (or, adding, reads and writes those of the words that occur).
+//
+// Backward, three launches and no floating-point atomics:
+//   k_embed_sort   a stable counting sort of the tokens.  A block owns a range of words; it reads all tokens (from the caches: N words of 4
+//                  bytes, a D-th of what the rows are) and so knows by itself how many tokens lie in front of its range and
+//                  where each of its own goes: no exchange between blocks, one launch.
+//   k_embed_sum    a wave per word with up to kRun tokens adds their rows in order; a wave per kRun sorted tokens adds what of them belongs to
+//                  longer runs (the commonest word of Zipf's law has a tenth of all tokens, padding more) into parts.
+//   k_embed_join   adds the parts of a long run in order.
+#include "../../include/echovocab.h"
+
+#include <hip/hip_runtime.h>
+
+#include "common.hpp"
+#include "launch.hpp"
+
+namespace echo {
+
+typedef __bf16 bf16_hw;
+__device__ __forceinline__ unsigned short bf16_bits(float x) { return __builtin_bit_cast(unsigned short, (bf16_hw)x); }
+
+// VEC consecutive elements (VEC 4: aligned, 1: any)
+template <int VEC> struct Quad { float v[VEC]; };
+template <int VEC> __device__ __forceinline__ Quad<VEC> load_vec(const float *p, size_t i) {
+    if constexpr (VEC == 4) {
+        const float4 x = ld4(p, i);
+        return {{x.x, x.y, x.z, x.w}};
+    } else {
+        return {{p[i]}};
+    }
+}
+template <int VEC> __device__ __forceinline__ Quad<VEC> load_vec(const bf16_t *p, size_t i) {
+    if constexpr (VEC == 4) {
+        const float4 x = ld4(p, i);
+        return {{x.x, x.y, x.z, x.w}};
+    } else {
+        return {{ld(p, i)}};
+    }
+}
+template <int VEC> __device__ __forceinline__ void store_vec(float *p, size_t i, const Quad<VEC> &q) {
+    if constexpr (VEC == 4) store4_streaming(p + i, make_float4(q.v[0], q.v[1], q.v[2], q.v[3]));
+    else store_streaming(p + i, q.v[0]);
+}
+template <int VEC> __device__ __forceinline__ void store_vec(bf16_t *p, size_t i, const Quad<VEC> &q) {
+    if constexpr (VEC == 4) {
+        const u32x2 u = {(unsigned)bf16_bits(q.v[0]) | (unsigned)bf16_bits(q.v[1]) << 16,
+                         (unsigned)bf16_bits(q.v[2]) | (unsigned)bf16_bits(q.v[3]) << 16};
+        __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(p + i));
+    } else {
+        p[i].bits = bf16_bits(q.v[0]);
+    }
+}
+
+// ---- forward: a wave per row and up to kFwdPieces x 64 VEC columns, whose loads leave together ------------------------
+constexpr int kFwdPieces = 4;
+template <typename TI, typename TO, int VEC>
+__global__ __launch_bounds__(256) void k_embed_fwd(const int *__restrict__ tokens, const TI *__restrict__ table, float scale,
+                                                   TO *__restrict__ out, int N, int V, int D) {
+    const int n = blockIdx.x * 4 + wave_id(), c0 = ((int)blockIdx.y * kFwdPieces * 64 + lane_id()) * VEC;
+    if (n >= N) return;
+    const int t = tokens[n];
+    Quad<VEC> q[kFwdPieces];
+#pragma unroll
+    for (int k = 0; k < kFwdPieces; ++k)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) q[k].v[j] = 0.f;
+    if ((unsigned)t < (unsigned)V) {
+#pragma unroll
+        for (int k = 0; k < kFwdPieces; ++k)
+            if (c0 + k * 64 * VEC < D) q[k] = load_vec<VEC>(table, (size_t)t * D + c0 + k * 64 * VEC);
+#pragma unroll
+        for (int k = 0; k < kFwdPieces; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) q[k].v[j] *= scale;
+    }
+#pragma unroll
+    for (int k = 0; k < kFwdPieces; ++k)
+        if (c0 + k * 64 * VEC < D) store_vec<VEC>(out, (size_t)n * D + c0 + k * 64 * VEC, q[k]);
+}
+
+// ---- backward --------------------------------------------------------------------------------------------------------
+constexpr int kRun = 32;              // tokens per part of a long run; longer runs than this are long
+constexpr int kSortWaves = 8;
+constexpr int kSortMinWords = 64, kSortMaxWords = 1024;      // 32 KB of counters at most
+
+// Words per block of the sort: about 512 blocks, so that reading the tokens once per block stays small against the rows.
+static int sort_words(int V) {
+    int r = kSortMinWords;
+    while (r < kSortMaxWords && (long long)r * 512 < V) r *= 2;
+    return r;
+}
+
+// order[p] = token's place n, word[p] = its word, for sorted positions p; first[v] = position of word v's first token, first[V] = number of
+// tokens that are words.  s_count: kSortWaves x R counters, in turn: tokens per wave and word, then the next position of each.
+__global__ __launch_bounds__(64 * kSortWaves) void k_embed_sort(const int *__restrict__ tokens, int N, int V, int R, int bits,
+                                                                int *__restrict__ order, int *__restrict__ word,
+                                                                int *__restrict__ first) {
+    extern __shared__ int s_count[];
+    __shared__ int s_before[kSortWaves], s_total;
+    const int lane = lane_id(), w = wave_id(), v0 = blockIdx.x * R;
+    const int share = ((N + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;      // a wave's tokens: whole groups of 64
+    const int begin = min(N, w * share), end = min(N, begin + share);
+    for (int i = threadIdx.x; i < kSortWaves * R; i += 64 * kSortWaves) s_count[i] = 0;
+    __syncthreads();
+    int *mine = s_count + w * R;
+    int before = 0;
+    constexpr int U = 8;
+    for (int i0 = begin; i0 < end; i0 += 64 * U) {
+        int t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = i0 + 64 * u + lane < end ? tokens[i0 + 64 * u + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            before += (unsigned)t[u] < (unsigned)v0 ? 1 : 0;
+            if (t[u] >= v0 && t[u] - v0 < R && t[u] < V) atomicAdd(&mine[t[u] - v0], 1);
+        }
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
+    if (lane == 0) s_before[w] = before;
+    __syncthreads();
+    if (w == 0) {                                                              // positions, in the order of words, then of waves
+        int base = 0;
+#pragma unroll
+        for (int k = 0; k < kSortWaves; ++k) base += s_before[k];
+        const int per = R / 64, r0 = lane * per;
+        int sum = 0;
+        for (int r = r0; r < r0 + per; ++r)
+            for (int k = 0; k < kSortWaves; ++k) sum += s_count[k * R + r];
+        int upto = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_up(upto, off);
+            if (lane >= off) upto += x;
+        }
+        int at = base + upto - sum;
+        for (int r = r0; r < r0 + per; ++r) {
+            if (v0 + r < V) first[v0 + r] = at;
+            for (int k = 0; k < kSortWaves; ++k) {
+                const int x = s_count[k * R + r];
+                s_count[k * R + r] = at;
+                at += x;
+            }
+        }
+        if (lane == 63) {
+            if (v0 + R >= V) first[V] = at;
+            s_total = at - base;
+        }
+    }
+    __syncthreads();
+    if (s_total == 0) return;
+    volatile int *next = mine;
+    for (int i0 = begin; i0 < end; i0 += 64 * U) {
+        int t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) t[u] = i0 + 64 * u + lane < end ? tokens[i0 + 64 * u + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool in = t[u] >= v0 && t[u] - v0 < R && t[u] < V;
+            unsigned long long same = __ballot(in);
+            if (same == 0) continue;
+            const int r = in ? t[u] - v0 : 0;
+            for (int b = 0; b < bits; ++b) {                                   // lanes with the same word
+                const unsigned long long ones = __ballot((r >> b) & 1);
+                same &= (r >> b) & 1 ? ones : ~ones;
+            }
+            if (in) {
+                const int rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+                const int p = next[r] + rank;                                  // read by all lanes before the first of each word adds
+                order[p] = i0 + 64 * u + lane;
+                word[p] = t[u];
+                if (rank == 0) next[r] = p + __builtin_popcountll(same);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// rows order[p0 .. p1) of dout, columns c .. c + VEC, added in order
+template <typename T, int VEC>
+__device__ __forceinline__ Quad<VEC> add_rows(const T *dout, const int *order, int p0, int p1, int D, int c) {
+    Quad<VEC> sum;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum.v[j] = 0.f;
+    int p = p0;
+    for (; p + 8 <= p1; p += 8) {
+        Quad<VEC> x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = load_vec<VEC>(dout, (size_t)order[p + u] * D + c);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum.v[j] += x[u].v[j];
+    }
+    for (; p < p1; ++p) {
+        const Quad<VEC> x = load_vec<VEC>(dout, (size_t)order[p] * D + c);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) sum.v[j] += x.v[j];
+    }
+    return sum;
+}
+
+template <int VEC> __device__ __forceinline__ void put_row(float *dtable, size_t i, Quad<VEC> q, float scale, bool acc) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) q.v[j] *= scale;
+    if (acc) {
+        const Quad<VEC> old = load_vec<VEC>(dtable, i);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) q.v[j] += old.v[j];
+    }
+    store_vec<VEC>(dtable, i, q);
+}
+
+// Blocks of four waves: first those of the groups of kRun sorted tokens, then those of the words.
+// parts: two rows of pitch P per group: 0 the long run that holds the group's first token, 1 the long run that begins behind it
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_embed_sum(const T *__restrict__ dout, const int *__restrict__ order,
+                                                   const int *__restrict__ word, const int *__restrict__ first, float scale,
+                                                   float *__restrict__ dtable, float *__restrict__ parts, int V, int D, int P,
+                                                   int groups, int group_blocks, bool acc) {
+    if ((int)blockIdx.x < group_blocks) {
+        const int g = blockIdx.x * 4 + wave_id();
+        if (g >= groups) return;
+        const int total = first[V], p0 = g * kRun;
+        if (p0 >= total) return;
+        const int p1 = min(p0 + kRun, total), a = word[p0], b = word[p1 - 1];
+        const int a1 = first[a + 1], b0 = first[b];
+        float *to = parts + (size_t)g * 2 * P;
+        if (a1 - first[a] > kRun)
+            for (int c = lane_id() * VEC; c < D; c += 64 * VEC) store_vec<VEC>(to, c, add_rows<T, VEC>(dout, order, p0, min(p1, a1), D, c));
+        if (b != a && first[b + 1] - b0 > kRun)
+            for (int c = lane_id() * VEC; c < D; c += 64 * VEC) store_vec<VEC>(to + P, c, add_rows<T, VEC>(dout, order, b0, p1, D, c));
+        return;
+    }
+    const long long v = (long long)((int)blockIdx.x - group_blocks) * 4 + wave_id();
+    if (v >= V) return;
+    const int p0 = first[v], p1 = first[v + 1];
+    if (p1 - p0 > kRun || (acc && p1 == p0)) return;
+    for (int c = lane_id() * VEC; c < D; c += 64 * VEC)
+        put_row<VEC>(dtable, (size_t)v * D + c, add_rows<T, VEC>(dout, order, p0, p1, D, c), scale, acc);
+}
+
+// A block per group and 64 VEC columns: the long run that begins in the group, if there is one.  The four waves add a quarter of
+// its parts each, in order.
+template <int VEC>
+__global__ __launch_bounds__(256) void k_embed_join(const int *__restrict__ word, const int *__restrict__ first, float scale,
+                                                    const float *__restrict__ parts, float *__restrict__ dtable, int V, int D,
+                                                    int P, bool acc) {
+    const int g = blockIdx.x, total = first[V], p0 = g * kRun;
+    if (p0 >= total) return;
+    const int v = word[min(p0 + kRun, total) - 1];        // a long run that begins here reaches past the group: it holds the last token
+    const int begin = first[v], end = first[v + 1];
+    if (end - begin <= kRun || begin < p0) return;        // (begin < p0: it began in an earlier group)
+    __shared__ Quad<VEC> s_sum[4][64];
+    const int w = wave_id(), lane = lane_id(), c = (int)blockIdx.y * 64 * VEC + lane * VEC;
+    const int last = (end - 1) / kRun, n = last - g + 1, share = (n + 3) / 4;
+    Quad<VEC> sum;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum.v[j] = 0.f;
+    if (c < D) {
+        const int k1 = min(n, (w + 1) * share);
+        for (int k0 = w * share; k0 < k1; k0 += 8) {
+            Quad<VEC> x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int k = min(k0 + u, k1 - 1);
+                x[u] = load_vec<VEC>(parts, ((size_t)(g + k) * 2 + (k == 0 && begin != p0 ? 1 : 0)) * P + c);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (k0 + u < k1)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) sum.v[j] += x[u].v[j];
+        }
+    }
+    s_sum[w][lane] = sum;
+    __syncthreads();
+    if (w == 0 && c < D) {
+        sum = s_sum[0][lane];
+#pragma unroll
+        for (int k = 1; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum.v[j] += s_sum[k][lane].v[j];
+        put_row<VEC>(dtable, (size_t)v * D + c, sum, scale, acc);
+    }
+}
+
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+struct EmbedWs {
+    size_t order, word, first, parts, total;
+    int groups, pitch;
+};
+static EmbedWs embed_layout(const echo_vocab_desc_t &d) {
+    EmbedWs w;
+    w.groups = (d.N + kRun - 1) / kRun;
+    w.pitch = (d.D + 3) / 4 * 4;
+    w.order = 0;
+    w.word = w.order + up256((size_t)d.N * 4);
+    w.first = w.word + up256((size_t)d.N * 4);
+    w.parts = w.first + up256(((size_t)d.V + 1) * 4);
+    w.total = w.parts + (size_t)w.groups * 2 * w.pitch * 4;
+    return w;
+}
+
+static echo_status_t check_embed(const echo_vocab_desc_t *d, float scale) {
+    if (!d) return ECHO_ERR_NULL;
+    if ((d->in_dtype != ECHO_F32 && d->in_dtype != ECHO_BF16) || (d->out_dtype != ECHO_F32 && d->out_dtype != ECHO_BF16)) return ECHO_ERR_DTYPE;
+    if (d->N < 1 || d->V < 1 || d->D < 1 || d->N > ECHO_VOCAB_MAX_ROWS || d->V > ECHO_VOCAB_MAX_ROWS || d->D > ECHO_VOCAB_MAX_D) return ECHO_ERR_SHAPE;
+    if (!(scale - scale == 0.f)) return ECHO_ERR_SHAPE;                        // infinite or NaN
+    return ECHO_OK;
+}
+
+template <typename TI, typename TO>
+static void embed_fwd_launch(const echo_vocab_desc_t &d, const int *tokens, const void *table, float scale, void *out, hipStream_t st) {
+    const TI *e = static_cast<const TI *>(table);
+    TO *o = static_cast<TO *>(out);
+    const int vec = d.D % 4 == 0 ? 4 : 1, width = kFwdPieces * 64 * vec;
+    const dim3 grid((d.N + 3) / 4, (d.D + width - 1) / width);
+    if (vec == 4) k_embed_fwd<TI, TO, 4><<<grid, 256, 0, st>>>(tokens, e, scale, o, d.N, d.V, d.D);
+    else k_embed_fwd<TI, TO, 1><<<grid, 256, 0, st>>>(tokens, e, scale, o, d.N, d.V, d.D);
+}
+
+template <typename T, int VEC>
+static void embed_sum_launch(const echo_vocab_desc_t &d, const EmbedWs &w, const void *dout, const int *order, const int *word,
+                             const int *first, float scale, float *dtable, float *parts, bool acc, hipStream_t st) {
+    const int group_blocks = (w.groups + 3) / 4, word_blocks = (d.V + 3) / 4;
+    k_embed_sum<T, VEC><<<group_blocks + word_blocks, 256, 0, st>>>(static_cast<const T *>(dout), order, word, first, scale, dtable, parts,
+                                                                    d.V, d.D, w.pitch, w.groups, group_blocks, acc);
+}
+
+static echo_status_t embed_bwd_impl(const echo_vocab_desc_t *desc, const int32_t *tokens, const void *dout, float scale, float *dtable,
+                                    void *workspace, size_t workspace_bytes, bool acc, void *stream) {
+    if (echo_status_t s = check_embed(desc, scale)) return s;
+    if (!tokens || !dout || !dtable || !workspace) return ECHO_ERR_NULL;
+    if (((uintptr_t)tokens | (uintptr_t)dout | (uintptr_t)dtable | (uintptr_t)workspace) & 15u) return ECHO_ERR_ALIGN;
+    const echo_vocab_desc_t d = *desc;
+    const EmbedWs w = embed_layout(d);
+    if (workspace_bytes < w.total) return ECHO_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char *ws = static_cast<char *>(workspace);
+    int *order = reinterpret_cast<int *>(ws + w.order), *word = reinterpret_cast<int *>(ws + w.word), *first = reinterpret_cast<int *>(ws + w.first);
+    float *parts = reinterpret_cast<float *>(ws + w.parts);
+    const int R = sort_words(d.V), bits = 31 - __builtin_clz((unsigned)R);
+    LaunchRecord r = launch_begin("embed_sort", st);
+    k_embed_sort<<<(d.V + R - 1) / R, 64 * kSortWaves, (size_t)kSortWaves * R * 4, st>>>(tokens, d.N, d.V, R, bits, order, word, first);
+    if (echo_status_t s = launch_end(r)) return s;
+    r = launch_begin("embed_sum", st);
+    const bool quads = d.D % 4 == 0;
+    if (d.out_dtype == ECHO_F32) {
+        if (quads) embed_sum_launch<float, 4>(d, w, dout, order, word, first, scale, dtable, parts, acc, st);
+        else embed_sum_launch<float, 1>(d, w, dout, order, word, first, scale, dtable, parts, acc, st);
+    } else {
+        if (quads) embed_sum_launch<bf16_t, 4>(d, w, dout, order, word, first, scale, dtable, parts, acc, st);
+        else embed_sum_launch<bf16_t, 1>(d, w, dout, order, word, first, scale, dtable, parts, acc, st);
+    }
+    if (echo_status_t s = launch_end(r)) return s;
+    if (d.N <= kRun) return ECHO_OK;                                           // no run is long
+    r = launch_begin("embed_join", st);
+    if (quads) k_embed_join<4><<<dim3(w.groups, (d.D + 255) / 256), 256, 0, st>>>(word, first, scale, parts, dtable, d.V, d.D, w.pitch, acc);
+    else k_embed_join<1><<<dim3(w.groups, (d.D + 63) / 64), 256, 0, st>>>(word, first, scale, parts, dtable, d.V, d.D, w.pitch, acc);
+    return launch_end(r);
+}
+
+}  // namespace echo
+
+extern "C" {
+
+echo_status_t echo_embed_fwd(const echo_vocab_desc_t *desc, const int32_t *tokens, const void *table, float scale, void *out,
+                             void *stream) {
+    if (echo_status_t s = echo::check_embed(desc, scale)) return s;
+    if (!tokens || !table || !out) return ECHO_ERR_NULL;
+    if (((uintptr_t)tokens | (uintptr_t)table | (uintptr_t)out) & 15u) return ECHO_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    echo::LaunchRecord r = echo::launch_begin("embed_fwd", st);
+    const bool ib = desc->in_dtype == ECHO_BF16, ob = desc->out_dtype == ECHO_BF16;
+    if (ib && ob) echo::embed_fwd_launch<echo::bf16_t, echo::bf16_t>(*desc, tokens, table, scale, out, st);
+    else if (ib) echo::embed_fwd_launch<echo::bf16_t, float>(*desc, tokens, table, scale, out, st);
+    else if (ob) echo::embed_fwd_launch<float, echo::bf16_t>(*desc, tokens, table, scale, out, st);
+    else echo::embed_fwd_launch<float, float>(*desc, tokens, table, scale, out, st);
+    return echo::launch_end(r);
+}
+
+size_t echo_embed_bwd_workspace_bytes(const echo_vocab_desc_t *desc) {
+    if (echo::check_embed(desc, 1.f)) return 0;
+    return echo::embed_layout(*desc).total;
+}
+
+echo_status_t echo_embed_bwd(const echo_vocab_desc_t *desc, const int32_t *tokens, const void *dout, float scale, float *dtable,
+                             void *workspace, size_t workspace_bytes, void *stream) {
+    return echo::embed_bwd_impl(desc, tokens, dout, scale, dtable, workspace, workspace_bytes, false, stream);
+}
+
+echo_status_t echo_embed_bwd_accumulate(const echo_vocab_desc_t *desc, const int32_t *tokens, const void *dout, float scale,
+                                        float *dtable, void *workspace, size_t workspace_bytes, void *stream) {
+    return echo::embed_bwd_impl(desc, tokens, dout, scale, dtable, workspace, workspace_bytes, true, stream);
+}
+
+}  // extern "C"

@@ -19,13 +19,17 @@
 #include <tuple>
 #include <utility>
 
+#include "../../include/echoclip.h"
 #include "../../include/echodropout.h"
 #include "../../include/echolstm.h"
+#include "../../include/echovocab.h"
 
 namespace {
 
 PyTypeObject *g_desc_type = nullptr;                       // binding.echo_attn_desc_t
-PyObject *g_s_data_ptr, *g_s_is_contiguous, *g_s_cuda_stream, *g_s_numel, *g_s_element_size;
+PyTypeObject *g_vocab_desc_type = nullptr;                 // binding.echo_vocab_desc_t
+PyTypeObject *g_grad_type = nullptr;                       // binding.echo_grad_t
+PyObject *g_s_type, *g_s_data_ptr, *g_s_is_contiguous, *g_s_cuda_stream, *g_s_numel, *g_s_element_size;
 
 bool int_value(PyObject *o, unsigned long long &out) {     // two's complement bits of any integer, as ctypes takes them
     if (!PyLong_Check(o)) {
@@ -47,18 +51,39 @@ bool address_from_attribute(PyObject *o, PyObject *attr, bool call, void *&out) 
 }
 
 // ---- one parameter kind each: how many Python parameters it takes, what it holds, how it is read ----------------
-struct Desc {                                              // echo_attn_desc_t, a ctypes structure
-    using C = const echo_attn_desc_t *;
+template <typename T, PyTypeObject *&TYPE> struct Struct {  // a ctypes structure
+    using C = const T *;
     Py_buffer view{};
     bool read(PyObject *o) {
-        if (!PyObject_TypeCheck(o, g_desc_type)) {
-            PyErr_Format(PyExc_TypeError, "expected echo_attn_desc_t, got %.100s", Py_TYPE(o)->tp_name);
+        if (!PyObject_TypeCheck(o, TYPE)) {
+            PyErr_Format(PyExc_TypeError, "expected %.100s, got %.100s", TYPE->tp_name, Py_TYPE(o)->tp_name);
             return false;
         }
         return PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) == 0;
     }
     C value() const { return static_cast<C>(view.buf); }
-    ~Desc() {
+    ~Struct() {
+        if (view.obj) PyBuffer_Release(&view);
+    }
+};
+using Desc = Struct<echo_attn_desc_t, g_desc_type>;
+using VocabDesc = Struct<echo_vocab_desc_t, g_vocab_desc_type>;
+struct Grads {                                             // a ctypes array of echo_grad_t
+    using C = const echo_grad_t *;
+    Py_buffer view{};
+    bool read(PyObject *o) {
+        PyObject *type = PyObject_GetAttr(o, g_s_type);    // what the array's elements are
+        const bool ok = type == reinterpret_cast<PyObject *>(g_grad_type);
+        if (!type) PyErr_Clear();
+        Py_XDECREF(type);
+        if (!ok) {
+            PyErr_Format(PyExc_TypeError, "expected an array of echo_grad_t (make_grads), got %.100s", Py_TYPE(o)->tp_name);
+            return false;
+        }
+        return PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) == 0;
+    }
+    C value() const { return static_cast<C>(view.buf); }
+    ~Grads() {
         if (view.obj) PyBuffer_Release(&view);
     }
 };
@@ -135,6 +160,13 @@ struct Float {
         return true;
     }
     C value() const { return x; }
+};
+struct Count : Int<int32_t> {                              // number of elements of the array in front of this one
+    bool resolve(PyObject *array) {
+        const Py_ssize_t n = PyObject_Size(array);
+        if (n >= 0 && x > n) PyErr_Format(PyExc_ValueError, "count %d of an array of %zd", (int)x, n);
+        return n >= 0 && x <= n;
+    }
 };
 struct Bytes {                                             // workspace_bytes; None: what the workspace tensor holds
     using C = size_t;
@@ -219,6 +251,7 @@ bool collect(Names &n, PyObject *const *args, Py_ssize_t nargs, PyObject *kwname
 
 template <typename P> bool resolve_bytes(P &, PyObject *) { return true; }
 bool resolve_bytes(Bytes &b, PyObject *ws) { return b.resolve(ws); }
+bool resolve_bytes(Count &n, PyObject *array) { return n.resolve(array); }
 
 template <typename... K, size_t... I>
 PyObject *call_with(Names &n, PyObject **slot, std::index_sequence<I...>) {
@@ -270,6 +303,13 @@ using LstmFwd = Call<13, I64, I64, InF, InF, InF, OutF, OutF, OutF, Stream>;
 using LstmBwd = Call<14, I64, I64, InF, InF, InF, InF, OutF, OutF, Stream>;
 using LstmFwdStash = Call<15, I64, I64, InF, InF, InF, OutF, OutF, OutF, OutF, Stream>;
 using LstmBwdStash = Call<16, I64, I64, InF, InF, InF, InF, InF, OutF, OutF, Stream>;
+using EmbedFwd = Call<17, VocabDesc, Len, In, Float, Work, Stream>;
+using EmbedBwd = Call<18, VocabDesc, Len, In, Float, OutF, Work, Bytes, Stream>;
+using EmbedBwdAccumulate = Call<19, VocabDesc, Len, In, Float, OutF, Work, Bytes, Stream>;
+using VocabLossFwd = Call<20, VocabDesc, In, In, Len, Float, OutF, OutF, Work, Bytes, Stream>;
+using VocabLossBwd = Call<21, VocabDesc, InF, InF, In, In, Len, Float, Work, Work, Work, Bytes, Stream>;
+using GradNorm = Call<22, Grads, Count, OutF, Work, Bytes, Stream>;
+using GradClip = Call<23, Grads, Count, Float, OutF, Work, Bytes, Stream>;
 
 #define NAMES(CALL, FN, REQUIRED, ...) template <> Names CALL::names = {FN, {__VA_ARGS__, nullptr}, REQUIRED, {}, 0, nullptr}
 NAMES(Fwd, "echo_attn_fwd", 9, "desc", "Qp", "Kp", "V", "v", "key_len", "context", "P", "workspace", "workspace_bytes", "stream");
@@ -297,26 +337,41 @@ NAMES(LstmFwd, "echo_lstm_cell_fwd", 8, "B", "H", "Gx", "Gh", "c_prev", "h", "c"
 NAMES(LstmBwd, "echo_lstm_cell_bwd", 8, "B", "H", "dh", "dc", "a", "c_prev", "da", "dc_prev", "stream");
 NAMES(LstmFwdStash, "echo_lstm_cell_fwd_stash", 9, "B", "H", "Gx", "Gh", "c_prev", "h", "c", "acts", "tanh_c", "stream");
 NAMES(LstmBwdStash, "echo_lstm_cell_bwd_stash", 9, "B", "H", "dh", "dc", "acts", "tanh_c", "c_prev", "da", "dc_prev", "stream");
+NAMES(EmbedFwd, "echo_embed_fwd", 5, "desc", "tokens", "table", "scale", "out", "stream");
+NAMES(EmbedBwd, "echo_embed_bwd", 6, "desc", "tokens", "dout", "scale", "dtable", "workspace", "workspace_bytes", "stream");
+NAMES(EmbedBwdAccumulate, "echo_embed_bwd_accumulate", 6, "desc", "tokens", "dout", "scale", "dtable", "workspace", "workspace_bytes",
+      "stream");
+NAMES(VocabLossFwd, "echo_vocab_loss_fwd", 8, "desc", "h", "W", "labels", "label_smoothing", "loss", "lse", "workspace", "workspace_bytes",
+      "stream");
+NAMES(VocabLossBwd, "echo_vocab_loss_bwd", 10, "desc", "dloss", "lse", "h", "W", "labels", "label_smoothing", "dh", "dW", "workspace",
+      "workspace_bytes", "stream");
+NAMES(GradNorm, "echo_grad_norm", 4, "grads", "count", "norm", "workspace", "workspace_bytes", "stream");
+NAMES(GradClip, "echo_grad_clip", 5, "grads", "count", "max_norm", "norm", "workspace", "workspace_bytes", "stream");
 #undef NAMES
 
 Names *const kAll[] = {&Fwd::names, &Bwd::names, &BwdStatic::names, &BwdAccumulate::names, &StepFwd::names, &StepBwd::names,
                        &StepFinish::names, &StepBwdQuery::names, &StepsBwdKeys::names, &FwdStash::names, &BwdStash::names,
                        &DropoutFwd::names, &DropoutBwd::names, &LstmFwd::names, &LstmBwd::names, &LstmFwdStash::names,
-                       &LstmBwdStash::names};
+                       &LstmBwdStash::names, &EmbedFwd::names, &EmbedBwd::names, &EmbedBwdAccumulate::names,
+                       &VocabLossFwd::names, &VocabLossBwd::names, &GradNorm::names, &GradClip::names};
 
-// bind(desc_type, {name: address of the loaded library's function}): the names that are not in the dict raise when called
+// bind(desc_type, vocab_desc_type, grad_type, {name: address of the loaded library's function}): the names that are not in the dict raise when called
 PyObject *bind(PyObject *, PyObject *args) {
-    PyObject *type = nullptr, *addresses = nullptr;
-    if (!PyArg_ParseTuple(args, "O!O!", &PyType_Type, &type, &PyDict_Type, &addresses)) return nullptr;
+    PyObject *type[3] = {}, *addresses = nullptr;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!", &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2], &PyDict_Type, &addresses))
+        return nullptr;
     for (Names *n : kAll) {
         PyObject *a = PyDict_GetItemString(addresses, n->fn);        // borrowed
         unsigned long long x = 0;
         if (a && !int_value(a, x)) return nullptr;
         n->target = reinterpret_cast<void *>(x);
     }
-    Py_INCREF(type);
-    Py_XDECREF(reinterpret_cast<PyObject *>(g_desc_type));
-    g_desc_type = reinterpret_cast<PyTypeObject *>(type);
+    PyTypeObject **const to[3] = {&g_desc_type, &g_vocab_desc_type, &g_grad_type};
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(type[i]);
+        Py_XDECREF(reinterpret_cast<PyObject *>(*to[i]));
+        *to[i] = reinterpret_cast<PyTypeObject *>(type[i]);
+    }
     Py_RETURN_NONE;
 }
 
@@ -325,7 +380,8 @@ PyObject *bind(PyObject *, PyObject *args) {
 PyMethodDef g_methods[] = {METHOD(Fwd), METHOD(Bwd), METHOD(BwdStatic), METHOD(BwdAccumulate), METHOD(StepFwd), METHOD(StepBwd),
                            METHOD(StepFinish), METHOD(StepBwdQuery), METHOD(StepsBwdKeys), METHOD(FwdStash), METHOD(BwdStash),
                            METHOD(DropoutFwd), METHOD(DropoutBwd), METHOD(LstmFwd), METHOD(LstmBwd), METHOD(LstmFwdStash),
-                           METHOD(LstmBwdStash), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                           METHOD(LstmBwdStash), METHOD(EmbedFwd), METHOD(EmbedBwd), METHOD(EmbedBwdAccumulate),
+                           METHOD(VocabLossFwd), METHOD(VocabLossBwd), METHOD(GradNorm), METHOD(GradClip), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_py_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -338,11 +394,12 @@ PyMODINIT_FUNC PyInit__py_calls() {
             n->interned[n->count] = PyUnicode_InternFromString(n->param[n->count]);
             if (!n->interned[n->count]) return nullptr;
         }
+    g_s_type = PyUnicode_InternFromString("_type_");
     g_s_data_ptr = PyUnicode_InternFromString("data_ptr");
     g_s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     g_s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     g_s_numel = PyUnicode_InternFromString("numel");
     g_s_element_size = PyUnicode_InternFromString("element_size");
-    if (!g_s_data_ptr || !g_s_is_contiguous || !g_s_cuda_stream || !g_s_numel || !g_s_element_size) return nullptr;
+    if (!g_s_type || !g_s_data_ptr || !g_s_is_contiguous || !g_s_cuda_stream || !g_s_numel || !g_s_element_size) return nullptr;
     return PyModule_Create(&g_module);
 }

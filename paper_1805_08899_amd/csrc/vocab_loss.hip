@@ -1,0 +1,698 @@
+// Softmax cross entropy over a vocabulary without kept logits, and its gradients (include/echovocab.h has the formulas).
+//
+//   rows, pack   the rows with a label are gathered (whoever has none takes part in nothing) and stored as bf16 planes; f32 words too, piece by piece
+//   logits       z = W h^T tile by tile on the matrix cores; a tile never leaves its block:
+//                  forward   maximum and sum of exponentials of its 128 or 256 words but the label, for label smoothing their sum, for every row; the
+//                            label's logit
+//                  backward  dz = dloss (exp(z - lse) - target) of one piece of the vocabulary, as bf16 planes
+//   finish       joins a row's tiles: loss and lse
+//   grads        dW of the piece = dz^T h, dh += dz W, both kinds of tiles in one launch
+//   dh finish    puts the sums of dh into the rows' places
+//
+// Bound by the matrix cores: 2 N V D forward, 8 N V D for both directions (the logits are formed twice, as the tanh map of the attention is: to keep
+// them would take 4 N V bytes written and read twice), times the number of plane pairs (product.hpp, split.hpp).
+#include "../../include/echovocab.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "common.hpp"
+#include "kernels.hpp"
+#include "launch.hpp"
+#include "product.hpp"
+
+namespace echo {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kDzScale = 0x1p24f;                   // on dz while it is in bf16 planes: small probabilities keep their digits (split.hpp)
+
+typedef TileConfig<256, 256, 4, 2, 2> BigTile;
+typedef TileConfig<128, 128, 2, 2, 2> MidTile;
+
+// ---- rows with a label ------------------------------------------------------------------------------------------------
+// rows[p] = n of the p-th row with a label, place[n] = p or -1, count[0] = their number.  A block writes kRowsBlock labels' entries and
+// counts all labels in front of them by itself.
+constexpr int kRowsBlock = 2048;
+__global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labels, int N, int V, int *__restrict__ rows,
+                                                    int *__restrict__ place, int *__restrict__ count) {
+    __shared__ int s_wave[4];
+    const int lane = lane_id(), w = wave_id(), begin = blockIdx.x * kRowsBlock;
+    int before = 0;
+    for (int i = threadIdx.x * 4; i < begin; i += 1024) {
+        const int4 t = *reinterpret_cast<const int4 *>(labels + i);
+        before += ((unsigned)t.x < (unsigned)V) + ((unsigned)t.y < (unsigned)V) + ((unsigned)t.z < (unsigned)V) + ((unsigned)t.w < (unsigned)V);
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) before += __shfl_xor(before, off);
+    if (lane == 0) s_wave[w] = before;
+    __syncthreads();
+    int at = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+    constexpr int U = kRowsBlock / 256;
+    int t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) t[u] = begin + u * 256 + (int)threadIdx.x < N ? labels[begin + u * 256 + threadIdx.x] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const bool in = (unsigned)t[u] < (unsigned)V;
+        const unsigned long long m = __ballot(in);
+        __syncthreads();
+        if (lane == 0) s_wave[w] = __builtin_popcountll(m);
+        __syncthreads();
+        int p = at + __builtin_popcountll(m & ((1ull << lane) - 1));
+        for (int k = 0; k < w; ++k) p += s_wave[k];
+        const int n = begin + u * 256 + threadIdx.x;
+        if (in) rows[p] = n;
+        if (n < N) place[n] = in ? p : -1;
+        at += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) count[0] = at;
+}
+
+// ---- bf16 planes ------------------------------------------------------------------------------------------------------
+// dst: planes of `pitch` elements a row, zeros behind D.  Row r of dst is row list[r] of src (r < *count), or row first + r
+// (r < n_rows).  A thread takes eight columns.
+__device__ __forceinline__ void split_planes(float x, unsigned short (&p)[3]) {
+    p[0] = __builtin_bit_cast(unsigned short, (__bf16)x);
+    x -= __uint_as_float((unsigned)p[0] << 16);
+    p[1] = __builtin_bit_cast(unsigned short, (__bf16)x);
+    x -= __uint_as_float((unsigned)p[1] << 16);
+    p[2] = __builtin_bit_cast(unsigned short, (__bf16)x);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_pack(const T *__restrict__ src, int D, const int *__restrict__ list,
+                                                    const int *__restrict__ count, int first, int n_rows, bf16_t *__restrict__ dst,
+                                                    int pitch, size_t plane) {
+    const int per_row = pitch / 8, r = blockIdx.x * 4 + wave_id();
+    if (r >= (count ? *count : n_rows)) return;
+    const size_t from = (size_t)(list ? list[r] : first + r) * D;
+    for (int g = lane_id(); g < per_row; g += 64) {
+        const int c = 8 * g;
+        if constexpr (sizeof(T) == 2) {
+            u32x4 u = {0, 0, 0, 0};
+            if (D % 8 == 0) {
+                u = *reinterpret_cast<const u32x4 *>(src + from + c);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < D) u[j / 2] |= (unsigned)src[from + c + j].bits << (16 * (j & 1));
+            }
+            *reinterpret_cast<u32x4 *>(dst + (size_t)r * pitch + c) = u;
+        } else {
+            float x[8];
+            if (D % 4 == 0) {
+                const float4 a = ld4(src, from + c), b = c + 4 < D ? ld4(src, from + c + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = c + j < D ? src[from + c + j] : 0.f;
+            }
+            unsigned short p[8][3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) split_planes(x[j], p[j]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                u32x4 u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[j] = (unsigned)p[2 * j][k] | (unsigned)p[2 * j + 1][k] << 16;
+                *reinterpret_cast<u32x4 *>(dst + k * plane + (size_t)r * pitch + c) = u;
+            }
+        }
+    }
+}
+
+// ---- order of the tiles -------------------------------------------------------------------------------------------------
+// Tile of block b of a grid of at least tm tn blocks: consecutive tiles to the same XCD (blocks are dealt to the 8 XCDs in turn), and
+// among them groups of 8 rows of tiles, column by column, so that what runs at the same time shares operands in the XCD's L2.
+__device__ __forceinline__ bool tile_of_block(int b, int tm, int tn, int &im, int &in) {
+    const int total = tm * tn, q = total / 8, rem = total % 8, x = b % 8, k = b / 8;
+    if (k >= q + (x < rem ? 1 : 0)) return false;
+    const int id = x * q + min(x, rem) + k;
+    constexpr int G = 8;
+    const int first = id / (G * tn) * G, size = min(G, tm - first), r = id - first * tn;
+    im = first + r % size;
+    in = r / size;
+    return true;
+}
+
+// ---- logits -----------------------------------------------------------------------------------------------------------
+struct LogitsArgs {
+    Operand W, h;                    // words of this piece; gathered rows
+    int D;
+    PlanePairs pairs;
+    const int *count, *rows, *labels;
+    int V, v0;                       // words of the vocabulary; this piece's first word
+    float eps;                       // label smoothing
+    // forward: [tiles][pitch] maximum, sum, sum of logits; the label's logit
+    float *part_max, *part_sum, *part_z, *z_label;
+    int first_tile;
+    size_t pitch;
+    // backward
+    const float *lse, *dloss;
+    bf16_t *dz;
+    size_t dz_plane;
+    int dz_pitch, dz_planes;
+};
+
+// a sum of exponentials relative to `from`, relative to `to` >= from (both may be minus infinity: an empty sum)
+__device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
+    return from == to ? sum : sum * fast_exp2((from - to) * kLog2e);
+}
+
+template <class C, bool BWD>
+__global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
+    extern __shared__ __align__(16) char lds[];
+    const int count = *a.count;
+    int im, in;
+    if (!tile_of_block(blockIdx.x, (a.W.rows + C::BM - 1) / C::BM, (count + C::BN - 1) / C::BN, im, in)) return;
+    const int m0 = im * C::BM, n0 = in * C::BN;
+    f32x16 acc[C::TM][C::TN];
+    Operand h = a.h;
+    h.rows = count;
+    tile_product<C, false, false>(acc, a.W, h, m0, n0, 0, a.D, a.pairs, lds);
+    block_barrier();                                                           // LDS has another use from here on
+    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
+    const int vw = a.v0 + m0 + wm * C::TM * 32;                                // this wave's first word
+    const bool tail = a.v0 + m0 + C::BM > a.V;
+    if constexpr (!BWD) {
+        float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+            const int nt = (wn * C::TN + j) * 32 + (lane & 31), n = n0 + nt;
+            const int y = n < count ? a.labels[a.rows[n]] - vw : -1;
+            float z = 0.f;
+            if (a.eps > 0.f) {
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z += !tail || vw + i * 32 + mfma32_row(r, lane) < a.V ? acc[i][j][r] : 0.f;
+                z += __shfl_xor(z, 32);
+            }
+            const bool here = y >= 0 && y < C::TM * 32;
+            if (__ballot(here)) {             // the label's logit: the lane that holds it writes it and leaves it out of maximum and sum
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (here && y == i * 32 + mfma32_row(r, lane)) {
+                            a.z_label[n] = acc[i][j][r];
+                            acc[i][j][r] = -__builtin_inff();
+                        }
+            }
+            if (tail) {
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (vw + i * 32 + mfma32_row(r, lane) >= a.V) acc[i][j][r] = -__builtin_inff();
+            }
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float at = top == -__builtin_inff() ? 0.f : top;             // nothing but the label and words past the end
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += fast_exp2((acc[i][j][r] - at) * kLog2e);
+            sum += __shfl_xor(sum, 32);
+            if (lane < 32) {
+                s_max[wm * C::BN + nt] = top;
+                s_sum[wm * C::BN + nt] = sum;
+                s_z[wm * C::BN + nt] = z;
+            }
+        }
+        __syncthreads();
+        for (int nt = threadIdx.x; nt < C::BN; nt += C::THREADS) {
+            if (n0 + nt >= count) break;
+            float top = s_max[nt], z = 0.f, sum = 0.f;
+#pragma unroll
+            for (int k = 1; k < C::WM; ++k) top = fmaxf(top, s_max[k * C::BN + nt]);
+#pragma unroll
+            for (int k = 0; k < C::WM; ++k) {
+                sum += scaled_sum(s_sum[k * C::BN + nt], s_max[k * C::BN + nt], top);
+                z += s_z[k * C::BN + nt];
+            }
+            const size_t at = (size_t)(a.first_tile + im) * a.pitch + n0 + nt;
+            a.part_max[at] = top;
+            a.part_sum[at] = sum;
+            if (a.eps > 0.f) a.part_z[at] = z;
+        }
+    } else {
+        const float off = 1.0f - a.eps, low = a.eps / (float)a.V;
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+            const int n = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+            const bool row = n < count;
+            const int at = row ? a.rows[n] : 0;
+            const int y = row ? a.labels[at] - vw : -1;
+            const float lse = row ? a.lse[at] : 0.f, g = row ? a.dloss[at] * kDzScale : 0.f;
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int v = i * 32 + mfma32_row(r, lane);
+                    const float p = fast_exp2((acc[i][j][r] - lse) * kLog2e) - (v == y ? off + low : low);
+                    acc[i][j][r] = vw + v < a.V ? p * g : 0.f;
+                }
+        }
+        // rows of dz through LDS, a plane at a time: each wave writes four words per lane and reads whole rows
+        constexpr int PITCH = C::BM * 2 + 16;                                  // bytes; 16 more per row spread the rows over the banks
+        for (int k = 0; k < a.dz_planes; ++k) {
+            if (k > 0) lds_barrier();
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) {
+                const int nt = (wn * C::TN + j) * 32 + (lane & 31);
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        u32x2 u;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const float x0 = acc[i][j][4 * q + 2 * e], x1 = acc[i][j][4 * q + 2 * e + 1];
+                            const unsigned b = bf16_pair(x0, x1);
+                            acc[i][j][4 * q + 2 * e] = x0 - __uint_as_float(b << 16);
+                            acc[i][j][4 * q + 2 * e + 1] = x1 - __uint_as_float(b & 0xffff0000u);
+                            u[e] = b;
+                        }
+                        *reinterpret_cast<u32x2 *>(lds + nt * PITCH + ((wm * C::TM + i) * 32 + 8 * q + 4 * (lane >> 5)) * 2) = u;
+                    }
+            }
+            lds_barrier();
+            bf16_t *out = a.dz + k * a.dz_plane + (size_t)n0 * a.dz_pitch + m0;
+            for (int c = threadIdx.x; c < C::BN * (C::BM / 8); c += C::THREADS) {
+                const int nt = c / (C::BM / 8), g = c % (C::BM / 8);
+                if (n0 + nt < count && m0 + g * 8 < a.dz_pitch)
+                    *reinterpret_cast<u32x4 *>(out + (size_t)nt * a.dz_pitch + g * 8) = *reinterpret_cast<const u32x4 *>(lds + nt * PITCH + g * 16);
+            }
+        }
+    }
+}
+
+// Joins the tiles of 64 rows: four waves take a quarter of the tiles each, lanes are rows.  Rows without a label get zeros.
+__global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restrict__ part_max, const float *__restrict__ part_sum,
+                                                           const float *__restrict__ part_z, const float *__restrict__ z_label,
+                                                           const int *__restrict__ place, int N, int V, int tiles, size_t pitch,
+                                                           float eps, float *__restrict__ loss, float *__restrict__ lse) {
+    __shared__ float s_max[4][64], s_sum[4][64], s_z[4][64];
+    const int lane = lane_id(), w = wave_id(), n = blockIdx.x * 64 + lane, p = n < N ? place[n] : -1;
+    const int share = (tiles + 3) / 4, t0 = w * share, t1 = min(tiles, t0 + share);
+    float top = -__builtin_inff(), sum = 0.f, z = 0.f;
+    if (p >= 0) {
+        for (int t = t0; t < t1; t += 8) {
+            float m[8], s[8], zz[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const size_t at = (size_t)min(t + u, t1 - 1) * pitch + p;
+                m[u] = part_max[at];
+                s[u] = part_sum[at];
+                zz[u] = eps > 0.f ? part_z[at] : 0.f;
+            }
+            float next = top;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) next = fmaxf(next, m[u]);
+            sum = scaled_sum(sum, top, next);
+            top = next;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (t + u < t1) {
+                    sum += scaled_sum(s[u], m[u], top);
+                    z += zz[u];
+                }
+        }
+    }
+    s_max[w][lane] = top;
+    s_sum[w][lane] = sum;
+    s_z[w][lane] = z;
+    __syncthreads();
+    if (w != 0 || n >= N) return;
+    float l = 0.f, e = 0.f;
+    if (p >= 0) {
+        float all = fmaxf(fmaxf(s_max[0][lane], s_max[1][lane]), fmaxf(s_max[2][lane], s_max[3][lane]));
+        sum = 0.f;
+        z = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sum += scaled_sum(s_sum[k][lane], s_max[k][lane], all);
+            z += s_z[k][lane];
+        }
+        // -log p of the label: log(1 + sum over the other words of exp(z - z_label)), which keeps the digits of a sure label's loss
+        const float zl = z_label[p], t = all - zl;
+        const float nll = t > 0.f ? t + logf(sum + expf(-t)) : log1pf(sum * expf(t));
+        e = zl + nll;
+        l = nll;
+        if (eps > 0.f) l += eps * (zl - z / (float)V);
+    }
+    loss[n] = l;
+    lse[n] = e;
+}
+
+// ---- gradients ----------------------------------------------------------------------------------------------------------
+struct GradsArgs {
+    Operand dz_words, dz_rows;       // dz with its words along m, with its rows along m
+    Operand h, W;                    // rows along k: columns of h and of W along n
+    const int *count;
+    int words, D;                    // of this piece
+    PlanePairs dw_pairs, dh_pairs;
+    void *dW;                        // this piece's first row; or null
+    float *dh_sum;                   // [splits][N][D] sums of dh in the rows' gathered places; or null
+    size_t dh_split;
+    int splits, split_words;         // parts of the piece's words per dh tile, multiples of 64
+    bool bf16_out, add;              // add: not the first piece
+    int dw_blocks;                   // blocks of the first kind
+};
+
+template <class C>
+__global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
+    extern __shared__ __align__(16) char lds[];
+    const int count = *a.count, tn = (a.D + C::BN - 1) / C::BN;
+    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
+    f32x16 acc[C::TM][C::TN];
+    int im, in;
+    if ((int)blockIdx.x < a.dw_blocks) {
+        if (!tile_of_block(blockIdx.x, (a.words + C::BM - 1) / C::BM, tn, im, in)) return;
+        const int m0 = im * C::BM, n0 = in * C::BN;
+        tile_product<C, true, true>(acc, a.dz_words, a.h, m0, n0, 0, count, a.dw_pairs, lds);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane), d = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+                    if (m < a.words && d < a.D) {
+                        const float x = acc[i][j][r] * (1.f / kDzScale);
+                        const size_t at = (size_t)m * a.D + d;
+                        if (a.bf16_out) static_cast<__bf16 *>(a.dW)[at] = (__bf16)x;
+                        else store_streaming(static_cast<float *>(a.dW) + at, x);
+                    }
+                }
+        return;
+    }
+    const int b = blockIdx.x - a.dw_blocks, tm = (count + C::BM - 1) / C::BM;
+    if (!tile_of_block(b, tm * a.splits, tn, im, in)) return;
+    const int split = im / tm, m0 = (im - split * tm) * C::BM, n0 = in * C::BN;
+    const int k0 = split * a.split_words, k1 = min(a.words, k0 + a.split_words);
+    Operand dz = a.dz_rows;
+    dz.rows = count;
+    tile_product<C, false, true>(acc, dz, a.W, m0, n0, k0, max(k0, k1), a.dh_pairs, lds);
+    float *to = a.dh_sum + split * a.dh_split;
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+            float old[16];
+            const int d = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane);
+                old[r] = a.add && m < count && d < a.D ? to[(size_t)m * a.D + d] : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane);
+                if (m < count && d < a.D) to[(size_t)m * a.D + d] = old[r] + acc[i][j][r];
+            }
+        }
+}
+
+// dh[n] = sum of the splits of row place[n], scaled back; zeros for rows without a label.  A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_dh_finish(const float *__restrict__ sums, size_t split, int splits,
+                                                         const int *__restrict__ place, int N, int D, T *__restrict__ dh) {
+    const int n = blockIdx.x * 4 + wave_id();
+    if (n >= N) return;
+    const int p = place[n];
+    for (int c = lane_id(); c < D; c += 64) {
+        float x = 0.f;
+        if (p >= 0)
+            for (int s = 0; s < splits; ++s) x += sums[s * split + (size_t)p * D + c];
+        x *= 1.f / kDzScale;
+        if constexpr (sizeof(T) == 4) dh[(size_t)n * D + c] = x;
+        else dh[(size_t)n * D + c].bits = __builtin_bit_cast(unsigned short, (__bf16)x);
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+static size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+constexpr size_t kPackBytes = (size_t)128 << 20;      // of f32 words' planes at a time
+constexpr size_t kDzBytes = (size_t)256 << 20;        // of dz at a time
+constexpr size_t kMaxTiles = (size_t)1 << 22;         // of 128 x 128 in a launch: a grid has fewer than 2^32 threads
+
+struct VocabPlan {
+    int planes, pitch;                                // of h and, if packed, of W
+    bool pack_words;
+    int piece;                                        // words per piece, a multiple of 256
+    int dz_planes, splits;
+    size_t count, rows, place, hp, wp, part_max, part_sum, part_z, z_label, dz, dh, total;
+    size_t h_plane, w_plane, dz_plane, part_pitch;
+    int tiles;                                        // most tiles along the vocabulary
+};
+
+static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
+    VocabPlan p{};
+    const size_t N = d.N, V = d.V, D = d.D;
+    p.planes = d.in_dtype == ECHO_F32 ? 3 : 1;
+    p.pitch = (int)up(D, 8);
+    p.pack_words = d.in_dtype == ECHO_F32 || D % 8 != 0;
+    p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 2;
+    size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
+    if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
+    if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (2 * p.dz_planes * N) / 256 * 256, 256));
+    p.piece = (int)piece;
+    p.h_plane = N * p.pitch;
+    p.w_plane = piece * p.pitch;
+    p.dz_plane = N * piece;
+    p.part_pitch = up(N, 64);
+    p.tiles = (int)(up(V, piece) / piece * (piece / 128));
+    p.splits = 1;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes, 256);
+        return here;
+    };
+    p.count = take(4);
+    p.rows = take(N * 4);
+    p.place = take(N * 4);
+    p.hp = take(p.planes * p.h_plane * 2);
+    if (p.pack_words) p.wp = take(p.planes * p.w_plane * 2);
+    if (!bwd) {
+        p.part_max = take(p.tiles * p.part_pitch * 4);
+        p.part_sum = take(p.tiles * p.part_pitch * 4);
+        p.part_z = take(p.tiles * p.part_pitch * 4);
+        p.z_label = take(N * 4);
+    } else {
+        p.dz = take(p.dz_planes * p.dz_plane * 2);
+        p.dh = take((size_t)p.splits * N * D * 4);
+    }
+    p.total = at;
+    return p;
+}
+
+static PlanePairs pairs_of(int a, int b) {             // planes of the operands: nibbles, the small terms first
+    if (a == 3 && b == 3) return {6, 0x001021u, 0x010201u};
+    if (a == 3 && b == 1) return {3, 0x012u, 0u};
+    if (a == 2 && b == 1) return {2, 0x01u, 0u};
+    return {1, 0u, 0u};
+}
+
+template <class C> static size_t product_lds() {
+    return std::max<size_t>(C::LDS_BYTES, (size_t)C::BN * (C::BM * 2 + 16));
+}
+
+// Launches a kernel whose LDS is above the default limit.
+template <typename K, typename A>
+static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &granted, size_t lds, long long blocks, int threads, const A &args, hipStream_t st) {
+    LaunchRecord r = launch_begin(name, st);
+    if (ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), lds, granted) == hipSuccess) kernel<<<(unsigned)blocks, threads, lds, st>>>(args);
+    return launch_end(r);
+}
+
+template <class C, bool BWD> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
+    static LdsGrants granted{};
+    const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
+    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, BWD>, granted, product_lds<C>(), blocks, C::THREADS, a, st);
+}
+template <class C> static echo_status_t launch_grads(GradsArgs a, int N, hipStream_t st) {
+    static LdsGrants granted{};
+    const long long tn = (a.D + C::BN - 1) / C::BN;
+    a.dw_blocks = a.dW ? (int)(((a.words + C::BM - 1) / C::BM * tn + 7) / 8 * 8) : 0;
+    const long long blocks = a.dw_blocks + (a.dh_sum ? (N + C::BM - 1) / C::BM * tn * a.splits : 0);
+    return launch_tiles("vocab_grads", &k_vocab_grads<C>, granted, product_lds<C>(), blocks, C::THREADS, a, st);
+}
+
+static echo_status_t check_vocab(const echo_vocab_desc_t *d, float eps) {
+    if (!d) return ECHO_ERR_NULL;
+    if ((d->in_dtype != ECHO_F32 && d->in_dtype != ECHO_BF16) || (d->out_dtype != ECHO_F32 && d->out_dtype != ECHO_BF16)) return ECHO_ERR_DTYPE;
+    if (d->in_dtype == ECHO_F32 && d->out_dtype == ECHO_BF16) return ECHO_ERR_DTYPE;
+    if (d->N < 1 || d->V < 1 || d->D < 1 || d->N > ECHO_VOCAB_MAX_ROWS || d->V > ECHO_VOCAB_MAX_ROWS || d->D > ECHO_VOCAB_MAX_D) return ECHO_ERR_SHAPE;
+    if (!(eps >= 0.f) || !(eps < 1.f)) return ECHO_ERR_SHAPE;
+    return ECHO_OK;
+}
+
+static bool unaligned(std::initializer_list<const void *> ps) {
+    uintptr_t m = 0;
+    for (const void *p : ps) m |= (uintptr_t)p;
+    return (m & 15u) != 0;
+}
+
+struct VocabRun {
+    echo_vocab_desc_t d;
+    VocabPlan p;
+    char *ws;
+    const void *h, *W;
+    const int *labels;
+    hipStream_t st;
+    template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
+
+    echo_status_t gather() const {
+        LaunchRecord r = launch_begin("vocab_rows", st);
+        k_vocab_rows<<<(d.N + kRowsBlock - 1) / kRowsBlock, 256, 0, st>>>(labels, d.N, d.V, at<int>(p.rows), at<int>(p.place), at<int>(p.count));
+        if (echo_status_t s = launch_end(r)) return s;
+        return pack("vocab_pack_rows", h, at<int>(p.rows), at<int>(p.count), 0, d.N, at<bf16_t>(p.hp), p.h_plane);
+    }
+    echo_status_t pack(const char *name, const void *src, const int *list, const int *count, int first, int n, bf16_t *dst, size_t plane) const {
+        LaunchRecord r = launch_begin(name, st);
+        if (d.in_dtype == ECHO_F32)
+            k_vocab_pack<<<(n + 3) / 4, 256, 0, st>>>(static_cast<const float *>(src), d.D, list, count, first, n, dst, p.pitch, plane);
+        else
+            k_vocab_pack<<<(n + 3) / 4, 256, 0, st>>>(static_cast<const bf16_t *>(src), d.D, list, count, first, n, dst, p.pitch, plane);
+        return launch_end(r);
+    }
+    // the words of a piece as an operand with words along m
+    echo_status_t words(int v0, int n, Operand &o) const {
+        if (!p.pack_words) {
+            o = Operand{static_cast<const bf16_t *>(W) + (size_t)v0 * d.D, 0, d.D, n};
+            return ECHO_OK;
+        }
+        o = Operand{at<bf16_t>(p.wp), p.w_plane, p.pitch, n};
+        return pack("vocab_pack_words", W, nullptr, nullptr, v0, n, at<bf16_t>(p.wp), p.w_plane);
+    }
+    Operand rows() const { return Operand{at<bf16_t>(p.hp), p.h_plane, p.pitch, d.N}; }
+};
+
+}  // namespace echo
+
+extern "C" {
+
+size_t echo_vocab_loss_fwd_workspace_bytes(const echo_vocab_desc_t *desc) {
+    if (echo::check_vocab(desc, 0.f)) return 0;
+    return echo::vocab_plan(*desc, false).total;
+}
+
+size_t echo_vocab_loss_bwd_workspace_bytes(const echo_vocab_desc_t *desc) {
+    if (echo::check_vocab(desc, 0.f)) return 0;
+    return echo::vocab_plan(*desc, true).total;
+}
+
+echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, const void *W, const int32_t *labels,
+                                  float label_smoothing, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                                  void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
+    if (!h || !W || !labels || !loss || !lse || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({h, W, labels, loss, lse, workspace})) return ECHO_ERR_ALIGN;
+    const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
+    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
+    const int N = desc->N, V = desc->V;
+    if (echo_status_t s = x.gather()) return s;
+    LogitsArgs a{};
+    a.h = x.rows();
+    a.D = x.p.pitch;
+    a.pairs = pairs_of(x.p.planes, x.p.planes);
+    a.count = x.at<int>(x.p.count);
+    a.rows = x.at<int>(x.p.rows);
+    a.labels = labels;
+    a.V = V;
+    a.eps = label_smoothing;
+    a.part_max = x.at<float>(x.p.part_max);
+    a.part_sum = x.at<float>(x.p.part_sum);
+    a.part_z = x.at<float>(x.p.part_z);
+    a.z_label = x.at<float>(x.p.z_label);
+    a.pitch = x.p.part_pitch;
+    const bool big = (long long)((V + 255) / 256) * ((N + 255) / 256) >= 512;
+    int tiles = 0;
+    for (int v0 = 0; v0 < V; v0 += x.p.piece) {
+        const int n = std::min(x.p.piece, V - v0);
+        if (echo_status_t s = x.words(v0, n, a.W)) return s;
+        a.v0 = v0;
+        a.first_tile = tiles;
+        if (echo_status_t s = big ? launch_logits<BigTile, false>(a, N, x.st) : launch_logits<MidTile, false>(a, N, x.st)) return s;
+        tiles += big ? (n + 255) / 256 : (n + 127) / 128;
+    }
+    LaunchRecord r = launch_begin("vocab_loss_finish", x.st);
+    k_vocab_loss_finish<<<(N + 63) / 64, 256, 0, x.st>>>(a.part_max, a.part_sum, a.part_z, a.z_label, x.at<int>(x.p.place), N, V, tiles, a.pitch,
+                                                         label_smoothing, loss, lse);
+    return launch_end(r);
+}
+
+echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dloss, const float *lse, const void *h, const void *W,
+                                  const int32_t *labels, float label_smoothing, void *dh, void *dW, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
+    if (!dloss || !lse || !h || !W || !labels || (!dh && !dW) || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({dloss, lse, h, W, labels, dh, dW, workspace})) return ECHO_ERR_ALIGN;
+    const VocabRun x{*desc, vocab_plan(*desc, true), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
+    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
+    const int N = desc->N, V = desc->V, D = desc->D;
+    const VocabPlan &p = x.p;
+    if (echo_status_t s = x.gather()) return s;
+    LogitsArgs a{};
+    a.h = x.rows();
+    a.D = p.pitch;
+    a.pairs = pairs_of(p.planes, p.planes);
+    a.count = x.at<int>(p.count);
+    a.rows = x.at<int>(p.rows);
+    a.labels = labels;
+    a.V = V;
+    a.eps = label_smoothing;
+    a.lse = lse;
+    a.dloss = dloss;
+    a.dz = x.at<bf16_t>(p.dz);
+    a.dz_plane = p.dz_plane;
+    a.dz_pitch = p.piece;
+    a.dz_planes = p.dz_planes;
+    GradsArgs g{};
+    g.dz_words = Operand{a.dz, p.dz_plane, p.piece, 0};
+    g.dz_rows = Operand{a.dz, p.dz_plane, p.piece, N};
+    g.h = x.rows();
+    g.h.rows = p.pitch;
+    g.count = a.count;
+    g.D = D;
+    g.dw_pairs = g.dh_pairs = pairs_of(p.dz_planes, p.planes);
+    g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
+    g.dh_split = (size_t)N * D;
+    g.splits = p.splits;
+    g.bf16_out = desc->out_dtype == ECHO_BF16;
+    const size_t out_bytes = g.bf16_out ? 2 : 4;
+    for (int v0 = 0; v0 < V; v0 += p.piece) {
+        const int n = std::min(p.piece, V - v0);
+        if (echo_status_t s = x.words(v0, n, a.W)) return s;
+        a.v0 = v0;
+        const bool big = (long long)((n + 255) / 256) * ((N + 255) / 256) >= 512;
+        if (echo_status_t s = big ? launch_logits<BigTile, true>(a, N, x.st) : launch_logits<MidTile, true>(a, N, x.st)) return s;
+        g.words = n;
+        g.dz_words.rows = (n + 7) / 8 * 8;
+        g.W = a.W;
+        g.W.rows = p.pitch;
+        g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
+        g.add = v0 > 0;
+        g.split_words = (int)up((n + g.splits - 1) / g.splits, 64);
+        const long long tiles = ((long long)(n + 255) / 256 + (N + 255) / 256) * ((D + 255) / 256);
+        if (echo_status_t s = tiles >= 512 ? launch_grads<BigTile>(g, N, x.st) : launch_grads<MidTile>(g, N, x.st)) return s;
+    }
+    if (!dh) return ECHO_OK;
+    LaunchRecord r = launch_begin("vocab_dh_finish", x.st);
+    if (g.bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.dh_sum, g.dh_split, g.splits, x.at<int>(p.place), N, D, static_cast<bf16_t *>(dh));
+    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.dh_sum, g.dh_split, g.splits, x.at<int>(p.place), N, D, static_cast<float *>(dh));
+    return launch_end(r);
+}
+
+}  // extern "C"

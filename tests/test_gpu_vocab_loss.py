@@ -1,0 +1,279 @@
+"""The vocabulary loss and its gradients against the float64 oracle.
+
+Tolerances, for every entry, from the arithmetic.  u = 2^-24.
+  z    is summed in fp32 over S = pairs x ceil(D / 16) matrix instructions, each of which rounds its own 16 products' sum and the running sum: at
+       most 4 S u of sum_d |h W|; fp32 operands' six plane pairs leave out less than 4 u of it.              ->  ez(n, v)
+  exp  the argument's product and difference round once each, the exponential is good to 2 u: (2 + 2 |argument|) u relative.
+  lse  the largest ez of the row, the exponentials, sums over at most V terms in groups (a running sum of V / 64 + 80 terms), logarithm
+       and two sums of fp32 numbers of the size of lse and of the label's logit.
+  dz   p times (ez + e_lse + exponential), three roundings; bf16 gradients: two bf16 parts hold it to 2^-16.
+  dh   the errors of dz through |W|, and the sum's own 4 S u of sum |dz| |W|; the rounding of the result.  dW alike.
+"""
+import numpy as np
+import pytest
+
+from oracle import vocab_ref as vr
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def _torch():
+    import torch
+    assert torch.cuda.is_available(), "needs the GPU"
+    from paper_1805_08899_amd import binding as eb
+    return torch, eb, {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _guarded(torch, n_bytes, guard=256):
+    whole = torch.full((n_bytes + 2 * guard + 16,), 0xFF, dtype=torch.uint8, device="cuda")
+    inner = whole[guard:guard + n_bytes]
+
+    def check():
+        assert bool((whole[:guard] == 0xFF).all()) and bool((whole[guard + n_bytes:] == 0xFF).all()), "written outside its buffer"
+    return inner, check
+
+
+class Problem:
+    def __init__(self, N, V, D, store="f32", out="f32", eps=0.0, pad=0.3, seed=0, scale=1.5):
+        torch, eb, types = _torch()
+        self.N, self.V, self.D, self.store, self.out, self.eps = N, V, D, store, out, eps
+        r = np.random.default_rng(seed)
+        W = r.standard_normal((V, D)) / np.sqrt(D)
+        labels = np.minimum(np.exp(r.random(N) * np.log(V + 0.5)).astype(np.int64) - 1, V - 1)
+        h = scale * r.standard_normal((N, D)) + r.random((N, 1)) * 12 * W[labels]
+        none = r.random(N) < pad
+        labels[none] = np.where(r.random(N) < 0.5, -1, V)[none]
+        self.labels = labels.astype(np.int32)
+        to = lambda x: torch.from_numpy(x.astype(np.float32)).to(types[store])
+        self.h, self.W = to(h), to(W)
+        self.dloss = torch.from_numpy(r.standard_normal(N).astype(np.float32))
+        self.desc = eb.make_vocab_desc(N, V, D, store, out)
+
+    def run(self, want_dh=True, want_dW=True, forward_only=False, h=None, stream=None):
+        torch, eb, types = _torch()
+        N, V, D, t = self.N, self.V, self.D, types[self.out]
+        size = 4 if self.out == "f32" else 2
+        bufs = {"loss": N * 4, "lse": N * 4, "dh": N * D * size, "dW": V * D * size,
+                "ws_f": eb.echo_vocab_loss_fwd_workspace_bytes(self.desc), "ws_b": eb.echo_vocab_loss_bwd_workspace_bytes(self.desc)}
+        b, checks = {}, []
+        for k, n in bufs.items():
+            b[k], c = _guarded(torch, n)
+            checks.append(c)
+        loss, lse = b["loss"].view(torch.float32), b["lse"].view(torch.float32)
+        dh, dW = b["dh"].view(t).view(N, D), b["dW"].view(t).view(V, D)
+        st = stream or torch.cuda.current_stream()
+        x = (self.h if h is None else h).cuda(), self.W.cuda(), torch.from_numpy(self.labels).cuda()
+        eb.check(eb.echo_vocab_loss_fwd(self.desc, *x, self.eps, loss, lse, b["ws_f"], stream=st))
+        if not forward_only:
+            eb.check(eb.echo_vocab_loss_bwd(self.desc, self.dloss.cuda(), lse, *x, self.eps, dh if want_dh else None,
+                                            dW if want_dW else None, b["ws_b"], stream=st))
+        torch.cuda.synchronize()
+        for c in checks:
+            c()
+        r = {"loss": loss, "lse": lse}
+        if not forward_only:
+            r.update({k: x for k, x, w in (("dh", dh, want_dh), ("dW", dW, want_dW)) if w})
+        return {k: x.double().cpu().numpy() for k, x in r.items()}
+
+    def check(self, got):
+        h, W = self.h.double().numpy(), self.W.double().numpy()
+        V, D, eps, labels = self.V, self.D, self.eps, self.labels
+        loss, lse = vr.loss_forward(h, W, labels, eps)
+        rows = vr.labelled(labels, V)
+        h_, y = h[rows], labels[rows]
+        size = np.abs(h_) @ np.abs(W).T
+        S = (6 if self.store == "f32" else 1) * -(-D // 16)
+        ez = (4 * S + 4) * U * size
+        z = h_ @ W.T
+        worst, zy, ezy = ez.max(1, initial=0), z[np.arange(len(rows)), y], ez[np.arange(len(rows)), y]
+        span = 2 + 2 * (z.max(1, initial=0) - z.min(1, initial=0)) if len(rows) else np.zeros(0)
+        e_lse = worst + (np.minimum(span, 220) + V / 64 + 80) * U + 3 * U * (np.abs(lse[rows]) + np.abs(zy) + 1)
+        e_loss = worst + ezy + e_lse + 3 * U * np.abs(loss[rows]) + eps * (worst + (V / 64 + 80) * U * np.abs(z).mean(1))
+        for k, ref, e in (("lse", lse, e_lse), ("loss", loss, e_loss)):
+            bound = np.zeros(self.N)
+            bound[rows] = e
+            assert (np.abs(got[k] - ref) <= bound).all(), (k, np.abs(got[k] - ref).max())
+        if "dh" not in got and "dW" not in got:
+            return
+        dh, dW, dz = vr.loss_backward(self.dloss.double().numpy(), h, W, labels, eps)
+        g = np.abs(self.dloss.double().numpy()[rows, None])
+        p = np.exp(z - lse[rows, None])
+        e_dz = g * (p * (ez + e_lse[:, None] + (4 + 2 * np.abs(z - lse[rows, None])) * U) + 3 * U) + 3 * U * np.abs(dz)
+        planes = 3
+        if self.out == "bf16":
+            e_dz = e_dz + 2.0 ** -16 * np.abs(dz)
+            planes = 2
+        pairs = 6 if self.store == "f32" else planes
+        half = 2.0 ** -8 if self.out == "bf16" else U
+        if "dh" in got:
+            bound = np.zeros_like(dh)
+            bound[rows] = e_dz @ np.abs(W) + (4 * pairs * (V // 16 + 4) + 8) * U * (np.abs(dz) @ np.abs(W)) + half * np.abs(dh[rows])
+            assert (np.abs(got["dh"] - dh) <= 1.01 * bound).all(), np.abs(got["dh"] - dh).max()
+        if "dW" in got:
+            bound = e_dz.T @ np.abs(h_) + (4 * pairs * (len(rows) // 16 + 4) + 8) * U * (np.abs(dz).T @ np.abs(h_)) + half * np.abs(dW)
+            assert (np.abs(got["dW"] - dW) <= 1.01 * bound).all(), np.abs(got["dW"] - dW).max()
+
+
+CASES = [
+    # N, V, D, storage, gradients, label smoothing
+    (1, 1, 1, "f32", "f32", 0.0),
+    (1, 2, 8, "bf16", "f32", 0.0),
+    (1, 300, 64, "bf16", "bf16", 0.1),
+    (3, 5, 7, "f32", "f32", 0.1),
+    (5, 129, 9, "bf16", "bf16", 0.0),          # rows that no 16-byte load can take
+    (31, 127, 63, "bf16", "f32", 0.3),
+    (64, 128, 64, "f32", "f32", 0.0),
+    (65, 257, 65, "f32", "f32", 0.0),
+    (127, 1000, 72, "bf16", "bf16", 0.1),
+    (128, 256, 512, "bf16", "f32", 0.0),
+    (129, 2047, 100, "f32", "f32", 0.1),
+    (200, 513, 520, "bf16", "f32", 0.0),
+    (300, 3001, 1000, "bf16", "bf16", 0.1),
+    (700, 1500, 260, "f32", "f32", 0.0),
+    (2500, 70, 136, "bf16", "f32", 0.1),       # more rows than words
+    (8, 2000, 16384, "f32", "f32", 0.0),       # words of f32 storage in two pieces; the widest rows
+    (4100, 8200, 64, "bf16", "bf16", 0.1),     # tiles of 256 x 256
+    (4100, 11000, 40, "f32", "f32", 0.0),      # the same, dz in two pieces
+]
+IDS = ["N%d_V%d_D%d_%s_%s_%g" % c for c in CASES]
+
+
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_against_the_oracle(case):
+    print("vocab loss", case, flush=True)
+    p = Problem(*case, seed=case[0] + case[1])
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_no_row_has_a_label(store):
+    p = Problem(40, 300, 64, store, "f32", 0.1, pad=1.1)
+    p.labels[:] = -1
+    p.labels[::3] = 300
+    got = p.run()
+    for k, x in got.items():
+        assert not x.any(), k
+
+
+def test_rows_without_a_label_may_hold_anything():
+    torch, eb, types = _torch()
+    p = Problem(150, 300, 72, "f32", "f32", 0.1, pad=0.5, seed=3)
+    none = (p.labels < 0) | (p.labels >= 300)
+    clean = p.run()
+    p.h[torch.from_numpy(none)] = float("nan")
+    p.dloss[torch.from_numpy(none)] = float("inf")
+    got = p.run()
+    for k in clean:
+        assert np.array_equal(got[k], clean[k]), k
+
+
+@pytest.mark.parametrize("scale", [0.0, 60.0, 1000.0])
+def test_flat_and_steep_logits(scale):
+    p = Problem(90, 400, 48, "f32", "f32", 0.1, seed=4, scale=scale)
+    p.check(p.run())
+
+
+def test_a_sure_label_keeps_the_digits_of_its_loss():
+    """Losses of 1e-5 from logits of 20: the difference of lse and the label's logit would have errors of 1e-6."""
+    torch, eb, types = _torch()
+    N, V, D = 64, 1000, 32
+    p = Problem(N, V, D, "f32", "f32", 0.0, pad=0.0, seed=5, scale=0.0)
+    p.h.zero_()
+    p.h[:, 0] = 20.0
+    p.labels[:] = np.arange(N)
+    for n in range(3):                                    # one word above the others in turn
+        p.W.zero_()
+        p.W[:, 0] = 1.0
+        p.W[n, 0] = 2.0
+        got = p.run(forward_only=True)["loss"][n]
+        ref = vr.loss_forward(p.h.numpy(), p.W.numpy(), p.labels, 0.0)[0][n]
+        assert abs(got - ref) <= 300 * U * ref
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_infinities_and_nan_reach_their_row(store):
+    torch, eb, types = _torch()
+    p = Problem(100, 200, 64, store, "f32", 0.0, pad=0.0, seed=6)
+    clean = p.run(forward_only=True)
+    p.h[17, 3] = float("nan")
+    p.h[80, 5] = float("inf")
+    got = p.run(forward_only=True)
+    bad = np.zeros(100, bool)
+    bad[[17, 80]] = True
+    assert not np.isfinite(got["loss"][bad]).any()
+    assert np.array_equal(got["loss"][~bad], clean["loss"][~bad])
+
+
+def test_one_gradient_alone():
+    p = Problem(140, 333, 80, "f32", "f32", 0.1, seed=7)
+    both = p.run()
+    assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"])
+    assert np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
+
+
+@pytest.mark.parametrize("store,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+def test_bit_identical_from_run_to_run(store, out):
+    p = Problem(1000, 3000, 128, store, out, 0.1, seed=8)
+    a, b = p.run(), p.run()
+    for k in a:
+        assert np.array_equal(a[k], b[k]), k
+
+
+def test_gradient_is_the_difference_of_losses():
+    """Central differences along a direction u: sum_n dloss (L(h + s u) - L(h - s u)) / 2 s against <dh, u>.  Bound: the losses'
+    own errors over s, and what central differences of this step leave out, taken from the oracle."""
+    torch, eb, types = _torch()
+    p = Problem(60, 500, 40, "f32", "f32", 0.1, seed=9)
+    u = torch.from_numpy(np.random.default_rng(10).standard_normal((60, 40)).astype(np.float32))
+    s = 2.0 ** -6
+    dloss, W = p.dloss.double().numpy(), p.W.double().numpy()
+    diff, exact = [], []
+    for sign in (1, -1):
+        h = (p.h + sign * s * u)
+        diff.append((dloss * p.run(forward_only=True, h=h)["loss"]).sum())
+        exact.append((dloss * vr.loss_forward(h.double().numpy(), W, p.labels, 0.1)[0]).sum())
+    got = (p.run()["dh"] * u.double().numpy()).sum()
+    formula = (vr.loss_backward(dloss, p.h.double().numpy(), W, p.labels, 0.1)[0] * u.double().numpy()).sum()
+    left_out = abs((exact[0] - exact[1]) / (2 * s) - formula)
+    size = (np.abs(p.h.numpy()) @ np.abs(W).T).max()
+    e_loss = 2 * (4 * 6 * 3 + 4) * U * size + 300 * U + 10 * U * 20
+    assert abs((diff[0] - diff[1]) / (2 * s) - got) <= left_out + 2 * np.abs(dloss).sum() * e_loss / s
+
+
+def test_replayed_from_a_graph_and_on_another_stream():
+    torch, eb, types = _torch()
+    N, V, D = 300, 700, 64
+    desc = eb.make_vocab_desc(N, V, D, "bf16", "f32")
+    h, W = torch.randn(N, D, device="cuda").bfloat16(), (torch.randn(V, D, device="cuda") / 8).bfloat16()
+    labels = torch.randint(-1, V, (N,), device="cuda").int()
+    dloss = torch.rand(N, device="cuda")
+    outs = [torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, D, device="cuda"), torch.empty(V, D, device="cuda")]
+    ws = torch.empty(max(eb.echo_vocab_loss_fwd_workspace_bytes(desc), eb.echo_vocab_loss_bwd_workspace_bytes(desc)), dtype=torch.uint8,
+                     device="cuda")
+
+    def step():
+        st = torch.cuda.current_stream()
+        eb.check(eb.echo_vocab_loss_fwd(desc, h, W, labels, 0.1, outs[0], outs[1], ws, stream=st))
+        eb.check(eb.echo_vocab_loss_bwd(desc, dloss, outs[1], h, W, labels, 0.1, outs[2], outs[3], ws, stream=st))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        labels.copy_(torch.randint(-1 if k else -V, V, (N,), device="cuda"))   # another number of rows each time
+        h.copy_(torch.randn(N, D, device="cuda"))
+        step()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in outs]
+        for x in outs:
+            x.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
