@@ -27,8 +27,8 @@ namespace echo {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kDzScale = 0x1p24f;                   // on dz while it is in bf16 planes: small probabilities keep their digits (split.hpp)
 
-typedef TileConfig<256, 256, 4, 2, 2> BigTile;
-typedef TileConfig<128, 128, 2, 2, 2> MidTile;
+typedef TileConfig<256, 256, 2, 4, true> BigTile;
+typedef TileConfig<128, 128, 2, 2, false> MidTile;
 
 // ---- rows with a label ------------------------------------------------------------------------------------------------
 // rows[p] = n of the p-th row with a label, place[n] = p or -1, count[0] = their number.  A block writes kRowsBlock labels' entries and
@@ -70,52 +70,69 @@ __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labe
 }
 
 // ---- bf16 planes ------------------------------------------------------------------------------------------------------
-// dst: planes of `pitch` elements a row, zeros behind D.  Row r of dst is row list[r] of src (r < *count), or row first + r
-// (r < n_rows).  A thread takes eight columns.
-__device__ __forceinline__ void split_planes(float x, unsigned short (&p)[3]) {
-    p[0] = __builtin_bit_cast(unsigned short, (__bf16)x);
-    x -= __uint_as_float((unsigned)p[0] << 16);
-    p[1] = __builtin_bit_cast(unsigned short, (__bf16)x);
-    x -= __uint_as_float((unsigned)p[1] << 16);
-    p[2] = __builtin_bit_cast(unsigned short, (__bf16)x);
-}
-template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_pack(const T *__restrict__ src, int D, const int *__restrict__ list,
-                                                    const int *__restrict__ count, int first, int n_rows, bf16_t *__restrict__ dst,
-                                                    int pitch, size_t plane) {
-    const int per_row = pitch / 8, r = blockIdx.x * 4 + wave_id();
-    if (r >= (count ? *count : n_rows)) return;
-    const size_t from = (size_t)(list ? list[r] : first + r) * D;
-    for (int g = lane_id(); g < per_row; g += 64) {
-        const int c = 8 * g;
-        if constexpr (sizeof(T) == 2) {
-            u32x4 u = {0, 0, 0, 0};
-            if (D % 8 == 0) {
-                u = *reinterpret_cast<const u32x4 *>(src + from + c);
-            } else {
+// Rows of src as bf16 planes, once with their columns in a row (dst, `pitch` elements a row, zeros behind D) and once turned (turned: a
+// row per column, `turned_pitch` elements, zeros behind the last row up to a multiple of 8), either of them optional.  Row r is row list[r] of
+// src (r < *count) or row first + r (r < n_rows).  A block takes 64 rows and 64 columns.
+struct PackArgs {
+    const void *src;
+    int D, first, n_rows, pitch, turned_pitch;
+    const int *list, *count;
+    bf16_t *dst, *turned;
+    size_t plane, turned_plane;
+};
+template <typename T> __global__ __launch_bounds__(256) void k_vocab_pack(const PackArgs a) {
+    constexpr int PLANES = sizeof(T) == 4 ? 3 : 1, LP = 72;                    // LDS pitch: 144 bytes, 16-byte aligned, spread over the banks
+    __shared__ __align__(16) unsigned short s[64 * LP];
+    const int rows = a.count ? *a.count : a.n_rows, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    if (r0 >= rows) return;
+    const int tr = threadIdx.x >> 2, tc = (threadIdx.x & 3) * 16, r = r0 + tr, c = c0 + tc;
+    const bool row = r < rows;
+    const T *src = static_cast<const T *>(a.src) + (row ? (size_t)(a.list ? a.list[r] : a.first + r) * a.D : 0);
+    float x[16];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < D) u[j / 2] |= (unsigned)src[from + c + j].bits << (16 * (j & 1));
-            }
-            *reinterpret_cast<u32x4 *>(dst + (size_t)r * pitch + c) = u;
+    for (int j = 0; j < 16; ++j) x[j] = 0.f;
+    if (row) {
+        if (a.D % 4 == 0) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+                if (c + j < a.D) {
+                    const float4 v = ld4(src, c + j);
+                    x[j] = v.x, x[j + 1] = v.y, x[j + 2] = v.z, x[j + 3] = v.w;
+                }
         } else {
-            float x[8];
-            if (D % 4 == 0) {
-                const float4 a = ld4(src, from + c), b = c + 4 < D ? ld4(src, from + c + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-                x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-            } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = c + j < D ? src[from + c + j] : 0.f;
+            for (int j = 0; j < 16; ++j)
+                if (c + j < a.D) x[j] = ld(src, c + j);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k) {
+        unsigned u[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            u[j] = bf16_pair(x[2 * j], x[2 * j + 1]);
+            x[2 * j] -= __uint_as_float(u[j] << 16);
+            x[2 * j + 1] -= __uint_as_float(u[j] & 0xffff0000u);
+        }
+        if (a.dst && row) {
+            bf16_t *to = a.dst + k * a.plane + (size_t)r * a.pitch + c;
+            if (c < a.pitch) *reinterpret_cast<u32x4 *>(to) = u32x4{u[0], u[1], u[2], u[3]};
+            if (c + 8 < a.pitch) *reinterpret_cast<u32x4 *>(to + 8) = u32x4{u[4], u[5], u[6], u[7]};
+        }
+        if (a.turned) {
+            if (k > 0) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[(tc + 2 * j) * LP + tr] = (unsigned short)u[j];
+                s[(tc + 2 * j + 1) * LP + tr] = (unsigned short)(u[j] >> 16);
             }
-            unsigned short p[8][3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) split_planes(x[j], p[j]);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                u32x4 u;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) u[j] = (unsigned)p[2 * j][k] | (unsigned)p[2 * j + 1][k] << 16;
-                *reinterpret_cast<u32x4 *>(dst + k * plane + (size_t)r * pitch + c) = u;
+            __syncthreads();
+            // here tr is the column and tc the first of 16 rows
+            if (c0 + tr < a.pitch) {
+                bf16_t *to = a.turned + k * a.turned_plane + (size_t)(c0 + tr) * a.turned_pitch + r0 + tc;
+                const u32x4 *from = reinterpret_cast<const u32x4 *>(s + tr * LP + tc);
+                if (r0 + tc < rows) *reinterpret_cast<u32x4 *>(to) = from[0];
+                if (r0 + tc + 8 < rows) *reinterpret_cast<u32x4 *>(to + 8) = from[1];
             }
         }
     }
@@ -149,9 +166,9 @@ struct LogitsArgs {
     size_t pitch;
     // backward
     const float *lse, *dloss;
-    bf16_t *dz;
-    size_t dz_plane;
-    int dz_pitch, dz_planes;
+    bf16_t *dz, *turned;             // [N][dz_pitch]; [words][turned_pitch]
+    size_t dz_plane, turned_plane;
+    int dz_pitch, turned_pitch, dz_planes;
 };
 
 // a sum of exponentials relative to `from`, relative to `to` >= from (both may be minus infinity: an empty sum)
@@ -166,35 +183,34 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     int im, in;
     if (!tile_of_block(blockIdx.x, (a.W.rows + C::BM - 1) / C::BM, (count + C::BN - 1) / C::BN, im, in)) return;
     const int m0 = im * C::BM, n0 = in * C::BN;
-    f32x16 acc[C::TM][C::TN];
+    f32x4 acc[C::TM][C::TN];
     Operand h = a.h;
     h.rows = count;
-    tile_product<C, false, false>(acc, a.W, h, m0, n0, 0, a.D, a.pairs, lds);
-    block_barrier();                                                           // LDS has another use from here on
-    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
-    const int vw = a.v0 + m0 + wm * C::TM * 32;                                // this wave's first word
+    tile_product<C>(acc, a.W, h, m0, n0, 0, a.D, a.pairs, lds);
+    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
+    const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
     if constexpr (!BWD) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
-            const int nt = (wn * C::TN + j) * 32 + (lane & 31), n = n0 + nt;
+            const int nt = (wn * C::TN + j) * 16 + (lane & 15), n = n0 + nt;
             const int y = n < count ? a.labels[a.rows[n]] - vw : -1;
             float z = 0.f;
             if (a.eps > 0.f) {
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) z += !tail || vw + i * 32 + mfma32_row(r, lane) < a.V ? acc[i][j][r] : 0.f;
+                    for (int r = 0; r < 4; ++r) z += !tail || vw + i * 16 + r < a.V ? acc[i][j][r] : 0.f;
+                z += __shfl_xor(z, 16);
                 z += __shfl_xor(z, 32);
             }
-            const bool here = y >= 0 && y < C::TM * 32;
-            if (__ballot(here)) {             // the label's logit: the lane that holds it writes it and leaves it out of maximum and sum
+            if (__ballot(y >= 0 && y < C::TM * 16 && y % 16 < 4)) {   // the label's logit: the lane that holds it writes it and leaves it out of maximum and sum
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (here && y == i * 32 + mfma32_row(r, lane)) {
+                    for (int r = 0; r < 4; ++r)
+                        if (y == i * 16 + r) {
                             a.z_label[n] = acc[i][j][r];
                             acc[i][j][r] = -__builtin_inff();
                         }
@@ -203,23 +219,25 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (vw + i * 32 + mfma32_row(r, lane) >= a.V) acc[i][j][r] = -__builtin_inff();
+                    for (int r = 0; r < 4; ++r)
+                        if (vw + i * 16 + r >= a.V) acc[i][j][r] = -__builtin_inff();
             }
             float top = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+                for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
+            top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float at = top == -__builtin_inff() ? 0.f : top;             // nothing but the label and words past the end
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += fast_exp2((acc[i][j][r] - at) * kLog2e);
+                for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[i][j][r] - at) * kLog2e);
+            sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            if (lane < 32) {
+            if (lane < 16) {
                 s_max[wm * C::BN + nt] = top;
                 s_sum[wm * C::BN + nt] = sum;
                 s_z[wm * C::BN + nt] = z;
@@ -245,7 +263,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
         const float off = 1.0f - a.eps, low = a.eps / (float)a.V;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
-            const int n = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+            const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
             const bool row = n < count;
             const int at = row ? a.rows[n] : 0;
             const int y = row ? a.labels[at] - vw : -1;
@@ -253,41 +271,54 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int v = i * 32 + mfma32_row(r, lane);
+                for (int r = 0; r < 4; ++r) {
+                    const int v = i * 16 + r;
                     const float p = fast_exp2((acc[i][j][r] - lse) * kLog2e) - (v == y ? off + low : low);
                     acc[i][j][r] = vw + v < a.V ? p * g : 0.f;
                 }
         }
-        // rows of dz through LDS, a plane at a time: each wave writes four words per lane and reads whole rows
+        // dz passes through LDS a plane at a time, [row][word]: each lane writes four words of a row; whole rows leave for dz, and read
+        // with the transposing load 16 words x 32 rows leave for its turned form
         constexpr int PITCH = C::BM * 2 + 16;                                  // bytes; 16 more per row spread the rows over the banks
+        const int rows = min(C::BN, (count - n0 + 7) / 8 * 8);                 // zeros up to a multiple of 8
         for (int k = 0; k < a.dz_planes; ++k) {
             if (k > 0) lds_barrier();
 #pragma unroll
             for (int j = 0; j < C::TN; ++j) {
-                const int nt = (wn * C::TN + j) * 32 + (lane & 31);
+                char *to = lds + ((wn * C::TN + j) * 16 + (lane & 15)) * PITCH + (wm * C::TM * 16 + lr) * 2;
 #pragma unroll
-                for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        u32x2 u;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float x0 = acc[i][j][4 * q + 2 * e], x1 = acc[i][j][4 * q + 2 * e + 1];
-                            const unsigned b = bf16_pair(x0, x1);
-                            acc[i][j][4 * q + 2 * e] = x0 - __uint_as_float(b << 16);
-                            acc[i][j][4 * q + 2 * e + 1] = x1 - __uint_as_float(b & 0xffff0000u);
-                            u[e] = b;
-                        }
-                        *reinterpret_cast<u32x2 *>(lds + nt * PITCH + ((wm * C::TM + i) * 32 + 8 * q + 4 * (lane >> 5)) * 2) = u;
-                    }
+                for (int i = 0; i < C::TM; ++i) {
+                    f32x4 &x = acc[i][j];
+                    const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+                    x[0] -= __uint_as_float(u.x << 16);
+                    x[1] -= __uint_as_float(u.x & 0xffff0000u);
+                    x[2] -= __uint_as_float(u.y << 16);
+                    x[3] -= __uint_as_float(u.y & 0xffff0000u);
+                    *reinterpret_cast<u32x2 *>(to + i * 32) = u;
+                }
             }
             lds_barrier();
-            bf16_t *out = a.dz + k * a.dz_plane + (size_t)n0 * a.dz_pitch + m0;
-            for (int c = threadIdx.x; c < C::BN * (C::BM / 8); c += C::THREADS) {
-                const int nt = c / (C::BM / 8), g = c % (C::BM / 8);
-                if (n0 + nt < count && m0 + g * 8 < a.dz_pitch)
-                    *reinterpret_cast<u32x4 *>(out + (size_t)nt * a.dz_pitch + g * 8) = *reinterpret_cast<const u32x4 *>(lds + nt * PITCH + g * 16);
+            if (a.dz) {
+                bf16_t *out = a.dz + k * a.dz_plane + (size_t)n0 * a.dz_pitch + m0;
+                for (int c = threadIdx.x; c < rows * (C::BM / 8); c += C::THREADS) {
+                    const int nt = c / (C::BM / 8), g = c % (C::BM / 8);
+                    if (m0 + g * 8 < a.dz_pitch)
+                        *reinterpret_cast<u32x4 *>(out + (size_t)nt * a.dz_pitch + g * 8) = *reinterpret_cast<const u32x4 *>(lds + nt * PITCH + g * 16);
+                }
+            }
+            if (a.turned) {
+                bf16_t *out = a.turned + k * a.turned_plane + (size_t)m0 * a.turned_pitch + n0;
+                typedef short s16x4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s16x4 *tr_ptr;
+                // block (x, y): words 16 x .., rows 32 y ..; lanes 16 g .. 16 g + 15 address 4 rows x 16 words and get a word's 4 rows each
+                for (int c = w; c < (C::BM / 16) * (C::BN / 32); c += C::WAVES) {
+                    const int x = c / (C::BN / 32), y = c % (C::BN / 32), nt = y * 32 + 8 * (lane >> 4), v = 16 * x + (lane & 15);
+                    const char *from = lds + (nt + ((lane & 15) >> 2)) * PITCH + (16 * x + 4 * (lane & 3)) * 2;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)from);
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(from + 4 * PITCH));
+                    const u32x2 p = __builtin_bit_cast(u32x2, lo), q = __builtin_bit_cast(u32x2, hi);
+                    if (nt < rows && a.v0 + m0 + v < a.V) *reinterpret_cast<u32x4 *>(out + (size_t)v * a.turned_pitch + nt) = u32x4{p.x, p.y, q.x, q.y};
+                }
             }
         }
     }
@@ -353,11 +384,11 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
 
 // ---- gradients ----------------------------------------------------------------------------------------------------------
 struct GradsArgs {
-    Operand dz_words, dz_rows;       // dz with its words along m, with its rows along m
-    Operand h, W;                    // rows along k: columns of h and of W along n
+    Operand dz, dz_turned;           // rows of dz; words of dz
+    Operand h_turned, W_turned;      // columns of h; of this piece's words
     const int *count;
     int words, D;                    // of this piece
-    PlanePairs dw_pairs, dh_pairs;
+    PlanePairs pairs;
     void *dW;                        // this piece's first row; or null
     float *dh_sum;                   // [splits][N][D] sums of dh in the rows' gathered places; or null
     size_t dh_split;
@@ -366,58 +397,82 @@ struct GradsArgs {
     int dw_blocks;                   // blocks of the first kind
 };
 
+// Tiles of dW (columns of h x words, over the rows) and of dh (columns of W x rows, over the piece's words): a lane holds four
+// consecutive columns of a result row.
 template <class C>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     extern __shared__ __align__(16) char lds[];
-    const int count = *a.count, tn = (a.D + C::BN - 1) / C::BN;
+    const int count = *a.count, tm = (a.D + C::BM - 1) / C::BM;
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
-    f32x16 acc[C::TM][C::TN];
+    const bool quads = a.D % 4 == 0;
+    f32x4 acc[C::TM][C::TN];
     int im, in;
     if ((int)blockIdx.x < a.dw_blocks) {
-        if (!tile_of_block(blockIdx.x, (a.words + C::BM - 1) / C::BM, tn, im, in)) return;
+        if (!tile_of_block(blockIdx.x, tm, (a.words + C::BN - 1) / C::BN, im, in)) return;
         const int m0 = im * C::BM, n0 = in * C::BN;
-        tile_product<C, true, true>(acc, a.dz_words, a.h, m0, n0, 0, count, a.dw_pairs, lds);
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane), d = n0 + (wn * C::TN + j) * 32 + (lane & 31);
-                    if (m < a.words && d < a.D) {
-                        const float x = acc[i][j][r] * (1.f / kDzScale);
-                        const size_t at = (size_t)m * a.D + d;
-                        if (a.bf16_out) static_cast<__bf16 *>(a.dW)[at] = (__bf16)x;
-                        else store_streaming(static_cast<float *>(a.dW) + at, x);
-                    }
-                }
-        return;
-    }
-    const int b = blockIdx.x - a.dw_blocks, tm = (count + C::BM - 1) / C::BM;
-    if (!tile_of_block(b, tm * a.splits, tn, im, in)) return;
-    const int split = im / tm, m0 = (im - split * tm) * C::BM, n0 = in * C::BN;
-    const int k0 = split * a.split_words, k1 = min(a.words, k0 + a.split_words);
-    Operand dz = a.dz_rows;
-    dz.rows = count;
-    tile_product<C, false, true>(acc, dz, a.W, m0, n0, k0, max(k0, k1), a.dh_pairs, lds);
-    float *to = a.dh_sum + split * a.dh_split;
-#pragma unroll
-    for (int i = 0; i < C::TM; ++i)
+        tile_product<C>(acc, a.h_turned, a.dz_turned, m0, n0, 0, count, a.pairs, lds);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
-            float old[16];
-            const int d = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+            const int v = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+            if (v >= a.words) continue;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane);
-                old[r] = a.add && m < count && d < a.D ? to[(size_t)m * a.D + d] : 0.f;
-            }
+            for (int i = 0; i < C::TM; ++i) {
+                const int d = m0 + (wm * C::TM + i) * 16 + 4 * (lane >> 4);
+                const f32x4 x = acc[i][j] * (1.f / kDzScale);
+                const size_t at = (size_t)v * a.D + d;
+                if (a.bf16_out) {
+                    bf16_t *to = static_cast<bf16_t *>(a.dW) + at;
+                    const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+                    if (quads) {
+                        if (d < a.D) __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(to));
+                    } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int m = m0 + (wm * C::TM + i) * 32 + mfma32_row(r, lane);
-                if (m < count && d < a.D) to[(size_t)m * a.D + d] = old[r] + acc[i][j][r];
+                        for (int r = 0; r < 4; ++r)
+                            if (d + r < a.D) to[r].bits = (unsigned short)(u[r / 2] >> (16 * (r & 1)));
+                    }
+                } else {
+                    float *to = static_cast<float *>(a.dW) + at;
+                    if (quads) {
+                        if (d < a.D) __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(to));
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (d + r < a.D) to[r] = x[r];
+                    }
+                }
             }
         }
+        return;
+    }
+    const int b = blockIdx.x - a.dw_blocks, tn = (count + C::BN - 1) / C::BN;
+    if (!tile_of_block(b, tm, tn * a.splits, im, in)) return;
+    const int split = in / tn, m0 = im * C::BM, n0 = (in - split * tn) * C::BN;
+    const int k0 = min(split * a.split_words, a.words), k1 = min(a.words, k0 + a.split_words);
+    Operand dz = a.dz;
+    dz.rows = count;
+    tile_product<C>(acc, a.W_turned, dz, m0, n0, k0, k1, a.pairs, lds);
+    float *sums = a.dh_sum + split * a.dh_split;
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+        const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+        if (n >= count) continue;
+        float *to = sums + (size_t)n * a.D + m0 + wm * C::TM * 16 + 4 * (lane >> 4);
+        const int left = a.D - (m0 + wm * C::TM * 16 + 4 * (lane >> 4));
+        if (quads) {
+            f32x4 old[C::TM];
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) old[i] = a.add && 16 * i < left ? *reinterpret_cast<const f32x4 *>(to + 16 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+                if (16 * i < left) *reinterpret_cast<f32x4 *>(to + 16 * i) = old[i] + acc[i][j];
+        } else {
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * i + r < left) to[16 * i + r] = (a.add ? to[16 * i + r] : 0.f) + acc[i][j][r];
+        }
+    }
 }
 
 // dh[n] = sum of the splits of row place[n], scaled back; zeros for rows without a label.  A wave per row.
@@ -441,16 +496,16 @@ __global__ __launch_bounds__(256) void k_vocab_dh_finish(const float *__restrict
 static size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr size_t kPackBytes = (size_t)128 << 20;      // of f32 words' planes at a time
-constexpr size_t kDzBytes = (size_t)256 << 20;        // of dz at a time
+constexpr size_t kDzBytes = (size_t)512 << 20;        // of dz and its turned form at a time
 constexpr size_t kMaxTiles = (size_t)1 << 22;         // of 128 x 128 in a launch: a grid has fewer than 2^32 threads
 
 struct VocabPlan {
-    int planes, pitch;                                // of h and, if packed, of W
+    int planes, pitch, turned_pitch;                  // of h and, if packed, of W; of h and dz turned
     bool pack_words;
     int piece;                                        // words per piece, a multiple of 256
     int dz_planes, splits;
-    size_t count, rows, place, hp, wp, part_max, part_sum, part_z, z_label, dz, dh, total;
-    size_t h_plane, w_plane, dz_plane, part_pitch;
+    size_t count, rows, place, hp, ht, wp, wt, dzt, part_max, part_sum, part_z, z_label, dz, dh, total;
+    size_t h_plane, ht_plane, w_plane, wt_plane, dz_plane, dzt_plane, part_pitch;
     int tiles;                                        // most tiles along the vocabulary
 };
 
@@ -463,11 +518,15 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 2;
     size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
     if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
-    if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (2 * p.dz_planes * N) / 256 * 256, 256));
+    if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (4 * p.dz_planes * N) / 256 * 256, 256));
     p.piece = (int)piece;
     p.h_plane = N * p.pitch;
     p.w_plane = piece * p.pitch;
-    p.dz_plane = N * piece;
+    p.turned_pitch = (int)up(N, 8);
+    p.ht_plane = (size_t)p.pitch * p.turned_pitch;
+    p.wt_plane = (size_t)p.pitch * piece;
+    p.dz_plane = up(N, 8) * piece;
+    p.dzt_plane = piece * p.turned_pitch;
     p.part_pitch = up(N, 64);
     p.tiles = (int)(up(V, piece) / piece * (piece / 128));
     p.splits = 1;
@@ -488,7 +547,10 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
         p.part_z = take(p.tiles * p.part_pitch * 4);
         p.z_label = take(N * 4);
     } else {
+        p.ht = take(p.planes * p.ht_plane * 2);
+        p.wt = take(p.planes * p.wt_plane * 2);
         p.dz = take(p.dz_planes * p.dz_plane * 2);
+        p.dzt = take(p.dz_planes * p.dzt_plane * 2);
         p.dh = take((size_t)p.splits * N * D * 4);
     }
     p.total = at;
@@ -497,8 +559,8 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
 
 static PlanePairs pairs_of(int a, int b) {             // planes of the operands: nibbles, the small terms first
     if (a == 3 && b == 3) return {6, 0x001021u, 0x010201u};
-    if (a == 3 && b == 1) return {3, 0x012u, 0u};
-    if (a == 2 && b == 1) return {2, 0x01u, 0u};
+    if (a == 1 && b == 3) return {3, 0u, 0x012u};
+    if (a == 1 && b == 2) return {2, 0u, 0x01u};
     return {1, 0u, 0u};
 }
 
@@ -517,14 +579,15 @@ static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &grante
 template <class C, bool BWD> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
-    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, BWD>, granted, product_lds<C>(), blocks, C::THREADS, a, st);
+    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, BWD>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
+                        C::THREADS, a, st);
 }
 template <class C> static echo_status_t launch_grads(GradsArgs a, int N, hipStream_t st) {
     static LdsGrants granted{};
-    const long long tn = (a.D + C::BN - 1) / C::BN;
-    a.dw_blocks = a.dW ? (int)(((a.words + C::BM - 1) / C::BM * tn + 7) / 8 * 8) : 0;
-    const long long blocks = a.dw_blocks + (a.dh_sum ? (N + C::BM - 1) / C::BM * tn * a.splits : 0);
-    return launch_tiles("vocab_grads", &k_vocab_grads<C>, granted, product_lds<C>(), blocks, C::THREADS, a, st);
+    const long long tm = (a.D + C::BM - 1) / C::BM;
+    a.dw_blocks = a.dW ? (int)(((a.words + C::BN - 1) / C::BN * tm + 7) / 8 * 8) : 0;
+    const long long blocks = a.dw_blocks + (a.dh_sum ? (N + C::BN - 1) / C::BN * tm * a.splits : 0);
+    return launch_tiles("vocab_grads", &k_vocab_grads<C>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
 }
 
 static echo_status_t check_vocab(const echo_vocab_desc_t *d, float eps) {
@@ -551,28 +614,27 @@ struct VocabRun {
     hipStream_t st;
     template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
 
-    echo_status_t gather() const {
+    // the rows with a label; turned: in their turned form too
+    echo_status_t gather(bool turned) const {
         LaunchRecord r = launch_begin("vocab_rows", st);
         k_vocab_rows<<<(d.N + kRowsBlock - 1) / kRowsBlock, 256, 0, st>>>(labels, d.N, d.V, at<int>(p.rows), at<int>(p.place), at<int>(p.count));
         if (echo_status_t s = launch_end(r)) return s;
-        return pack("vocab_pack_rows", h, at<int>(p.rows), at<int>(p.count), 0, d.N, at<bf16_t>(p.hp), p.h_plane);
+        return pack("vocab_pack_rows", PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<int>(p.count), at<bf16_t>(p.hp),
+                                                turned ? at<bf16_t>(p.ht) : nullptr, p.h_plane, p.ht_plane});
     }
-    echo_status_t pack(const char *name, const void *src, const int *list, const int *count, int first, int n, bf16_t *dst, size_t plane) const {
+    echo_status_t pack(const char *name, const PackArgs &a) const {
         LaunchRecord r = launch_begin(name, st);
-        if (d.in_dtype == ECHO_F32)
-            k_vocab_pack<<<(n + 3) / 4, 256, 0, st>>>(static_cast<const float *>(src), d.D, list, count, first, n, dst, p.pitch, plane);
-        else
-            k_vocab_pack<<<(n + 3) / 4, 256, 0, st>>>(static_cast<const bf16_t *>(src), d.D, list, count, first, n, dst, p.pitch, plane);
+        const dim3 grid((a.n_rows + 63) / 64, (a.pitch + 63) / 64);
+        if (d.in_dtype == ECHO_F32) k_vocab_pack<float><<<grid, 256, 0, st>>>(a);
+        else k_vocab_pack<bf16_t><<<grid, 256, 0, st>>>(a);
         return launch_end(r);
     }
-    // the words of a piece as an operand with words along m
-    echo_status_t words(int v0, int n, Operand &o) const {
-        if (!p.pack_words) {
-            o = Operand{static_cast<const bf16_t *>(W) + (size_t)v0 * d.D, 0, d.D, n};
-            return ECHO_OK;
-        }
-        o = Operand{at<bf16_t>(p.wp), p.w_plane, p.pitch, n};
-        return pack("vocab_pack_words", W, nullptr, nullptr, v0, n, at<bf16_t>(p.wp), p.w_plane);
+    // the words of a piece as an operand, and their turned form if it is wanted
+    echo_status_t words(int v0, int n, bool turned, Operand &o) const {
+        o = p.pack_words ? Operand{at<bf16_t>(p.wp), p.w_plane, p.pitch, n} : Operand{static_cast<const bf16_t *>(W) + (size_t)v0 * d.D, 0, d.D, n};
+        if (!p.pack_words && !turned) return ECHO_OK;
+        return pack("vocab_pack_words", PackArgs{W, d.D, v0, n, p.pitch, p.piece, nullptr, nullptr, p.pack_words ? at<bf16_t>(p.wp) : nullptr,
+                                                 turned ? at<bf16_t>(p.wt) : nullptr, p.w_plane, p.wt_plane});
     }
     Operand rows() const { return Operand{at<bf16_t>(p.hp), p.h_plane, p.pitch, d.N}; }
 };
@@ -601,7 +663,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V;
-    if (echo_status_t s = x.gather()) return s;
+    if (echo_status_t s = x.gather(false)) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = x.p.pitch;
@@ -620,7 +682,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     int tiles = 0;
     for (int v0 = 0; v0 < V; v0 += x.p.piece) {
         const int n = std::min(x.p.piece, V - v0);
-        if (echo_status_t s = x.words(v0, n, a.W)) return s;
+        if (echo_status_t s = x.words(v0, n, false, a.W)) return s;
         a.v0 = v0;
         a.first_tile = tiles;
         if (echo_status_t s = big ? launch_logits<BigTile, false>(a, N, x.st) : launch_logits<MidTile, false>(a, N, x.st)) return s;
@@ -643,7 +705,7 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V, D = desc->D;
     const VocabPlan &p = x.p;
-    if (echo_status_t s = x.gather()) return s;
+    if (echo_status_t s = x.gather(dW != nullptr)) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = p.pitch;
@@ -655,18 +717,20 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     a.eps = label_smoothing;
     a.lse = lse;
     a.dloss = dloss;
-    a.dz = x.at<bf16_t>(p.dz);
+    a.dz = dh ? x.at<bf16_t>(p.dz) : nullptr;
     a.dz_plane = p.dz_plane;
     a.dz_pitch = p.piece;
+    a.turned = dW ? x.at<bf16_t>(p.dzt) : nullptr;
+    a.turned_plane = p.dzt_plane;
+    a.turned_pitch = p.turned_pitch;
     a.dz_planes = p.dz_planes;
     GradsArgs g{};
-    g.dz_words = Operand{a.dz, p.dz_plane, p.piece, 0};
-    g.dz_rows = Operand{a.dz, p.dz_plane, p.piece, N};
-    g.h = x.rows();
-    g.h.rows = p.pitch;
+    g.dz = Operand{a.dz, p.dz_plane, p.piece, N};
+    g.h_turned = Operand{x.at<bf16_t>(p.ht), p.ht_plane, p.turned_pitch, p.pitch};
+    g.W_turned = Operand{x.at<bf16_t>(p.wt), p.wt_plane, p.piece, p.pitch};
     g.count = a.count;
     g.D = D;
-    g.dw_pairs = g.dh_pairs = pairs_of(p.dz_planes, p.planes);
+    g.pairs = pairs_of(p.planes, p.dz_planes);
     g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
     g.dh_split = (size_t)N * D;
     g.splits = p.splits;
@@ -674,14 +738,12 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     const size_t out_bytes = g.bf16_out ? 2 : 4;
     for (int v0 = 0; v0 < V; v0 += p.piece) {
         const int n = std::min(p.piece, V - v0);
-        if (echo_status_t s = x.words(v0, n, a.W)) return s;
+        if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
         const bool big = (long long)((n + 255) / 256) * ((N + 255) / 256) >= 512;
         if (echo_status_t s = big ? launch_logits<BigTile, true>(a, N, x.st) : launch_logits<MidTile, true>(a, N, x.st)) return s;
         g.words = n;
-        g.dz_words.rows = (n + 7) / 8 * 8;
-        g.W = a.W;
-        g.W.rows = p.pitch;
+        g.dz_turned = Operand{a.turned, p.dzt_plane, p.turned_pitch, n};
         g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
         g.add = v0 > 0;
         g.split_words = (int)up((n + g.splits - 1) / g.splits, 64);
