@@ -30,12 +30,54 @@ constexpr float kDzScale = 0x1p24f;                   // on dz while it is in bf
 typedef TileConfig<256, 256, 2, 4, true> BigTile;
 typedef TileConfig<128, 128, 2, 2, false> MidTile;
 
+// How a piece's tiles of dW and dh are cut along k, so that the units fill whole rounds of the chip: with few tiles, and with k axes of
+// very different lengths (rows for dW, the piece's words for dh), uncut ones leave most of it idle.  Among lengths of 1 / q of either axis, the one
+// with the least rounds x (length + what a unit costs besides) + what the parts cost that are written and read again.  The number of rows
+// is known on the device only: k_vocab_rows works it out for all launches behind it.
+struct Cut {
+    int dw, dh;                      // parts of each kind
+};
+struct CutArgs {
+    int words, D;                    // of a whole piece: the last one, which may be narrower, is cut into as many parts
+    int most_dw, most_dh;            // parts there is room for; 0: that gradient is not wanted
+    int tile, slots;                 // tile x tile; blocks that run at once
+    int pairs;
+    float round;                     // what a step of a round takes, against one of 256 blocks of 256 x 256
+};
+constexpr int kMostParts = 8;
+constexpr float kUnitSteps = 8.f;                       // steps that a unit's start and end take
+constexpr float kPartSteps = 1.f / 1.1e6f;              // steps (of 1.7 us) that it takes to write and read one number of a part (8 bytes at 5 TB/s)
+__host__ __device__ inline Cut cut_of(const CutArgs &a, int count, float *cost_out = nullptr) {
+    const int tm = (a.D + a.tile - 1) / a.tile, tw = tm * ((a.words + a.tile - 1) / a.tile), th = tm * ((count + a.tile - 1) / a.tile);
+    const int kw = count > 0 ? (count + 63) / 64 : 1, kh = (a.words + 63) / 64;
+    Cut best = {a.most_dw ? 1 : 0, a.most_dh ? 1 : 0};
+    float least = 3e38f;
+    for (int i = 0; i < 2 * kMostParts; ++i) {
+        const int q = i / 2 + 1, len = ((i % 2 ? kw : kh) + q - 1) / q;
+        Cut c = {(kw + len - 1) / len, (kh + len - 1) / len};
+        c.dw = c.dw < a.most_dw ? c.dw : a.most_dw;
+        c.dh = c.dh < a.most_dh ? c.dh : a.most_dh;
+        const int lw = c.dw ? (kw + c.dw - 1) / c.dw : 0, lh = c.dh ? (kh + c.dh - 1) / c.dh : 0, longest = lw > lh ? lw : lh;
+        const long long units = (long long)tw * c.dw + (long long)th * c.dh;
+        const float rounds = (float)((units + a.slots - 1) / a.slots);
+        const float cost = rounds * ((float)(longest * a.pairs) + kUnitSteps) * a.round +
+                           ((c.dw > 1 ? (float)c.dw * a.words : 0.f) + (c.dh > 1 ? (float)(c.dh - 1) * count : 0.f)) * a.D * kPartSteps;
+        if (cost < least) least = cost, best = c;
+    }
+    if (cost_out) *cost_out = least;
+    return best;
+}
+
 // ---- rows with a label ------------------------------------------------------------------------------------------------
-// rows[p] = n of the p-th row with a label, place[n] = p or -1, count[0] = their number.  A block writes kRowsBlock labels' entries and
-// counts all labels in front of them by itself.
+// rows[p] = n of the p-th row with a label, place[n] = p or -1.  A block writes kRowsBlock labels' entries and counts all labels in
+// front of them by itself.
+struct Rows {
+    int count;                       // rows with a label
+    Cut cut;
+};
 constexpr int kRowsBlock = 2048;
 __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labels, int N, int V, int *__restrict__ rows,
-                                                    int *__restrict__ place, int *__restrict__ count) {
+                                                    int *__restrict__ place, Rows *__restrict__ out, const CutArgs cut) {
     __shared__ int s_wave[4];
     const int lane = lane_id(), w = wave_id(), begin = blockIdx.x * kRowsBlock;
     int before = 0;
@@ -66,7 +108,7 @@ __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labe
         if (n < N) place[n] = in ? p : -1;
         at += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) count[0] = at;
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *out = Rows{at, cut.slots ? cut_of(cut, at) : Cut{0, 0}};
 }
 
 // ---- bf16 planes ------------------------------------------------------------------------------------------------------
@@ -76,14 +118,15 @@ __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labe
 struct PackArgs {
     const void *src;
     int D, first, n_rows, pitch, turned_pitch;
-    const int *list, *count;
+    const int *list;
+    const Rows *count;
     bf16_t *dst, *turned;
     size_t plane, turned_plane;
 };
 template <typename T> __global__ __launch_bounds__(256) void k_vocab_pack(const PackArgs a) {
     constexpr int PLANES = sizeof(T) == 4 ? 3 : 1, LP = 72;                    // LDS pitch: 144 bytes, 16-byte aligned, spread over the banks
     __shared__ __align__(16) unsigned short s[64 * LP];
-    const int rows = a.count ? *a.count : a.n_rows, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int rows = a.count ? a.count->count : a.n_rows, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
     if (r0 >= rows) return;
     const int tr = threadIdx.x >> 2, tc = (threadIdx.x & 3) * 16, r = r0 + tr, c = c0 + tc;
     const bool row = r < rows;
@@ -157,7 +200,8 @@ struct LogitsArgs {
     Operand W, h;                    // words of this piece; gathered rows
     int D;
     PlanePairs pairs;
-    const int *count, *rows, *labels;
+    const Rows *count;
+    const int *rows, *labels;
     int V, v0;                       // words of the vocabulary; this piece's first word
     float eps;                       // label smoothing
     // forward: [tiles][pitch] maximum, sum, sum of logits; the label's logit
@@ -179,7 +223,7 @@ __device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
 template <class C, bool BWD>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
     extern __shared__ __align__(16) char lds[];
-    const int count = *a.count;
+    const int count = a.count->count;
     int im, in;
     if (!tile_of_block(blockIdx.x, (a.W.rows + C::BM - 1) / C::BM, (count + C::BN - 1) / C::BN, im, in)) return;
     const int m0 = im * C::BM, n0 = in * C::BN;
@@ -386,78 +430,85 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
 struct GradsArgs {
     Operand dz, dz_turned;           // rows of dz; words of dz
     Operand h_turned, W_turned;      // columns of h; of this piece's words
-    const int *count;
+    const Rows *rows;
     int words, D;                    // of this piece
     PlanePairs pairs;
-    void *dW;                        // this piece's first row; or null
-    float *dh_sum;                   // [splits][N][D] sums of dh in the rows' gathered places; or null
-    size_t dh_split;
-    int splits, split_words;         // parts of the piece's words per dh tile, multiples of 64
+    void *dW;                        // this piece's first row
+    float *dw_sum, *dh_sum;          // [parts][words][D]; [parts][N][D], in the rows' gathered places
+    size_t dw_part, dh_part;
     bool bf16_out, add;              // add: not the first piece
-    int dw_blocks;                   // blocks of the first kind
 };
 
-// Tiles of dW (columns of h x words, over the rows) and of dh (columns of W x rows, over the piece's words): a lane holds four
-// consecutive columns of a result row.
+// four consecutive columns of a result row, of which `left` exist; quads: all four or none, aligned
+__device__ __forceinline__ void put4(float *to, f32x4 x, int left, bool quads) {
+    if (quads) {
+        if (left > 0) __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(to));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) to[r] = x[r];
+    }
+}
+__device__ __forceinline__ void put4(bf16_t *to, f32x4 x, int left, bool quads) {
+    const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+    if (quads) {
+        if (left > 0) __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(to));
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < left) to[r].bits = (unsigned short)(u[r / 2] >> (16 * (r & 1)));
+    }
+}
+
+// Units of dW (columns of h x words, over rows) and, behind them, of dh (columns of W x rows, over the piece's words): a lane holds
+// four consecutive columns of a result row.
 template <class C>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     extern __shared__ __align__(16) char lds[];
-    const int count = *a.count, tm = (a.D + C::BM - 1) / C::BM;
+    const int count = a.rows->count, words = a.words, D = a.D, tm = (D + C::BM - 1) / C::BM;
+    Cut cut = a.rows->cut;
+    if (!a.dW) cut.dw = 0;
+    if (!a.dh_sum) cut.dh = 0;
+    const int tw = (words + C::BN - 1) / C::BN, th = (count + C::BN - 1) / C::BN;
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
-    const bool quads = a.D % 4 == 0;
+    const bool quads = D % 4 == 0;
+    const int dw_blocks = (tm * tw * cut.dw + 7) / 8 * 8;
     f32x4 acc[C::TM][C::TN];
     int im, in;
-    if ((int)blockIdx.x < a.dw_blocks) {
-        if (!tile_of_block(blockIdx.x, tm, (a.words + C::BN - 1) / C::BN, im, in)) return;
-        const int m0 = im * C::BM, n0 = in * C::BN;
-        tile_product<C>(acc, a.h_turned, a.dz_turned, m0, n0, 0, count, a.pairs, lds);
+    if ((int)blockIdx.x < dw_blocks) {
+        if (!tile_of_block(blockIdx.x, tm, tw * cut.dw, im, in)) return;
+        const int part = in / tw, m0 = im * C::BM, n0 = (in - part * tw) * C::BN;
+        const int len = ((count + kStepK - 1) / kStepK + cut.dw - 1) / cut.dw * kStepK, k0 = min(count, part * len);
+        tile_product<C>(acc, a.h_turned, a.dz_turned, m0, n0, k0, min(count, k0 + len), a.pairs, lds);
+        const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int v = n0 + (wn * C::TN + j) * 16 + (lane & 15);
-            if (v >= a.words) continue;
+            if (v >= words) continue;
+            const size_t at = (size_t)v * D + d0;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
-                const int d = m0 + (wm * C::TM + i) * 16 + 4 * (lane >> 4);
-                const f32x4 x = acc[i][j] * (1.f / kDzScale);
-                const size_t at = (size_t)v * a.D + d;
-                if (a.bf16_out) {
-                    bf16_t *to = static_cast<bf16_t *>(a.dW) + at;
-                    const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-                    if (quads) {
-                        if (d < a.D) __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(to));
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (d + r < a.D) to[r].bits = (unsigned short)(u[r / 2] >> (16 * (r & 1)));
-                    }
-                } else {
-                    float *to = static_cast<float *>(a.dW) + at;
-                    if (quads) {
-                        if (d < a.D) __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(to));
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (d + r < a.D) to[r] = x[r];
-                    }
-                }
+                if (cut.dw > 1) put4(a.dw_sum + part * a.dw_part + at + 16 * i, acc[i][j], D - d0 - 16 * i, quads);
+                else if (a.bf16_out) put4(static_cast<bf16_t *>(a.dW) + at + 16 * i, acc[i][j] * (1.f / kDzScale), D - d0 - 16 * i, quads);
+                else put4(static_cast<float *>(a.dW) + at + 16 * i, acc[i][j] * (1.f / kDzScale), D - d0 - 16 * i, quads);
             }
         }
         return;
     }
-    const int b = blockIdx.x - a.dw_blocks, tn = (count + C::BN - 1) / C::BN;
-    if (!tile_of_block(b, tm, tn * a.splits, im, in)) return;
-    const int split = in / tn, m0 = im * C::BM, n0 = (in - split * tn) * C::BN;
-    const int k0 = min(split * a.split_words, a.words), k1 = min(a.words, k0 + a.split_words);
+    if (!tile_of_block(blockIdx.x - dw_blocks, tm, th * cut.dh, im, in)) return;
+    const int part = in / th, m0 = im * C::BM, n0 = (in - part * th) * C::BN;
+    const int len = ((words + kStepK - 1) / kStepK + cut.dh - 1) / cut.dh * kStepK, k0 = min(words, part * len);
     Operand dz = a.dz;
     dz.rows = count;
-    tile_product<C>(acc, a.W_turned, dz, m0, n0, k0, k1, a.pairs, lds);
-    float *sums = a.dh_sum + split * a.dh_split;
+    tile_product<C>(acc, a.W_turned, dz, m0, n0, k0, min(words, k0 + len), a.pairs, lds);
+    float *sums = a.dh_sum + part * a.dh_part;
+    const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4);
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
         const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
         if (n >= count) continue;
-        float *to = sums + (size_t)n * a.D + m0 + wm * C::TM * 16 + 4 * (lane >> 4);
-        const int left = a.D - (m0 + wm * C::TM * 16 + 4 * (lane >> 4));
+        float *to = sums + (size_t)n * D + d0;
+        const int left = D - d0;
         if (quads) {
             f32x4 old[C::TM];
 #pragma unroll
@@ -475,20 +526,51 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     }
 }
 
-// dh[n] = sum of the splits of row place[n], scaled back; zeros for rows without a label.  A wave per row.
+// Parts of dW added in order and scaled back, where there are any.
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_dh_finish(const float *__restrict__ sums, size_t split, int splits,
+__global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict__ rows, const float *__restrict__ sums, size_t part, int words,
+                                                         int D, T *__restrict__ dW) {
+    const int parts = rows->cut.dw, v = blockIdx.x * 4 + wave_id();
+    if (parts < 2 || v >= words) return;
+    const bool quads = D % 4 == 0;
+    for (int d = lane_id() * 4; d < D; d += 256) {
+        const size_t at = (size_t)v * D + d;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < parts; ++k) {
+            if (quads) {
+                x += *reinterpret_cast<const f32x4 *>(sums + k * part + at);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d + r < D) x[r] += sums[k * part + at + r];
+            }
+        }
+        put4(dW + at, x * (1.f / kDzScale), D - d, quads);
+    }
+}
+
+// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict__ rows, const float *__restrict__ sums, size_t part,
                                                          const int *__restrict__ place, int N, int D, T *__restrict__ dh) {
     const int n = blockIdx.x * 4 + wave_id();
     if (n >= N) return;
-    const int p = place[n];
-    for (int c = lane_id(); c < D; c += 64) {
-        float x = 0.f;
+    const int p = place[n], parts = rows->cut.dh;
+    const bool quads = D % 4 == 0;
+    for (int d = lane_id() * 4; d < D; d += 256) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (p >= 0)
-            for (int s = 0; s < splits; ++s) x += sums[s * split + (size_t)p * D + c];
-        x *= 1.f / kDzScale;
-        if constexpr (sizeof(T) == 4) dh[(size_t)n * D + c] = x;
-        else dh[(size_t)n * D + c].bits = __builtin_bit_cast(unsigned short, (__bf16)x);
+            for (int k = 0; k < parts; ++k) {
+                const float *from = sums + k * part + (size_t)p * D + d;
+                if (quads) {
+                    x += *reinterpret_cast<const f32x4 *>(from);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (d + r < D) x[r] += from[r];
+                }
+            }
+        put4(dh + (size_t)n * D + d, x * (1.f / kDzScale), D - d, quads);
     }
 }
 
@@ -497,14 +579,19 @@ static size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr size_t kPackBytes = (size_t)128 << 20;      // of f32 words' planes at a time
 constexpr size_t kDzBytes = (size_t)512 << 20;        // of dz and its turned form at a time
+constexpr size_t kPartBytes = (size_t)256 << 20;      // of the parts of dW, and of dh
+// A round of 512 blocks of 128 x 128 against one of 256 blocks of 256 x 256, twice its work at 1315 instead of 1130 TFLOP/s.
+constexpr float kMidRound = 0.5f * 1315 / 1130;
 constexpr size_t kMaxTiles = (size_t)1 << 22;         // of 128 x 128 in a launch: a grid has fewer than 2^32 threads
 
 struct VocabPlan {
     int planes, pitch, turned_pitch;                  // of h and, if packed, of W; of h and dz turned
     bool pack_words;
     int piece;                                        // words per piece, a multiple of 256
-    int dz_planes, splits;
-    size_t count, rows, place, hp, ht, wp, wt, dzt, part_max, part_sum, part_z, z_label, dz, dh, total;
+    int dz_planes;
+    bool big_grads;
+    CutArgs cut;
+    size_t count, rows, place, hp, ht, wp, wt, dzt, dw, part_max, part_sum, part_z, z_label, dz, dh, total;
     size_t h_plane, ht_plane, w_plane, wt_plane, dz_plane, dzt_plane, part_pitch;
     int tiles;                                        // most tiles along the vocabulary
 };
@@ -519,6 +606,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
     if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
     if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (4 * p.dz_planes * N) / 256 * 256, 256));
+    piece = up((V + (V + piece - 1) / piece - 1) / ((V + piece - 1) / piece), 256);   // pieces of about the same width
     p.piece = (int)piece;
     p.h_plane = N * p.pitch;
     p.w_plane = piece * p.pitch;
@@ -529,14 +617,34 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.dzt_plane = piece * p.turned_pitch;
     p.part_pitch = up(N, 64);
     p.tiles = (int)(up(V, piece) / piece * (piece / 128));
-    p.splits = 1;
+    if (bwd) {
+        CutArgs cuts[2];
+        float times[2];
+        for (int big = 0; big < 2; ++big) {
+            CutArgs &c = cuts[big];
+            c = CutArgs{(int)std::min(piece, V), (int)D, 1, 1, big ? 256 : 128, big ? 256 : 512, p.planes == 3 ? 6 : p.dz_planes, big ? 1.f : kMidRound};
+            c.most_dw = (int)std::min<size_t>(kMostParts, std::max<size_t>(1, kPartBytes / (piece * D * 4)));
+            c.most_dh = (int)std::min<size_t>(kMostParts, std::max<size_t>(1, kPartBytes / (N * D * 4)));
+            // room for what the numbers of rows with a label from a quarter to all of N ask for
+            Cut most = {1, 1};
+            for (int k = 4; k <= 16; ++k) {
+                const Cut x = cut_of(c, (int)((N * k + 15) / 16), &times[big]);
+                most.dw = std::max(most.dw, x.dw);
+                most.dh = std::max(most.dh, x.dh);
+            }
+            c.most_dw = most.dw;
+            c.most_dh = most.dh;
+        }
+        p.big_grads = times[1] <= times[0];
+        p.cut = cuts[p.big_grads];
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at += up(bytes, 256);
         return here;
     };
-    p.count = take(4);
+    p.count = take(sizeof(Rows));
     p.rows = take(N * 4);
     p.place = take(N * 4);
     p.hp = take(p.planes * p.h_plane * 2);
@@ -551,10 +659,17 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
         p.wt = take(p.planes * p.wt_plane * 2);
         p.dz = take(p.dz_planes * p.dz_plane * 2);
         p.dzt = take(p.dz_planes * p.dzt_plane * 2);
-        p.dh = take((size_t)p.splits * N * D * 4);
+        if (p.cut.most_dw > 1) p.dw = take(p.cut.most_dw * piece * D * 4);
+        p.dh = take(p.cut.most_dh * N * D * 4);
     }
     p.total = at;
     return p;
+}
+
+// Which tile the logits take: rounds of 256 blocks of 256 x 256 against rounds of 512 (two to a compute unit) of 128 x 128.
+static bool big_logits(size_t words, size_t N) {
+    const size_t big = (up(words, 256) / 256) * (up(N, 256) / 256), mid = (up(words, 128) / 128) * (up(N, 128) / 128);
+    return (float)((big + 255) / 256) <= kMidRound * (float)((mid + 511) / 512);
 }
 
 static PlanePairs pairs_of(int a, int b) {             // planes of the operands: nibbles, the small terms first
@@ -582,11 +697,10 @@ template <class C, bool BWD> static echo_status_t launch_logits(const LogitsArgs
     return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, BWD>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
                         C::THREADS, a, st);
 }
-template <class C> static echo_status_t launch_grads(GradsArgs a, int N, hipStream_t st) {
+template <class C> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
     static LdsGrants granted{};
-    const long long tm = (a.D + C::BM - 1) / C::BM;
-    a.dw_blocks = a.dW ? (int)(((a.words + C::BN - 1) / C::BN * tm + 7) / 8 * 8) : 0;
-    const long long blocks = a.dw_blocks + (a.dh_sum ? (N + C::BN - 1) / C::BN * tm * a.splits : 0);
+    const long long tm = (a.D + C::BM - 1) / C::BM, tw = (a.words + C::BN - 1) / C::BN, th = (N + C::BN - 1) / C::BN;
+    const long long blocks = (tm * tw * (a.dW ? cut.most_dw : 0) + 7) / 8 * 8 + tm * th * (a.dh_sum ? cut.most_dh : 0);
     return launch_tiles("vocab_grads", &k_vocab_grads<C>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
 }
 
@@ -615,11 +729,12 @@ struct VocabRun {
     template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
 
     // the rows with a label; turned: in their turned form too
-    echo_status_t gather(bool turned) const {
+    echo_status_t gather(bool turned, const CutArgs &cut) const {
         LaunchRecord r = launch_begin("vocab_rows", st);
-        k_vocab_rows<<<(d.N + kRowsBlock - 1) / kRowsBlock, 256, 0, st>>>(labels, d.N, d.V, at<int>(p.rows), at<int>(p.place), at<int>(p.count));
+        k_vocab_rows<<<(d.N + kRowsBlock - 1) / kRowsBlock, 256, 0, st>>>(labels, d.N, d.V, at<int>(p.rows), at<int>(p.place), at<Rows>(p.count),
+                                                                             cut);
         if (echo_status_t s = launch_end(r)) return s;
-        return pack("vocab_pack_rows", PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<int>(p.count), at<bf16_t>(p.hp),
+        return pack("vocab_pack_rows", PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<Rows>(p.count), at<bf16_t>(p.hp),
                                                 turned ? at<bf16_t>(p.ht) : nullptr, p.h_plane, p.ht_plane});
     }
     echo_status_t pack(const char *name, const PackArgs &a) const {
@@ -663,12 +778,12 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V;
-    if (echo_status_t s = x.gather(false)) return s;
+    if (echo_status_t s = x.gather(false, CutArgs{})) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = x.p.pitch;
     a.pairs = pairs_of(x.p.planes, x.p.planes);
-    a.count = x.at<int>(x.p.count);
+    a.count = x.at<Rows>(x.p.count);
     a.rows = x.at<int>(x.p.rows);
     a.labels = labels;
     a.V = V;
@@ -678,7 +793,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     a.part_z = x.at<float>(x.p.part_z);
     a.z_label = x.at<float>(x.p.z_label);
     a.pitch = x.p.part_pitch;
-    const bool big = (long long)((V + 255) / 256) * ((N + 255) / 256) >= 512;
+    const bool big = big_logits(std::min(x.p.piece, V), N);
     int tiles = 0;
     for (int v0 = 0; v0 < V; v0 += x.p.piece) {
         const int n = std::min(x.p.piece, V - v0);
@@ -705,12 +820,12 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V, D = desc->D;
     const VocabPlan &p = x.p;
-    if (echo_status_t s = x.gather(dW != nullptr)) return s;
+    if (echo_status_t s = x.gather(dW != nullptr, x.p.cut)) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = p.pitch;
     a.pairs = pairs_of(p.planes, p.planes);
-    a.count = x.at<int>(p.count);
+    a.count = x.at<Rows>(p.count);
     a.rows = x.at<int>(p.rows);
     a.labels = labels;
     a.V = V;
@@ -728,32 +843,37 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     g.dz = Operand{a.dz, p.dz_plane, p.piece, N};
     g.h_turned = Operand{x.at<bf16_t>(p.ht), p.ht_plane, p.turned_pitch, p.pitch};
     g.W_turned = Operand{x.at<bf16_t>(p.wt), p.wt_plane, p.piece, p.pitch};
-    g.count = a.count;
+    g.rows = a.count;
     g.D = D;
     g.pairs = pairs_of(p.planes, p.dz_planes);
+    g.dw_sum = x.at<float>(p.dw);
+    g.dw_part = (size_t)p.piece * D;
     g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
-    g.dh_split = (size_t)N * D;
-    g.splits = p.splits;
+    g.dh_part = (size_t)N * D;
     g.bf16_out = desc->out_dtype == ECHO_BF16;
     const size_t out_bytes = g.bf16_out ? 2 : 4;
+    const bool big = big_logits(std::min(p.piece, V), N);
     for (int v0 = 0; v0 < V; v0 += p.piece) {
         const int n = std::min(p.piece, V - v0);
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
-        const bool big = (long long)((n + 255) / 256) * ((N + 255) / 256) >= 512;
         if (echo_status_t s = big ? launch_logits<BigTile, true>(a, N, x.st) : launch_logits<MidTile, true>(a, N, x.st)) return s;
         g.words = n;
         g.dz_turned = Operand{a.turned, p.dzt_plane, p.turned_pitch, n};
         g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
         g.add = v0 > 0;
-        g.split_words = (int)up((n + g.splits - 1) / g.splits, 64);
-        const long long tiles = ((long long)(n + 255) / 256 + (N + 255) / 256) * ((D + 255) / 256);
-        if (echo_status_t s = tiles >= 512 ? launch_grads<BigTile>(g, N, x.st) : launch_grads<MidTile>(g, N, x.st)) return s;
+        if (echo_status_t s = p.big_grads ? launch_grads<BigTile>(g, p.cut, N, x.st) : launch_grads<MidTile>(g, p.cut, N, x.st)) return s;
+        if (dW && p.cut.most_dw > 1) {
+            LaunchRecord r = launch_begin("vocab_dw_finish", x.st);
+            if (g.bf16_out) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
+            else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
+            if (echo_status_t s = launch_end(r)) return s;
+        }
     }
     if (!dh) return ECHO_OK;
     LaunchRecord r = launch_begin("vocab_dh_finish", x.st);
-    if (g.bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.dh_sum, g.dh_split, g.splits, x.at<int>(p.place), N, D, static_cast<bf16_t *>(dh));
-    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.dh_sum, g.dh_split, g.splits, x.at<int>(p.place), N, D, static_cast<float *>(dh));
+    if (g.bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), N, D, static_cast<bf16_t *>(dh));
+    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), N, D, static_cast<float *>(dh));
     return launch_end(r);
 }
 
