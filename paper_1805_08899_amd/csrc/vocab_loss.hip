@@ -368,6 +368,276 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     }
 }
 
+// ---- few rows -----------------------------------------------------------------------------------------------------------
+// Up to 64 rows (a decoder step scored, one token): bound by reading the words once.  Every wave takes words straight from memory as operands (f32
+// ones are split in registers) and multiplies them with all rows; no rows are gathered, and a block's maxima, sums and label logits go to part
+// [row][tile].  Up to 16 rows each wave works on its own, the rows coming to it from the caches as operands too.  For more rows that would be more
+// bytes than the caches deliver (64 f32 rows as planes: 256 MB, 36 us), so a block of eight waves passes the rows through LDS as planes.
+constexpr int kFewRows = 64, kFewAlone = 16;
+template <typename T> static bool few_rows_apply(int N, int D) { return N <= kFewRows && D % (16 / (int)sizeof(T)) == 0; }
+constexpr int few_words(int rows) { return rows <= kFewAlone ? 64 : 128; }     // per block of four or eight waves of 16 words
+
+struct FewArgs {
+    const void *h, *W;
+    const int *labels;
+    int N, V, D, tiles;
+    float eps;
+    float *part_max, *part_sum, *part_z, *z_label;
+};
+
+// 16 rows x 32 k of a matrix as an operand: as loaded (lane l: row l % 16, k = 8 (l / 16) .. + 7), and as planes
+template <typename T> struct FewFragment {
+    static constexpr int LOADS = (int)sizeof(T) / 2, PLANES = sizeof(T) == 4 ? 3 : 1;
+    u32x4 raw[LOADS];
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rsrc, unsigned row_off, int k, int D) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = k + 4 * i;
+            raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at < D ? row_off + at * (unsigned)sizeof(T) : kOutside, 0, 0));
+        }
+    }
+    __device__ __forceinline__ void planes(u32x4 (&p)[PLANES]) const {
+        if constexpr (PLANES == 1) {
+            p[0] = raw[0];
+        } else {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(raw[j / 4][j % 4]);
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned u = bf16_pair(x[2 * j], x[2 * j + 1]);
+                    x[2 * j] -= __uint_as_float(u << 16);
+                    x[2 * j + 1] -= __uint_as_float(u & 0xffff0000u);
+                    p[i][j] = u;
+                }
+        }
+    }
+};
+template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 (&a)[PLANES], const u32x4 (&b)[PLANES], f32x4 c) {
+    if constexpr (PLANES == 3) {                                               // the small terms first
+        c = mfma16(a[1], b[1], c);
+        c = mfma16(a[2], b[0], c);
+        c = mfma16(a[0], b[2], c);
+        c = mfma16(a[1], b[0], c);
+        c = mfma16(a[0], b[1], c);
+    }
+    return mfma16(a[0], b[0], c);
+}
+
+// The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
+template <int NT, int WAVES>
+__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int v0, float *s_max, float *s_sum, float *s_z) {
+    constexpr int ROWS = 16 * NT;
+    const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int n = 16 * j + (lane & 15), y = n < a.N ? a.labels[n] - vw : -1;
+        float z = 0.f, top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (vw + r >= a.V) {
+                acc[j][r] = -__builtin_inff();
+            } else {
+                z += acc[j][r];
+                if (y == r) {                                                  // the label's logit is left out of maximum and sum
+                    a.z_label[n] = acc[j][r];
+                    acc[j][r] = -__builtin_inff();
+                }
+            }
+            top = fmaxf(top, acc[j][r]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float at = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[j][r] - at) * kLog2e);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        z += __shfl_xor(z, 16);
+        z += __shfl_xor(z, 32);
+        if (lane < 16) s_max[w * ROWS + n] = top, s_sum[w * ROWS + n] = sum, s_z[w * ROWS + n] = z;
+    }
+    __syncthreads();
+    const int n = threadIdx.x;
+    if (n >= a.N) return;
+    float top = s_max[n], sum = 0.f, z = 0.f;
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) top = fmaxf(top, s_max[k * ROWS + n]);
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) {
+        sum += scaled_sum(s_sum[k * ROWS + n], s_max[k * ROWS + n], top);
+        z += s_z[k * ROWS + n];
+    }
+    const size_t at = (size_t)n * a.tiles + blockIdx.x;
+    a.part_max[at] = top;
+    a.part_sum[at] = sum;
+    a.part_z[at] = z;
+}
+
+// AHEAD: how many times 32 k are on their way.
+template <typename T, int AHEAD>
+__global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
+    constexpr int PLANES = FewFragment<T>::PLANES;
+    __shared__ float s_max[64], s_sum[64], s_z[64];
+    const int lane = lane_id(), v0 = (blockIdx.x * 4 + wave_id()) * 16, steps = (a.D + 31) / 32, k_lane = 8 * (lane >> 4);
+    const int first = min(v0, a.V - 1);
+    const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(a.W) + (size_t)first * a.D), 0, 0x7ffffff0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.h), 0, 0x7ffffff0, 0x00020000);
+    const unsigned word_off = (unsigned)(min(lane & 15, a.V - 1 - first) * a.D) * sizeof(T);
+    const unsigned row_off = (unsigned)(min(lane & 15, a.N - 1) * a.D) * sizeof(T);
+    FewFragment<T> fw[AHEAD], fh[AHEAD];
+    auto fetch = [&](int d, int t) __attribute__((always_inline)) {
+        fw[d].load(words, word_off, 32 * t + k_lane, a.D);
+        fh[d].load(rows, row_off, 32 * t + k_lane, a.D);
+        loads_stay();
+    };
+    f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+        if (d < steps) fetch(d, d);
+    for (int t0 = 0; t0 < steps; t0 += AHEAD)
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            if (t0 + d >= steps) break;
+            u32x4 pw[PLANES], ph[PLANES];
+            fw[d].planes(pw);
+            fh[d].planes(ph);
+            if (t0 + d + AHEAD < steps) fetch(d, t0 + d + AHEAD);
+            acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
+        }
+    few_join<1, 4>(a, acc, v0, s_max, s_sum, s_z);
+}
+
+// 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
+constexpr int kFewK = 128, kFewPitch = kFewK * 2 + 16;                         // bytes of a row in LDS: 16 rows of a fragment take all banks
+template <typename T, int NT>
+__global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs a) {
+    constexpr int PLANES = FewFragment<T>::PLANES, SUB = kFewK / 32, ROWS = 16 * NT, WAVES = 8;
+    constexpr int GROUPS = ROWS * kFewK / 8, ITEMS = (GROUPS + 64 * WAVES - 1) / (64 * WAVES);      // groups of 8 numbers of the rows, per thread
+    constexpr int STAGE = PLANES * ROWS * kFewPitch;
+    __shared__ __align__(16) char s_h[2 * STAGE];
+    __shared__ float s_max[WAVES * ROWS], s_sum[WAVES * ROWS], s_z[WAVES * ROWS];
+    const int lane = lane_id(), v0 = (blockIdx.x * WAVES + wave_id()) * 16, steps = (a.D + kFewK - 1) / kFewK, k_lane = 8 * (lane >> 4);
+    const int first = min(v0, a.V - 1);
+    const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(a.W) + (size_t)first * a.D), 0, 0x7ffffff0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.h), 0, 0x7ffffff0, 0x00020000);
+    const unsigned word_off = (unsigned)(min(lane & 15, a.V - 1 - first) * a.D) * sizeof(T);
+    FewFragment<T> fw[2][SUB], fh[ITEMS];
+    auto fetch_words = [&](int buf, int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) fw[buf][s].load(words, word_off, t * kFewK + 32 * s + k_lane, a.D);
+    };
+    auto fetch_rows = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int g = i * 64 * WAVES + threadIdx.x, n = min(g / (kFewK / 8), a.N - 1), k = t * kFewK + g % (kFewK / 8) * 8;
+            fh[i].load(rows, (unsigned)(n * a.D) * sizeof(T), k, a.D);
+        }
+    };
+    auto put_rows = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int g = i * 64 * WAVES + threadIdx.x;
+            u32x4 p[PLANES];
+            fh[i].planes(p);
+            if (GROUPS % (64 * WAVES) == 0 || g < GROUPS) {
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k)
+                    *reinterpret_cast<u32x4 *>(s_h + (t & 1) * STAGE + (k * ROWS + g / (kFewK / 8)) * kFewPitch + g % (kFewK / 8) * 16) = p[k];
+            }
+        }
+    };
+    f32x4 acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    fetch_rows(0);
+    fetch_words(0, 0);
+    fetch_words(1, 1);
+    loads_stay();
+    put_rows(0);
+    lds_barrier();
+    auto step = [&](int t, FewFragment<T> (&f)[SUB]) __attribute__((always_inline)) {
+        u32x4 pw[SUB][PLANES];
+        if (t + 1 < steps) fetch_rows(t + 1);                                  // in front of the words behind it: loads arrive in order
+        loads_stay();
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) f[s].planes(pw[s]);
+        if (t + 2 < steps) {
+#pragma unroll
+            for (int s = 0; s < SUB; ++s) f[s].load(words, word_off, (t + 2) * kFewK + 32 * s + k_lane, a.D);
+        }
+        loads_stay();
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+            const char *from = s_h + (t & 1) * STAGE + (lane & 15) * kFewPitch + (4 * s + (lane >> 4)) * 16;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                u32x4 ph[PLANES];
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k) ph[k] = *reinterpret_cast<const u32x4 *>(from + (k * ROWS + 16 * j) * kFewPitch);
+                acc[j] = few_multiply<PLANES>(pw[s], ph, acc[j]);
+            }
+        }
+        if (t + 1 < steps) put_rows(t + 1);
+        lds_barrier();
+    };
+    for (int t = 0; t < steps; t += 2) {
+        step(t, fw[0]);
+        if (t + 1 < steps) step(t + 1, fw[1]);
+    }
+    few_join<NT, WAVES>(a, acc, v0, s_max, s_sum, s_z);
+}
+
+// loss and lse of a row from its maximum, sum and sum of logits without and with the label:
+// -log p of the label: log(1 + sum over the other words of exp(z - z_label)), which keeps the digits of a sure label's loss
+__device__ __forceinline__ void loss_of_row(float top, float sum, float z, float zl, int V, float eps, float &loss, float &lse) {
+    const float t = top - zl;
+    const float nll = t > 0.f ? t + logf(sum + expf(-t)) : log1pf(sum * expf(t));
+    lse = zl + nll;
+    loss = nll;
+    if (eps > 0.f) loss += eps * (zl - z / (float)V);
+}
+
+// A block per row.
+__global__ __launch_bounds__(256) void k_vocab_few_finish(const FewArgs a, float *__restrict__ loss, float *__restrict__ lse) {
+    __shared__ float s_max[4], s_sum[4], s_z[4];
+    const int n = blockIdx.x, lane = lane_id(), w = wave_id(), y = a.labels[n];
+    if ((unsigned)y >= (unsigned)a.V) {
+        if (threadIdx.x == 0) loss[n] = 0.f, lse[n] = 0.f;
+        return;
+    }
+    float top = -__builtin_inff(), sum = 0.f, z = 0.f;
+    for (int t0 = threadIdx.x; t0 < a.tiles; t0 += 1024) {
+        float m[4], s[4], zz[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const size_t at = (size_t)n * a.tiles + min(t0 + 256 * u, a.tiles - 1);
+            m[u] = a.part_max[at], s[u] = a.part_sum[at], zz[u] = a.part_z[at];
+        }
+        float next = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) next = fmaxf(next, m[u]);
+        sum = scaled_sum(sum, top, next);
+        top = next;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (t0 + 256 * u < a.tiles) sum += scaled_sum(s[u], m[u], top), z += zz[u];
+    }
+    const float wave_top = wave_max(top);
+    sum = wave_sum(scaled_sum(sum, top, wave_top));
+    z = wave_sum(z);
+    if (lane == 0) s_max[w] = wave_top, s_sum[w] = sum, s_z[w] = z;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+    sum = 0.f, z = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum += scaled_sum(s_sum[k], s_max[k], top), z += s_z[k];
+    loss_of_row(top, sum, z, a.z_label[n], a.V, a.eps, loss[n], lse[n]);
+}
+
 // Joins the tiles of 64 rows: four waves take a quarter of the tiles each, lanes are rows.  Rows without a label get zeros.
 __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restrict__ part_max, const float *__restrict__ part_sum,
                                                            const float *__restrict__ part_z, const float *__restrict__ z_label,
@@ -415,12 +685,7 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
             sum += scaled_sum(s_sum[k][lane], s_max[k][lane], all);
             z += s_z[k][lane];
         }
-        // -log p of the label: log(1 + sum over the other words of exp(z - z_label)), which keeps the digits of a sure label's loss
-        const float zl = z_label[p], t = all - zl;
-        const float nll = t > 0.f ? t + logf(sum + expf(-t)) : log1pf(sum * expf(t));
-        e = zl + nll;
-        l = nll;
-        if (eps > 0.f) l += eps * (zl - z / (float)V);
+        loss_of_row(all, sum, z, z_label[p], V, eps, l, e);
     }
     loss[n] = l;
     lse[n] = e;
@@ -586,7 +851,7 @@ constexpr size_t kMaxTiles = (size_t)1 << 22;         // of 128 x 128 in a launc
 
 struct VocabPlan {
     int planes, pitch, turned_pitch;                  // of h and, if packed, of W; of h and dz turned
-    bool pack_words;
+    bool pack_words, few;                             // few: forward of few rows
     int piece;                                        // words per piece, a multiple of 256
     int dz_planes;
     bool big_grads;
@@ -603,6 +868,16 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.pitch = (int)up(D, 8);
     p.pack_words = d.in_dtype == ECHO_F32 || D % 8 != 0;
     p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 2;
+    p.few = !bwd && (d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : few_rows_apply<bf16_t>(d.N, d.D));
+    if (p.few) {
+        p.tiles = (int)((V + few_words(d.N) - 1) / few_words(d.N));
+        const size_t part = up(N * p.tiles * 4, 256);
+        p.part_sum = part;
+        p.part_z = 2 * part;
+        p.z_label = 3 * part;
+        p.total = 3 * part + up(N * 4, 256);
+        return p;
+    }
     size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
     if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
     if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (4 * p.dz_planes * N) / 256 * 256, 256));
@@ -691,6 +966,11 @@ static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &grante
     return launch_end(r);
 }
 
+template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
+    if (a.N <= kFewAlone) k_vocab_few_alone<T, sizeof(T) == 2 ? 8 : 6><<<a.tiles, 256, 0, st>>>(a);
+    else if (a.N <= 32) k_vocab_few_shared<T, 2><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<T, 4><<<a.tiles, 512, 0, st>>>(a);
+}
 template <class C, bool BWD> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
@@ -778,6 +1058,17 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V;
+    if (x.p.few) {
+        const FewArgs a{h, W, labels, N, V, desc->D, x.p.tiles, label_smoothing, x.at<float>(x.p.part_max), x.at<float>(x.p.part_sum),
+                        x.at<float>(x.p.part_z), x.at<float>(x.p.z_label)};
+        LaunchRecord r = launch_begin("vocab_few", x.st);
+        if (desc->in_dtype == ECHO_F32) launch_few<float>(a, x.st);
+        else launch_few<bf16_t>(a, x.st);
+        if (echo_status_t s = launch_end(r)) return s;
+        r = launch_begin("vocab_few_finish", x.st);
+        k_vocab_few_finish<<<N, 256, 0, x.st>>>(a, loss, lse);
+        return launch_end(r);
+    }
     if (echo_status_t s = x.gather(false, CutArgs{})) return s;
     LogitsArgs a{};
     a.h = x.rows();
