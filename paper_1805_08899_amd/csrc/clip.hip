@@ -39,17 +39,34 @@ struct ClipTable {
     int count;
 };
 
-// the tensor that span s belongs to: the last one whose first span is not behind s (tensors without elements have no span: they
-// are not in the table)
-__device__ __forceinline__ int clip_find(const ClipTable &tab, long long s) {
-    int lo = 0, hi = tab.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if ((tab.t[mid].first_bf16 >> 1) <= s) lo = mid;
-        else hi = mid - 1;
+// A span: where it begins, and how much of its tensor is left there.  The tensor is the last one whose first span is not behind this one
+// (tensors without elements have no span: they are not in the table); the lanes look at all of the table at once, one trip to
+// memory where a search would take seven.
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+constexpr int kSpanLoads = kSpanBytes / 16 / kClipThreads;
+struct ClipSpan {
+    const char *src;
+    char *dst;
+    long long left;                   // elements
+    bool bf16;
+    __device__ __forceinline__ bool whole() const { return left * (bf16 ? 2 : 4) >= kSpanBytes; }
+    __device__ __forceinline__ void find(const ClipTable &tab, long long s) {
+        static_assert(kClipBatch <= 128, "two tensors per lane");
+        const int l = lane_id();
+        const int i = __builtin_popcountll(__ballot(l < tab.count && (tab.t[min(l, kClipBatch - 1)].first_bf16 >> 1) <= s)) +
+                      __builtin_popcountll(__ballot(l + 64 < tab.count && (tab.t[min(l + 64, kClipBatch - 1)].first_bf16 >> 1) <= s)) - 1;
+        const ClipTensor &t = tab.t[i];
+        bf16 = t.first_bf16 & 1;
+        const long long size = bf16 ? 2 : 4, begin = (s - (t.first_bf16 >> 1)) * (kSpanBytes / size);
+        src = static_cast<const char *>(t.src) + begin * size;
+        dst = static_cast<char *>(t.dst) + begin * size;
+        left = t.n - begin;
     }
-    return lo;
-}
+    __device__ __forceinline__ void load(u4 (&v)[kSpanLoads]) const {          // of a whole span
+#pragma unroll
+        for (int k = 0; k < kSpanLoads; ++k) v[k] = *reinterpret_cast<const u4 *>(src + (k * kClipThreads + threadIdx.x) * 16);
+    }
+};
 
 __device__ __forceinline__ void clip_square(double &acc, float x) { acc = __builtin_fma((double)x, (double)x, acc); }
 __device__ __forceinline__ float bf_lo(unsigned u) { return __uint_as_float(u << 16); }
@@ -76,24 +93,21 @@ __device__ __forceinline__ double block_sum_f64(double x, double *s) {
 }
 
 __global__ __launch_bounds__(kClipThreads) void k_grad_norm(const ClipTable tab, double *parts) {
-    __shared__ double s[kClipThreads / 64];
+    __shared__ double s_sum[kClipThreads / 64];
     double acc[4] = {0., 0., 0., 0.};
+    ClipSpan s;
+    if (blockIdx.x < tab.spans) s.find(tab, blockIdx.x);
     for (long long span = blockIdx.x; span < tab.spans; span += gridDim.x) {
-        const ClipTensor &t = tab.t[clip_find(tab, span)];
-        const bool bf = t.first_bf16 & 1;
-        const long long size = bf ? 2 : 4, begin = (span - (t.first_bf16 >> 1)) * (kSpanBytes / size);
-        const char *p = static_cast<const char *>(t.src) + begin * size;
-        const long long left = t.n - begin;                                   // elements from here to the tensor's end
-        if (left * size >= kSpanBytes) {
-            typedef unsigned u4 __attribute__((ext_vector_type(4)));
-            u4 v[4];
+        const ClipSpan here = s;
+        u4 v[kSpanLoads];
+        if (here.whole()) here.load(v);
+        if (span + gridDim.x < tab.spans) s.find(tab, span + gridDim.x);      // while the loads are under way
+        if (here.whole()) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const u4 *>(p + (k * kClipThreads + threadIdx.x) * 16);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kSpanLoads; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (bf) {
+                    if (here.bf16) {
                         clip_square(acc[j], bf_lo(v[k][j]));
                         clip_square(acc[j], bf_hi(v[k][j]));
                     } else {
@@ -101,12 +115,12 @@ __global__ __launch_bounds__(kClipThreads) void k_grad_norm(const ClipTable tab,
                     }
                 }
         } else {
-            for (int i = threadIdx.x; i < (int)left; i += kClipThreads)
-                clip_square(acc[0], bf ? __uint_as_float((unsigned)reinterpret_cast<const unsigned short *>(p)[i] << 16)
-                                       : reinterpret_cast<const float *>(p)[i]);
+            for (int i = threadIdx.x; i < (int)here.left; i += kClipThreads)
+                clip_square(acc[0], here.bf16 ? __uint_as_float((unsigned)reinterpret_cast<const unsigned short *>(here.src)[i] << 16)
+                                              : reinterpret_cast<const float *>(here.src)[i]);
         }
     }
-    const double sum = block_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]), s);
+    const double sum = block_sum_f64((acc[0] + acc[1]) + (acc[2] + acc[3]), s_sum);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
@@ -124,44 +138,43 @@ __global__ __launch_bounds__(kClipThreads) void k_grad_norm_finish(const double 
 
 __global__ __launch_bounds__(kClipThreads) void k_grad_scale(const ClipTable tab, const double *parts, int n_parts,
                                                              float max_norm, float *norm) {
-    __shared__ double s[kClipThreads / 64];
-    const double x = grad_norm_of(parts, n_parts, s);
+    __shared__ double s_sum[kClipThreads / 64];
+    // the block's first span is on its way before the norm is worked out
+    ClipSpan s;
+    u4 v[kSpanLoads];
+    const bool any = blockIdx.x < tab.spans;
+    if (any) s.find(tab, tab.spans - 1 - blockIdx.x);
+    if (any && s.whole()) s.load(v);
+    const double x = grad_norm_of(parts, n_parts, s_sum);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
     // false for NaN; an infinite norm clips nothing either
     const bool clip = x > (double)max_norm && x < __builtin_inf();
     const float f = clip ? (float)((double)max_norm / x) : 1.0f;
     for (long long r = blockIdx.x; r < tab.spans; r += gridDim.x) {
-        const long long span = tab.spans - 1 - r;
-        const ClipTensor &t = tab.t[clip_find(tab, span)];
-        if (!clip && t.src == t.dst) continue;
-        const bool bf = t.first_bf16 & 1;
-        const long long size = bf ? 2 : 4, begin = (span - (t.first_bf16 >> 1)) * (kSpanBytes / size);
-        const char *p = static_cast<const char *>(t.src) + begin * size;
-        char *q = static_cast<char *>(t.dst) + begin * size;
-        const long long left = t.n - begin;
-        if (left * size >= kSpanBytes) {
-            typedef unsigned u4 __attribute__((ext_vector_type(4)));
-            u4 v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const u4 *>(p + (k * kClipThreads + threadIdx.x) * 16);
+        if (r > blockIdx.x) {
+            s.find(tab, tab.spans - 1 - r);
+            if (s.whole() && (clip || s.src != s.dst)) s.load(v);
+        }
+        if (!clip && s.src == s.dst) continue;
+        if (s.whole()) {
             if (clip) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                for (int k = 0; k < kSpanLoads; ++k)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        v[k][j] = bf ? bf16_round2(bf_lo(v[k][j]) * f, bf_hi(v[k][j]) * f) : __float_as_uint(__uint_as_float(v[k][j]) * f);
+                        v[k][j] = s.bf16 ? bf16_round2(bf_lo(v[k][j]) * f, bf_hi(v[k][j]) * f) : __float_as_uint(__uint_as_float(v[k][j]) * f);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                __builtin_nontemporal_store(v[k], reinterpret_cast<u4 *>(q + (k * kClipThreads + threadIdx.x) * 16));
+            for (int k = 0; k < kSpanLoads; ++k)
+                __builtin_nontemporal_store(v[k], reinterpret_cast<u4 *>(s.dst + (k * kClipThreads + threadIdx.x) * 16));
         } else {
-            for (int i = threadIdx.x; i < (int)left; i += kClipThreads) {
-                if (bf) {
-                    const unsigned short u = reinterpret_cast<const unsigned short *>(p)[i];
-                    reinterpret_cast<unsigned short *>(q)[i] = clip ? bf16_round(__uint_as_float((unsigned)u << 16) * f) : u;
+            for (int i = threadIdx.x; i < (int)s.left; i += kClipThreads) {
+                if (s.bf16) {
+                    const unsigned short u = reinterpret_cast<const unsigned short *>(s.src)[i];
+                    reinterpret_cast<unsigned short *>(s.dst)[i] = clip ? bf16_round(__uint_as_float((unsigned)u << 16) * f) : u;
                 } else {
-                    const float u = reinterpret_cast<const float *>(p)[i];
-                    reinterpret_cast<float *>(q)[i] = clip ? u * f : u;
+                    const float u = reinterpret_cast<const float *>(s.src)[i];
+                    reinterpret_cast<float *>(s.dst)[i] = clip ? u * f : u;
                 }
             }
         }
