@@ -1,4 +1,4 @@
-// Tiled products of bf16 matrices with fp32 sums on the matrix cores, for the vocabulary loss: C[m, n] = sum_k A(m, k) B(n, k).
+// Tiled products of bf16 (HALF: fp16) matrices with fp32 sums on the matrix cores, for the vocabulary loss: C[m, n] = sum_k A(m, k) B(n, k).
 //
 // Both operands have their rows along k: element (m, k) at m * pitch + k, pitch a multiple of 8, first element 16-byte aligned.  An operand may
 // consist of several planes, whose sum it is; the product then is the sum over a list of plane pairs, one pair's whole k axis after another's, which
@@ -51,8 +51,10 @@ constexpr unsigned kOutside = 0x80000000u;                                     /
 
 typedef __attribute__((address_space(3))) void *lds_ptr;
 
-__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {           // 32 k: lane l: row l % 16, k = 8 (l / 16) .. + 7
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <bool HALF = false> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {   // 32 k: lane l: row l % 16, k = 8 (l / 16) .. + 7
+    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 // accumulator r of lane l: row 4 (l / 16) + r, column l % 16
 
@@ -94,7 +96,7 @@ template <int N> __device__ __forceinline__ void wait_loads() {
     asm volatile("" ::: "memory");
 }
 
-template <class C> struct Pipeline {
+template <class C, bool HALF> struct Pipeline {
     static constexpr int TM = C::TM, TN = C::TN, F = TM + TN;
     typedef Loader<C::BM, C::WAVES> LoadA;
     typedef Loader<C::BN, C::WAVES> LoadB;
@@ -141,7 +143,7 @@ template <class C> struct Pipeline {
     static constexpr int PER = 16, G = TM * TN / PER;
     __device__ __forceinline__ void multiply(Acc &acc, int buf, int g) {
 #pragma unroll
-        for (int x = g * PER; x < (g + 1) * PER; ++x) acc[x / TN][x % TN] = mfma16(fa[buf][x / TN], fb[buf][x % TN], acc[x / TN][x % TN]);
+        for (int x = g * PER; x < (g + 1) * PER; ++x) acc[x / TN][x % TN] = mfma16<HALF>(fa[buf][x / TN], fb[buf][x % TN], acc[x / TN][x % TN]);
     }
     __device__ __forceinline__ void step_ahead(Acc &acc, int t, char *a, char *b, const char *next_a, const char *next_b) {
 #pragma unroll
@@ -201,7 +203,7 @@ template <class C> struct Pipeline {
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(fa[0][i], fb[0][j], acc[i][j]);
+                        for (int j = 0; j < TN; ++j) acc[i][j] = mfma16<HALF>(fa[0][i], fb[0][j], acc[i][j]);
                 }
             }
         }
@@ -210,11 +212,11 @@ template <class C> struct Pipeline {
 
 // acc[i][j]: rows m0 + 16 (wm TM + i), columns n0 + 16 (wn TN + j) of the product over k_begin <= k < k_end (k_begin a multiple of 64).
 // On return all waves are done with LDS.
-template <class C>
+template <class C, bool HALF = false>
 __device__ __forceinline__ void tile_product(f32x4 (&acc)[C::TM][C::TN], const Operand &A, const Operand &B, int m0, int n0, int k_begin,
                                              int k_end, const PlanePairs &pairs, char *lds) {
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
-    Pipeline<C> p;
+    Pipeline<C, HALF> p;
     p.la.init(A, m0, k_begin, w, lane);
     p.lb.init(B, n0, k_begin, w, lane);
 #pragma unroll

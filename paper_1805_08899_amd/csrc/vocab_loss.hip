@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -25,7 +26,8 @@
 namespace echo {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kDzScale = 0x1p24f;                   // on dz while it is in bf16 planes: small probabilities keep their digits (split.hpp)
+constexpr int kDzExponent = 24;
+constexpr float kDzScale = 1 << kDzExponent;          // on dz while it is in bf16 planes: small probabilities keep their digits (split.hpp)
 
 typedef TileConfig<256, 256, 2, 4, true> BigTile;
 typedef TileConfig<128, 128, 2, 2, false> MidTile;
@@ -68,12 +70,33 @@ __host__ __device__ inline Cut cut_of(const CutArgs &a, int count, float *cost_o
     return best;
 }
 
+// ---- fp16 operands of bf16 gradients --------------------------------------------------------------------------------------
+// Gradients in bf16 are rounded by up to 2^-8 of themselves, so dz may enter their products with fewer digits than the 24 it has: one fp16 plane
+// rounds it by up to 2^-11 (one of bf16 by 2^-8, which would double the results' variance; two of bf16 take twice the products and bytes:
+// 8192 x 100003 x 2048 17.9 ms).  h and W, bf16, are the other operand: their 8 digits are exact in fp16.
+// fp16 ends at 2^-24 and 2^16, so the operands are scaled by powers of two: h and W so that their largest value has exponent 15, dz so that the
+// largest dloss times p = 1 has 14.  Values of dz (h, W) below 2^-28 (2^-29) of those are rounded by up to 2^-39 (2^-40) of them instead of
+// relatively; p - 1 itself has an error of 2^-25 in fp32.
+// The rows of dh are scaled each for itself (dloss is multiplied with them at the end), so none suffers from another's large dloss.
+struct Largest {                     // bits of |x| as fp32, among the finite values
+    unsigned h, W, dloss;            // of the rows with a label; of all words
+};
+// n: 2^n x has exponent 15
+__device__ __forceinline__ int exponent_for(unsigned largest) { return 142 - (int)(largest >> 23); }
+__device__ __forceinline__ float scaled(float x, int n) { return __builtin_amdgcn_ldexpf(x, n); }
+__device__ __forceinline__ f32x4 scaled(f32x4 x, int n) { return f32x4{scaled(x[0], n), scaled(x[1], n), scaled(x[2], n), scaled(x[3], n)}; }
+__device__ __forceinline__ unsigned half_pair(float a, float b) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
+}
+
 // ---- rows with a label ------------------------------------------------------------------------------------------------
 // rows[p] = n of the p-th row with a label, place[n] = p or -1.  A block writes kRowsBlock labels' entries and counts all labels in
 // front of them by itself.
 struct Rows {
     int count;                       // rows with a label
     Cut cut;
+    Largest most;
 };
 constexpr int kRowsBlock = 2048;
 __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labels, int N, int V, int *__restrict__ rows,
@@ -108,25 +131,85 @@ __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labe
         if (n < N) place[n] = in ? p : -1;
         at += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *out = Rows{at, cut.slots ? cut_of(cut, at) : Cut{0, 0}};
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *out = Rows{at, cut.slots ? cut_of(cut, at) : Cut{0, 0}, Largest{0, 0, 0}};
+}
+
+// Largest values: blocks in front of h_block0 take the words, the others a row per wave of h, and dloss.  Bound by reading them once.
+struct LargestArgs {
+    const bf16_t *h, *W;
+    const float *dloss;
+    const int *labels;
+    int N, V, D, h_block0;
+    Rows *out;
+};
+__global__ __launch_bounds__(256) void k_vocab_largest(const LargestArgs a) {
+    __shared__ unsigned s[2][4];
+    const int lane = lane_id(), w = wave_id();
+    const auto finite = [](unsigned x) { return x < 0x7f80u ? x : 0u; };
+    const auto largest8 = [&](u32x4 u) {
+        unsigned m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = max(m, max(finite(u[j] & 0x7fffu), finite(u[j] >> 16 & 0x7fffu)));
+        return m;
+    };
+    unsigned m = 0, g = 0;
+    const bool words = (int)blockIdx.x < a.h_block0;
+    if (words) {
+        const long long n = (long long)a.V * a.D, step = (long long)a.h_block0 * 256;
+        const u32x4 *W = reinterpret_cast<const u32x4 *>(a.W);
+        constexpr int U = 4;
+        for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n / 8; i += U * step) {
+            u32x4 u[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) u[k] = W[min(i + k * step, n / 8 - 1)];
+#pragma unroll
+            for (int k = 0; k < U; ++k) m = max(m, largest8(u[k]));
+        }
+        if (blockIdx.x == 0 && threadIdx.x < n % 8) m = max(m, finite(a.W[n / 8 * 8 + threadIdx.x].bits & 0x7fffu));
+    } else {
+        for (int n = ((int)blockIdx.x - a.h_block0) * 4 + w; n < a.N; n += ((int)gridDim.x - a.h_block0) * 4) {
+            if ((unsigned)a.labels[n] >= (unsigned)a.V) continue;
+            const bf16_t *h = a.h + (size_t)n * a.D;
+            const unsigned x = __float_as_uint(a.dloss[n]) & 0x7fffffffu;
+            if (x < 0x7f800000u) g = max(g, x);
+            if (a.D % 8 == 0)
+                for (int d = lane * 8; d < a.D; d += 512) m = max(m, largest8(*reinterpret_cast<const u32x4 *>(h + d)));
+            else
+                for (int d = lane; d < a.D; d += 64) m = max(m, finite(h[d].bits & 0x7fffu));
+        }
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, off));
+    if (lane == 0) s[0][w] = m, s[1][w] = g;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    m = max(max(s[0][0], s[0][1]), max(s[0][2], s[0][3])) << 16;
+    g = max(max(s[1][0], s[1][1]), max(s[1][2], s[1][3]));
+    // a maximum of integers does not depend on the order
+    if (words) {
+        atomicMax(&a.out->most.W, m);
+    } else {
+        atomicMax(&a.out->most.h, m);
+        atomicMax(&a.out->most.dloss, g);
+    }
 }
 
 // ---- bf16 planes ------------------------------------------------------------------------------------------------------
 // Rows of src as bf16 planes, once with their columns in a row (dst, `pitch` elements a row, zeros behind D) and once turned (turned: a
 // row per column, `turned_pitch` elements, zeros behind the last row up to a multiple of 8), either of them optional.  Row r is row list[r] of
-// src (r < *count) or row first + r (r < n_rows).  A block takes 64 rows and 64 columns.
+// src (r < *count) or row first + r (r < n_rows).  A block takes 64 rows and 64 columns.  HALF: the turned form is fp16, scaled.
 struct PackArgs {
     const void *src;
     int D, first, n_rows, pitch, turned_pitch;
-    const int *list;
-    const Rows *count;
+    const int *list;                 // or null: consecutive rows
+    const Rows *rows;
     bf16_t *dst, *turned;
     size_t plane, turned_plane;
 };
-template <typename T> __global__ __launch_bounds__(256) void k_vocab_pack(const PackArgs a) {
+template <typename T, bool HALF> __global__ __launch_bounds__(256) void k_vocab_pack(const PackArgs a) {
     constexpr int PLANES = sizeof(T) == 4 ? 3 : 1, LP = 72;                    // LDS pitch: 144 bytes, 16-byte aligned, spread over the banks
     __shared__ __align__(16) unsigned short s[64 * LP];
-    const int rows = a.count ? a.count->count : a.n_rows, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
+    const int rows = a.list ? a.rows->count : a.n_rows, r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
     if (r0 >= rows) return;
     const int tr = threadIdx.x >> 2, tc = (threadIdx.x & 3) * 16, r = r0 + tr, c = c0 + tc;
     const bool row = r < rows;
@@ -163,6 +246,12 @@ template <typename T> __global__ __launch_bounds__(256) void k_vocab_pack(const 
             if (c + 8 < a.pitch) *reinterpret_cast<u32x4 *>(to + 8) = u32x4{u[4], u[5], u[6], u[7]};
         }
         if (a.turned) {
+            if constexpr (HALF) {
+                static_assert(PLANES == 1, "bf16 values are exact in fp16");
+                const int e = exponent_for(a.list ? a.rows->most.h : a.rows->most.W);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = half_pair(scaled(__uint_as_float(u[j] << 16), e), scaled(__uint_as_float(u[j] & 0xffff0000u), e));
+            }
             if (k > 0) __syncthreads();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -212,15 +301,16 @@ struct LogitsArgs {
     const float *lse, *dloss;
     bf16_t *dz, *turned;             // [N][dz_pitch]; [words][turned_pitch]
     size_t dz_plane, turned_plane;
-    int dz_pitch, turned_pitch, dz_planes;
+    int dz_pitch, turned_pitch;
 };
+enum class Logits { kForward, kPlanes, kHalf };       // kPlanes, kHalf: backward, dz as three bf16 planes or as fp16
 
 // a sum of exponentials relative to `from`, relative to `to` >= from (both may be minus infinity: an empty sum)
 __device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
     return from == to ? sum : sum * fast_exp2((from - to) * kLog2e);
 }
 
-template <class C, bool BWD>
+template <class C, Logits MODE>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int count = a.count->count;
@@ -234,7 +324,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
     const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
-    if constexpr (!BWD) {
+    if constexpr (MODE == Logits::kForward) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
@@ -311,7 +401,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
             const bool row = n < count;
             const int at = row ? a.rows[n] : 0;
             const int y = row ? a.labels[at] - vw : -1;
-            const float lse = row ? a.lse[at] : 0.f, g = row ? a.dloss[at] * kDzScale : 0.f;
+            const float lse = row ? a.lse[at] : 0.f, g = !row ? 0.f : MODE == Logits::kHalf ? 0x1p15f : a.dloss[at] * kDzScale;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -325,44 +415,76 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
         // with the transposing load 16 words x 32 rows leave for its turned form
         constexpr int PITCH = C::BM * 2 + 16;                                  // bytes; 16 more per row spread the rows over the banks
         const int rows = min(C::BN, (count - n0 + 7) / 8 * 8);                 // zeros up to a multiple of 8
-        for (int k = 0; k < a.dz_planes; ++k) {
-            if (k > 0) lds_barrier();
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j) {
-                char *to = lds + ((wn * C::TN + j) * 16 + (lane & 15)) * PITCH + (wm * C::TM * 16 + lr) * 2;
-#pragma unroll
-                for (int i = 0; i < C::TM; ++i) {
-                    f32x4 &x = acc[i][j];
-                    const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-                    x[0] -= __uint_as_float(u.x << 16);
-                    x[1] -= __uint_as_float(u.x & 0xffff0000u);
-                    x[2] -= __uint_as_float(u.y << 16);
-                    x[3] -= __uint_as_float(u.y & 0xffff0000u);
-                    *reinterpret_cast<u32x2 *>(to + i * 32) = u;
-                }
+        const auto place = [&](int j, int i) { return lds + ((wn * C::TN + j) * 16 + (lane & 15)) * PITCH + (wm * C::TM * 16 + lr) * 2 + i * 32; };
+        const auto store_rows = [&](bf16_t *plane) {
+            bf16_t *out = plane + (size_t)n0 * a.dz_pitch + m0;
+            for (int c = threadIdx.x; c < rows * (C::BM / 8); c += C::THREADS) {
+                const int nt = c / (C::BM / 8), g = c % (C::BM / 8);
+                if (m0 + g * 8 < a.dz_pitch)
+                    *reinterpret_cast<u32x4 *>(out + (size_t)nt * a.dz_pitch + g * 8) = *reinterpret_cast<const u32x4 *>(lds + nt * PITCH + g * 16);
             }
-            lds_barrier();
+        };
+        const auto store_turned = [&](bf16_t *plane) {
+            bf16_t *out = plane + (size_t)m0 * a.turned_pitch + n0;
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 *tr_ptr;
+            // block (x, y): words 16 x .., rows 32 y ..; lanes 16 g .. 16 g + 15 address 4 rows x 16 words and get a word's 4 rows each
+            for (int c = w; c < (C::BM / 16) * (C::BN / 32); c += C::WAVES) {
+                const int x = c / (C::BN / 32), y = c % (C::BN / 32), nt = y * 32 + 8 * (lane >> 4), v = 16 * x + (lane & 15);
+                const char *from = lds + (nt + ((lane & 15) >> 2)) * PITCH + (16 * x + 4 * (lane & 3)) * 2;
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)from);
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(from + 4 * PITCH));
+                const u32x2 p = __builtin_bit_cast(u32x2, lo), q = __builtin_bit_cast(u32x2, hi);
+                if (nt < rows && a.v0 + m0 + v < a.V) *reinterpret_cast<u32x4 *>(out + (size_t)v * a.turned_pitch + nt) = u32x4{p.x, p.y, q.x, q.y};
+            }
+        };
+        if constexpr (MODE == Logits::kHalf) {
             if (a.dz) {
-                bf16_t *out = a.dz + k * a.dz_plane + (size_t)n0 * a.dz_pitch + m0;
-                for (int c = threadIdx.x; c < rows * (C::BM / 8); c += C::THREADS) {
-                    const int nt = c / (C::BM / 8), g = c % (C::BM / 8);
-                    if (m0 + g * 8 < a.dz_pitch)
-                        *reinterpret_cast<u32x4 *>(out + (size_t)nt * a.dz_pitch + g * 8) = *reinterpret_cast<const u32x4 *>(lds + nt * PITCH + g * 16);
-                }
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i) {
+                        const f32x4 x = acc[i][j];
+                        *reinterpret_cast<u32x2 *>(place(j, i)) = u32x2{half_pair(x[0], x[1]), half_pair(x[2], x[3])};
+                    }
+                lds_barrier();
+                store_rows(a.dz);
+                if (a.turned) lds_barrier();
             }
             if (a.turned) {
-                bf16_t *out = a.turned + k * a.turned_plane + (size_t)m0 * a.turned_pitch + n0;
-                typedef short s16x4 __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) s16x4 *tr_ptr;
-                // block (x, y): words 16 x .., rows 32 y ..; lanes 16 g .. 16 g + 15 address 4 rows x 16 words and get a word's 4 rows each
-                for (int c = w; c < (C::BM / 16) * (C::BN / 32); c += C::WAVES) {
-                    const int x = c / (C::BN / 32), y = c % (C::BN / 32), nt = y * 32 + 8 * (lane >> 4), v = 16 * x + (lane & 15);
-                    const char *from = lds + (nt + ((lane & 15) >> 2)) * PITCH + (16 * x + 4 * (lane & 3)) * 2;
-                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)from);
-                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(from + 4 * PITCH));
-                    const u32x2 p = __builtin_bit_cast(u32x2, lo), q = __builtin_bit_cast(u32x2, hi);
-                    if (nt < rows && a.v0 + m0 + v < a.V) *reinterpret_cast<u32x4 *>(out + (size_t)v * a.turned_pitch + nt) = u32x4{p.x, p.y, q.x, q.y};
+                const int e = exponent_for(a.count->most.dloss) - 16;
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j) {
+                    const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+                    const float g = n < count ? scaled(a.dloss[a.rows[n]], e) : 0.f;
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i) {
+                        const f32x4 x = acc[i][j];
+                        *reinterpret_cast<u32x2 *>(place(j, i)) = u32x2{half_pair(x[0] * g, x[1] * g), half_pair(x[2] * g, x[3] * g)};
+                    }
                 }
+                lds_barrier();
+                store_turned(a.turned);
+            }
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < 3; ++k) {
+                if (k > 0) lds_barrier();
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i) {
+                        f32x4 &x = acc[i][j];
+                        const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+                        x[0] -= __uint_as_float(u.x << 16);
+                        x[1] -= __uint_as_float(u.x & 0xffff0000u);
+                        x[2] -= __uint_as_float(u.y << 16);
+                        x[3] -= __uint_as_float(u.y & 0xffff0000u);
+                        *reinterpret_cast<u32x2 *>(place(j, i)) = u;
+                    }
+                lds_barrier();
+                if (a.dz) store_rows(a.dz + k * a.dz_plane);
+                if (a.turned) store_turned(a.turned + k * a.turned_plane);
             }
         }
     }
@@ -701,8 +823,13 @@ struct GradsArgs {
     void *dW;                        // this piece's first row
     float *dw_sum, *dh_sum;          // [parts][words][D]; [parts][N][D], in the rows' gathered places
     size_t dw_part, dh_part;
-    bool bf16_out, add;              // add: not the first piece
+    bool add;                        // not the first piece
 };
+// powers of two that the sums carry
+template <bool HALF> __device__ __forceinline__ int dw_exponent(const Rows &r) {
+    return HALF ? exponent_for(r.most.dloss) - 1 + exponent_for(r.most.h) : kDzExponent;
+}
+template <bool HALF> __device__ __forceinline__ int dh_exponent(const Rows &r) { return HALF ? 15 + exponent_for(r.most.W) : kDzExponent; }
 
 // four consecutive columns of a result row, of which `left` exist; quads: all four or none, aligned
 __device__ __forceinline__ void put4(float *to, f32x4 x, int left, bool quads) {
@@ -727,7 +854,7 @@ __device__ __forceinline__ void put4(bf16_t *to, f32x4 x, int left, bool quads) 
 
 // Units of dW (columns of h x words, over rows) and, behind them, of dh (columns of W x rows, over the piece's words): a lane holds
 // four consecutive columns of a result row.
-template <class C>
+template <class C, bool HALF>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int count = a.rows->count, words = a.words, D = a.D, tm = (D + C::BM - 1) / C::BM;
@@ -744,8 +871,9 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
         if (!tile_of_block(blockIdx.x, tm, tw * cut.dw, im, in)) return;
         const int part = in / tw, m0 = im * C::BM, n0 = (in - part * tw) * C::BN;
         const int len = ((count + kStepK - 1) / kStepK + cut.dw - 1) / cut.dw * kStepK, k0 = min(count, part * len);
-        tile_product<C>(acc, a.h_turned, a.dz_turned, m0, n0, k0, min(count, k0 + len), a.pairs, lds);
-        const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4);
+        tile_product<C, HALF>(acc, a.h_turned, a.dz_turned, m0, n0, k0, min(count, k0 + len), a.pairs, lds);
+        const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4), e = dw_exponent<HALF>(*a.rows);
+        typedef std::conditional_t<HALF, bf16_t, float> grad_t;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int v = n0 + (wn * C::TN + j) * 16 + (lane & 15);
@@ -754,8 +882,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
                 if (cut.dw > 1) put4(a.dw_sum + part * a.dw_part + at + 16 * i, acc[i][j], D - d0 - 16 * i, quads);
-                else if (a.bf16_out) put4(static_cast<bf16_t *>(a.dW) + at + 16 * i, acc[i][j] * (1.f / kDzScale), D - d0 - 16 * i, quads);
-                else put4(static_cast<float *>(a.dW) + at + 16 * i, acc[i][j] * (1.f / kDzScale), D - d0 - 16 * i, quads);
+                else put4(static_cast<grad_t *>(a.dW) + at + 16 * i, scaled(acc[i][j], -e), D - d0 - 16 * i, quads);
             }
         }
         return;
@@ -765,7 +892,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     const int len = ((words + kStepK - 1) / kStepK + cut.dh - 1) / cut.dh * kStepK, k0 = min(words, part * len);
     Operand dz = a.dz;
     dz.rows = count;
-    tile_product<C>(acc, a.W_turned, dz, m0, n0, k0, min(words, k0 + len), a.pairs, lds);
+    tile_product<C, HALF>(acc, a.W_turned, dz, m0, n0, k0, min(words, k0 + len), a.pairs, lds);
     float *sums = a.dh_sum + part * a.dh_part;
     const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4);
 #pragma unroll
@@ -798,6 +925,7 @@ __global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict_
     const int parts = rows->cut.dw, v = blockIdx.x * 4 + wave_id();
     if (parts < 2 || v >= words) return;
     const bool quads = D % 4 == 0;
+    const int e = dw_exponent<sizeof(T) == 2>(*rows);
     for (int d = lane_id() * 4; d < D; d += 256) {
         const size_t at = (size_t)v * D + d;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -810,18 +938,20 @@ __global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict_
                     if (d + r < D) x[r] += sums[k * part + at + r];
             }
         }
-        put4(dW + at, x * (1.f / kDzScale), D - d, quads);
+        put4(dW + at, scaled(x, -e), D - d, quads);
     }
 }
 
-// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.
+// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.  bf16: dloss is not in the sums yet.
 template <typename T>
 __global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict__ rows, const float *__restrict__ sums, size_t part,
-                                                         const int *__restrict__ place, int N, int D, T *__restrict__ dh) {
+                                                         const int *__restrict__ place, const float *__restrict__ dloss, int N, int D,
+                                                         T *__restrict__ dh) {
     const int n = blockIdx.x * 4 + wave_id();
     if (n >= N) return;
-    const int p = place[n], parts = rows->cut.dh;
+    const int p = place[n], parts = rows->cut.dh, e = dh_exponent<sizeof(T) == 2>(*rows);
     const bool quads = D % 4 == 0;
+    const float g = p >= 0 && sizeof(T) == 2 ? dloss[n] : 1.f;
     for (int d = lane_id() * 4; d < D; d += 256) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (p >= 0)
@@ -835,7 +965,7 @@ __global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict_
                         if (d + r < D) x[r] += from[r];
                 }
             }
-        put4(dh + (size_t)n * D + d, x * (1.f / kDzScale), D - d, quads);
+        put4(dh + (size_t)n * D + d, scaled(x, -e) * g, D - d, quads);
     }
 }
 
@@ -867,7 +997,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.planes = d.in_dtype == ECHO_F32 ? 3 : 1;
     p.pitch = (int)up(D, 8);
     p.pack_words = d.in_dtype == ECHO_F32 || D % 8 != 0;
-    p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 2;
+    p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 1;
     p.few = !bwd && (d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : few_rows_apply<bf16_t>(d.N, d.D));
     if (p.few) {
         p.tiles = (int)((V + few_words(d.N) - 1) / few_words(d.N));
@@ -950,7 +1080,6 @@ static bool big_logits(size_t words, size_t N) {
 static PlanePairs pairs_of(int a, int b) {             // planes of the operands: nibbles, the small terms first
     if (a == 3 && b == 3) return {6, 0x001021u, 0x010201u};
     if (a == 1 && b == 3) return {3, 0u, 0x012u};
-    if (a == 1 && b == 2) return {2, 0u, 0x01u};
     return {1, 0u, 0u};
 }
 
@@ -971,17 +1100,18 @@ template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
     else if (a.N <= 32) k_vocab_few_shared<T, 2><<<a.tiles, 512, 0, st>>>(a);
     else k_vocab_few_shared<T, 4><<<a.tiles, 512, 0, st>>>(a);
 }
-template <class C, bool BWD> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
+template <class C, Logits MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
-    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, BWD>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
+    constexpr bool BWD = MODE != Logits::kForward;
+    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, MODE>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
                         C::THREADS, a, st);
 }
-template <class C> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
+template <class C, bool HALF> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long tm = (a.D + C::BM - 1) / C::BM, tw = (a.words + C::BN - 1) / C::BN, th = (N + C::BN - 1) / C::BN;
     const long long blocks = (tm * tw * (a.dW ? cut.most_dw : 0) + 7) / 8 * 8 + tm * th * (a.dh_sum ? cut.most_dh : 0);
-    return launch_tiles("vocab_grads", &k_vocab_grads<C>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
+    return launch_tiles("vocab_grads", &k_vocab_grads<C, HALF>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
 }
 
 static echo_status_t check_vocab(const echo_vocab_desc_t *d, float eps) {
@@ -1008,27 +1138,39 @@ struct VocabRun {
     hipStream_t st;
     template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
 
+    bool half() const { return d.out_dtype == ECHO_BF16; }                    // backward: dz and the turned forms in fp16
+
     // the rows with a label; turned: in their turned form too
-    echo_status_t gather(bool turned, const CutArgs &cut) const {
+    echo_status_t gather(bool turned, const CutArgs &cut, const LargestArgs &largest) const {
         LaunchRecord r = launch_begin("vocab_rows", st);
         k_vocab_rows<<<(d.N + kRowsBlock - 1) / kRowsBlock, 256, 0, st>>>(labels, d.N, d.V, at<int>(p.rows), at<int>(p.place), at<Rows>(p.count),
                                                                              cut);
         if (echo_status_t s = launch_end(r)) return s;
-        return pack("vocab_pack_rows", PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<Rows>(p.count), at<bf16_t>(p.hp),
+        if (largest.h || largest.W) {
+            LargestArgs a = largest;
+            a.out = at<Rows>(p.count);
+            const long long per = 4 * 256 * 8;                                 // values of a block at a time
+            a.h_block0 = a.W ? (int)std::min<long long>(((long long)d.V * d.D + per - 1) / per, 1024) : 0;
+            r = launch_begin("vocab_largest", st);
+            k_vocab_largest<<<a.h_block0 + (a.h ? std::min((d.N + 3) / 4, 1024) : 0), 256, 0, st>>>(a);
+            if (echo_status_t s = launch_end(r)) return s;
+        }
+        return pack("vocab_pack_rows", half() && turned, PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<Rows>(p.count), at<bf16_t>(p.hp),
                                                 turned ? at<bf16_t>(p.ht) : nullptr, p.h_plane, p.ht_plane});
     }
-    echo_status_t pack(const char *name, const PackArgs &a) const {
+    echo_status_t pack(const char *name, bool half, const PackArgs &a) const {
         LaunchRecord r = launch_begin(name, st);
         const dim3 grid((a.n_rows + 63) / 64, (a.pitch + 63) / 64);
-        if (d.in_dtype == ECHO_F32) k_vocab_pack<float><<<grid, 256, 0, st>>>(a);
-        else k_vocab_pack<bf16_t><<<grid, 256, 0, st>>>(a);
+        if (d.in_dtype == ECHO_F32) k_vocab_pack<float, false><<<grid, 256, 0, st>>>(a);
+        else if (half) k_vocab_pack<bf16_t, true><<<grid, 256, 0, st>>>(a);
+        else k_vocab_pack<bf16_t, false><<<grid, 256, 0, st>>>(a);
         return launch_end(r);
     }
     // the words of a piece as an operand, and their turned form if it is wanted
     echo_status_t words(int v0, int n, bool turned, Operand &o) const {
         o = p.pack_words ? Operand{at<bf16_t>(p.wp), p.w_plane, p.pitch, n} : Operand{static_cast<const bf16_t *>(W) + (size_t)v0 * d.D, 0, d.D, n};
         if (!p.pack_words && !turned) return ECHO_OK;
-        return pack("vocab_pack_words", PackArgs{W, d.D, v0, n, p.pitch, p.piece, nullptr, nullptr, p.pack_words ? at<bf16_t>(p.wp) : nullptr,
+        return pack("vocab_pack_words", half() && turned, PackArgs{W, d.D, v0, n, p.pitch, p.piece, nullptr, at<Rows>(p.count), p.pack_words ? at<bf16_t>(p.wp) : nullptr,
                                                  turned ? at<bf16_t>(p.wt) : nullptr, p.w_plane, p.wt_plane});
     }
     Operand rows() const { return Operand{at<bf16_t>(p.hp), p.h_plane, p.pitch, d.N}; }
@@ -1069,7 +1211,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
         k_vocab_few_finish<<<N, 256, 0, x.st>>>(a, loss, lse);
         return launch_end(r);
     }
-    if (echo_status_t s = x.gather(false, CutArgs{})) return s;
+    if (echo_status_t s = x.gather(false, CutArgs{}, LargestArgs{})) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = x.p.pitch;
@@ -1091,7 +1233,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
         if (echo_status_t s = x.words(v0, n, false, a.W)) return s;
         a.v0 = v0;
         a.first_tile = tiles;
-        if (echo_status_t s = big ? launch_logits<BigTile, false>(a, N, x.st) : launch_logits<MidTile, false>(a, N, x.st)) return s;
+        if (echo_status_t s = big ? launch_logits<BigTile, Logits::kForward>(a, N, x.st) : launch_logits<MidTile, Logits::kForward>(a, N, x.st)) return s;
         tiles += big ? (n + 255) / 256 : (n + 127) / 128;
     }
     LaunchRecord r = launch_begin("vocab_loss_finish", x.st);
@@ -1111,7 +1253,9 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V, D = desc->D;
     const VocabPlan &p = x.p;
-    if (echo_status_t s = x.gather(dW != nullptr, x.p.cut)) return s;
+    LargestArgs l{};
+    if (x.half()) l = LargestArgs{dW ? static_cast<const bf16_t *>(h) : nullptr, dh ? static_cast<const bf16_t *>(W) : nullptr, dloss, labels, N, V, D};
+    if (echo_status_t s = x.gather(dW != nullptr, x.p.cut, l)) return s;
     LogitsArgs a{};
     a.h = x.rows();
     a.D = p.pitch;
@@ -1129,7 +1273,6 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     a.turned = dW ? x.at<bf16_t>(p.dzt) : nullptr;
     a.turned_plane = p.dzt_plane;
     a.turned_pitch = p.turned_pitch;
-    a.dz_planes = p.dz_planes;
     GradsArgs g{};
     g.dz = Operand{a.dz, p.dz_plane, p.piece, N};
     g.h_turned = Operand{x.at<bf16_t>(p.ht), p.ht_plane, p.turned_pitch, p.pitch};
@@ -1141,30 +1284,34 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     g.dw_part = (size_t)p.piece * D;
     g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
     g.dh_part = (size_t)N * D;
-    g.bf16_out = desc->out_dtype == ECHO_BF16;
-    const size_t out_bytes = g.bf16_out ? 2 : 4;
+    const size_t out_bytes = x.half() ? 2 : 4;
     const bool big = big_logits(std::min(p.piece, V), N);
     for (int v0 = 0; v0 < V; v0 += p.piece) {
         const int n = std::min(p.piece, V - v0);
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
-        if (echo_status_t s = big ? launch_logits<BigTile, true>(a, N, x.st) : launch_logits<MidTile, true>(a, N, x.st)) return s;
+        echo_status_t s;
+        if (x.half()) s = big ? launch_logits<BigTile, Logits::kHalf>(a, N, x.st) : launch_logits<MidTile, Logits::kHalf>(a, N, x.st);
+        else s = big ? launch_logits<BigTile, Logits::kPlanes>(a, N, x.st) : launch_logits<MidTile, Logits::kPlanes>(a, N, x.st);
+        if (s) return s;
         g.words = n;
         g.dz_turned = Operand{a.turned, p.dzt_plane, p.turned_pitch, n};
         g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
         g.add = v0 > 0;
-        if (echo_status_t s = p.big_grads ? launch_grads<BigTile>(g, p.cut, N, x.st) : launch_grads<MidTile>(g, p.cut, N, x.st)) return s;
+        if (x.half()) s = p.big_grads ? launch_grads<BigTile, true>(g, p.cut, N, x.st) : launch_grads<MidTile, true>(g, p.cut, N, x.st);
+        else s = p.big_grads ? launch_grads<BigTile, false>(g, p.cut, N, x.st) : launch_grads<MidTile, false>(g, p.cut, N, x.st);
+        if (s) return s;
         if (dW && p.cut.most_dw > 1) {
             LaunchRecord r = launch_begin("vocab_dw_finish", x.st);
-            if (g.bf16_out) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
+            if (x.half()) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
             else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
             if (echo_status_t s = launch_end(r)) return s;
         }
     }
     if (!dh) return ECHO_OK;
     LaunchRecord r = launch_begin("vocab_dh_finish", x.st);
-    if (g.bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), N, D, static_cast<bf16_t *>(dh));
-    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), N, D, static_cast<float *>(dh));
+    if (x.half()) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
+    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
     return launch_end(r);
 }
 

@@ -6,7 +6,9 @@ Tolerances, for every entry, from the arithmetic.  u = 2^-24.
   exp  the argument's product and difference round once each, the exponential is good to 2 u: (2 + 2 |argument|) u relative.
   lse  the largest ez of the row, the exponentials, sums over at most V terms in groups (a running sum of V / 64 + 80 terms), logarithm
        and two sums of fp32 numbers of the size of lse and of the label's logit.
-  dz   p times (ez + e_lse + exponential), three roundings; bf16 gradients: two bf16 parts hold it to 2^-16.
+  dz   p times (ez + e_lse + exponential), three roundings.  bf16 gradients: fp16 rounds it by 2^-11; it has 2^15 at p = 1 (for dh, dloss left
+       out) or at least 2^14 at the largest dloss (for dW), and fp16's last place is 2^-24: 2^-40 of dloss, 2^-39 of the largest dloss.  The
+       other operand, scaled to at least 2^15, is off by at most 2^-40 of its largest value.
   dh   the errors of dz through |W|, and the sum's own 4 S u of sum |dz| |W|; the rounding of the result.  dW alike.
 """
 import numpy as np
@@ -102,17 +104,20 @@ class Problem:
         p = np.exp(z - lse[rows, None])
         e_dz = g * (p * (ez + e_lse[:, None] + (4 + 2 * np.abs(z - lse[rows, None])) * U) + 3 * U) + 3 * U * np.abs(dz)
         planes = 3
-        if self.out == "bf16":
-            e_dz = e_dz + 2.0 ** -16 * np.abs(dz)
-            planes = 2
+        e_dh, e_dW = 0.0, 0.0
+        if self.out == "bf16" and len(rows):
+            planes = 1
+            e_dz = e_dz + 2.0 ** -11 * np.abs(dz)
+            e_dh = 2.0 ** -40 * (g * np.abs(W).sum(0) + np.abs(dz).sum(1, keepdims=True) * np.abs(W).max())
+            e_dW = 2.0 ** -39 * g.max() * np.abs(h_).sum(0) + 2.0 ** -40 * np.abs(dz).sum(0)[:, None] * np.abs(h_).max()
         pairs = 6 if self.store == "f32" else planes
         half = 2.0 ** -8 if self.out == "bf16" else U
         if "dh" in got:
             bound = np.zeros_like(dh)
-            bound[rows] = e_dz @ np.abs(W) + (4 * pairs * (V // 16 + 4) + 8) * U * (np.abs(dz) @ np.abs(W)) + half * np.abs(dh[rows])
+            bound[rows] = e_dz @ np.abs(W) + (4 * pairs * (V // 16 + 4) + 8) * U * (np.abs(dz) @ np.abs(W)) + half * np.abs(dh[rows]) + e_dh
             assert (np.abs(got["dh"] - dh) <= 1.01 * bound).all(), np.abs(got["dh"] - dh).max()
         if "dW" in got:
-            bound = e_dz.T @ np.abs(h_) + (4 * pairs * (len(rows) // 16 + 4) + 8) * U * (np.abs(dz).T @ np.abs(h_)) + half * np.abs(dW)
+            bound = e_dz.T @ np.abs(h_) + (4 * pairs * (len(rows) // 16 + 4) + 8) * U * (np.abs(dz).T @ np.abs(h_)) + half * np.abs(dW) + e_dW
             assert (np.abs(got["dW"] - dW) <= 1.01 * bound).all(), np.abs(got["dW"] - dW).max()
 
 
@@ -175,6 +180,61 @@ def test_flat_and_steep_logits(scale):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("power", [0, 60, -60])
+def test_bf16_gradients_of_operands_and_dloss_of_any_size(power):
+    """h up, W down by a power of two leave the logits as they are; the dloss of neighbouring rows differ by up to 2^60."""
+    torch, eb, types = _torch()
+    p = Problem(300, 900, 136, "bf16", "bf16", 0.1, seed=12)
+    p.dloss *= torch.exp2(torch.randint(-30, 31, (300,), generator=torch.Generator().manual_seed(13)).float())
+    p.h, p.W = p.h * 2.0 ** power, p.W * 2.0 ** -power
+    p.check(p.run())
+
+
+def test_bf16_gradient_of_a_dloss_far_below_another():
+    """2^-34 of it, in a word to which the other row gives nothing: dz in fp16 has 2^-20 there, in steps of 2^-24."""
+    torch, eb, types = _torch()
+    p = Problem(2, 64, 64, "bf16", "bf16", 0.0, pad=0.0, seed=15)
+    p.W[:] = torch.eye(64)
+    p.h[:] = 0.0
+    p.h[0, 0], p.h[1, 1:] = 120.0, -1.0
+    p.labels[:] = (0, 1)
+    p.dloss[:] = torch.tensor([1.0, 2.0 ** -34])
+    got = p.run()
+    p.check(got)
+    assert got["dW"][1].any()
+
+
+def test_bf16_rows_without_a_label_do_not_reach_the_gradients():
+    torch, eb, types = _torch()
+    p = Problem(150, 300, 72, "bf16", "bf16", 0.1, pad=0.5, seed=3)
+    none = torch.from_numpy((p.labels < 0) | (p.labels >= 300))
+    clean = p.run()
+    for h, g in ((float("nan"), float("inf")), (1e30, 1e30), (float("inf"), float("nan"))):
+        p.h[none], p.dloss[none] = h, g
+        got = p.run()
+        for k in clean:
+            assert np.array_equal(got[k], clean[k]), k
+
+
+def test_bf16_gradients_of_nothing():
+    """dloss of zero everywhere, then words and rows of zeros."""
+    p = Problem(100, 260, 64, "bf16", "bf16", 0.0, seed=14)
+    p.dloss.zero_()
+    got = p.run()
+    assert not got["dh"].any() and not got["dW"].any()
+    p = Problem(100, 260, 64, "bf16", "bf16", 0.0, seed=14)
+    p.h.zero_()
+    p.W.zero_()
+    got = p.run()
+    assert not got["dh"].any() and not got["dW"].any()
+
+
+@pytest.mark.parametrize("scale", [60.0, 1000.0])
+def test_steep_logits_with_bf16_gradients(scale):
+    p = Problem(90, 400, 48, "bf16", "bf16", 0.1, seed=4, scale=scale)
+    p.check(p.run())
+
+
 def test_a_sure_label_keeps_the_digits_of_its_loss():
     """Losses of 1e-5 from logits of 20: the difference of lse and the label's logit would have errors of 1e-6."""
     torch, eb, types = _torch()
@@ -207,10 +267,11 @@ def test_infinities_and_nan_reach_their_row(store):
 
 
 def test_one_gradient_alone():
-    p = Problem(140, 333, 80, "f32", "f32", 0.1, seed=7)
-    both = p.run()
-    assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"])
-    assert np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
+    for t in ("f32", "bf16"):
+        p = Problem(140, 333, 80, t, t, 0.1, seed=7)
+        both = p.run()
+        assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"])
+        assert np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
 
 
 @pytest.mark.parametrize("store,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
