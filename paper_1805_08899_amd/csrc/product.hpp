@@ -27,10 +27,12 @@ struct Operand {
     int pitch;              // elements from row to row
     int rows;               // extent along m (or n)
 };
-// plane pairs, the small terms first: nibble i of a and b
+// plane pairs, the small terms first: nibble i of a and b.  HALF: of two pairs the first one's operand was stored kLowScale times as large (its
+// values, 2^-11 of the other plane's, would meet the end of fp16's exponents): its sums are scaled back before the second pair.
 struct PlanePairs {
     unsigned n, a, b;
 };
+constexpr float kLowScale = 0x1p11f;
 
 constexpr int kStepK = 64;
 constexpr int kStepBytes = kStepK * 2;
@@ -108,7 +110,7 @@ template <class C, bool HALF> struct Pipeline {
     unsigned a_at[2], b_at[2];                                                 // this lane's place in a stage, by half step
     u32x4 fa[C::AHEAD ? 2 : 1][TM], fb[C::AHEAD ? 2 : 1][TN];
     PlanePairs pairs;
-    int w, len, total, issued, k_issued, pair;
+    int w, len, total, issued, k_issued, pair, scale_at;
 
     // fragment f of half step s: A 0, then B, then the rest of A
     __device__ __forceinline__ void read(int buf, const char *a, const char *b, int s, int f) {
@@ -145,7 +147,17 @@ template <class C, bool HALF> struct Pipeline {
 #pragma unroll
         for (int x = g * PER; x < (g + 1) * PER; ++x) acc[x / TN][x % TN] = mfma16<HALF>(fa[buf][x / TN], fb[buf][x % TN], acc[x / TN][x % TN]);
     }
+    __device__ __forceinline__ void scale_low(Acc &acc, int t) {
+        if constexpr (HALF) {
+            if (t != scale_at) return;
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] *= 1.f / kLowScale;
+        }
+    }
     __device__ __forceinline__ void step_ahead(Acc &acc, int t, char *a, char *b, const char *next_a, const char *next_b) {
+        scale_low(acc, t);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             multiply(acc, 0, g);
@@ -190,6 +202,7 @@ template <class C, bool HALF> struct Pipeline {
             }
         } else {
             for (int t = 0; t < total; ++t) {
+                scale_low(acc, t);
                 // step t's operands are there, for all waves; and everybody is done with the stage that is filled next
                 wait_loads<0>();
                 lds_barrier();
@@ -230,6 +243,7 @@ __device__ __forceinline__ void tile_product(f32x4 (&acc)[C::TM][C::TN], const O
     p.len = k_end - k_begin;
     p.total = p.len > 0 ? (p.len + kStepK - 1) / kStepK * (int)pairs.n : 0;
     p.issued = p.k_issued = p.pair = 0;
+    p.scale_at = pairs.n == 2 ? p.total / 2 : -1;
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll

@@ -70,13 +70,15 @@ __host__ __device__ inline Cut cut_of(const CutArgs &a, int count, float *cost_o
     return best;
 }
 
-// ---- fp16 operands of bf16 gradients --------------------------------------------------------------------------------------
-// Gradients in bf16 are rounded by up to 2^-8 of themselves, so dz may enter their products with fewer digits than the 24 it has: one fp16 plane
-// rounds it by up to 2^-11 (one of bf16 by 2^-8, which would double the results' variance; two of bf16 take twice the products and bytes:
-// 8192 x 100003 x 2048 17.9 ms).  h and W, bf16, are the other operand: their 8 digits are exact in fp16.
+// ---- fp16 operands of the gradients of bf16 storage ------------------------------------------------------------------------
+// h and W, bf16, have 8 digits, which are exact in fp16; so dz may be fp16 as well, with 11 digits to a plane where bf16 has 8.
+//   bf16 gradients  are rounded by up to 2^-8 of themselves: one plane of dz, rounded by up to 2^-11 (one of bf16, by 2^-8, would double the
+//                   results' variance; two of bf16 take twice the products and bytes: 8192 x 100003 x 2048 17.9 ms, this 12.1).
+//   f32 gradients   two planes, together rounded by up to 2^-22: a dz has larger errors from its logit (three of bf16: 6400 x 32000 x 1024
+//                   2.15 ms, this 1.59).
 // fp16 ends at 2^-24 and 2^16, so the operands are scaled by powers of two: h and W so that their largest value has exponent 15, dz so that the
-// largest dloss times p = 1 has 14.  Values of dz (h, W) below 2^-28 (2^-29) of those are rounded by up to 2^-39 (2^-40) of them instead of
-// relatively; p - 1 itself has an error of 2^-25 in fp32.
+// largest dloss times p = 1 has 14.  What of dz (h, W) is below 2^-28 (2^-29) of those is rounded by up to 2^-39 (2^-40) of them
+// instead, with two planes 2^-50; p - 1 itself has an error of 2^-25 in fp32.
 // The rows of dh are scaled each for itself (dloss is multiplied with them at the end), so none suffers from another's large dloss.
 struct Largest {                     // bits of |x| as fp32, among the finite values
     unsigned h, W, dloss;            // of the rows with a label; of all words
@@ -303,14 +305,16 @@ struct LogitsArgs {
     size_t dz_plane, turned_plane;
     int dz_pitch, turned_pitch;
 };
-enum class Logits { kForward, kPlanes, kHalf };       // kPlanes, kHalf: backward, dz as three bf16 planes or as fp16
+// Forward, or backward by what dz is: three bf16 planes (f32 storage), two of fp16 (bf16 storage, f32 gradients), one of fp16 (bf16 gradients)
+enum class Mode { kForward, kPlanes, kHalves, kHalf };
+constexpr bool half_of(Mode m) { return m == Mode::kHalves || m == Mode::kHalf; }
 
 // a sum of exponentials relative to `from`, relative to `to` >= from (both may be minus infinity: an empty sum)
 __device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
     return from == to ? sum : sum * fast_exp2((from - to) * kLog2e);
 }
 
-template <class C, Logits MODE>
+template <class C, Mode MODE>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int count = a.count->count;
@@ -324,7 +328,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
     const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
-    if constexpr (MODE == Logits::kForward) {
+    if constexpr (MODE == Mode::kForward) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
@@ -401,7 +405,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
             const bool row = n < count;
             const int at = row ? a.rows[n] : 0;
             const int y = row ? a.labels[at] - vw : -1;
-            const float lse = row ? a.lse[at] : 0.f, g = !row ? 0.f : MODE == Logits::kHalf ? 0x1p15f : a.dloss[at] * kDzScale;
+            const float lse = row ? a.lse[at] : 0.f, g = !row ? 0.f : half_of(MODE) ? 0x1p15f : a.dloss[at] * kDzScale;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -438,33 +442,49 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 if (nt < rows && a.v0 + m0 + v < a.V) *reinterpret_cast<u32x4 *>(out + (size_t)v * a.turned_pitch + nt) = u32x4{p.x, p.y, q.x, q.y};
             }
         };
-        if constexpr (MODE == Logits::kHalf) {
-            if (a.dz) {
+        if constexpr (half_of(MODE)) {
+            // x, and of two planes what fp16 left of it
+            const auto put = [&](char *to, f32x4 x, int k) {
+                u32x2 u = {half_pair(x[0], x[1]), half_pair(x[2], x[3])};
+                if (k > 0) {
+                    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+                    const f16x4 top = __builtin_bit_cast(f16x4, u);
 #pragma unroll
-                for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-                    for (int i = 0; i < C::TM; ++i) {
-                        const f32x4 x = acc[i][j];
-                        *reinterpret_cast<u32x2 *>(place(j, i)) = u32x2{half_pair(x[0], x[1]), half_pair(x[2], x[3])};
-                    }
-                lds_barrier();
-                store_rows(a.dz);
-                if (a.turned) lds_barrier();
-            }
-            if (a.turned) {
-                const int e = exponent_for(a.count->most.dloss) - 16;
-#pragma unroll
-                for (int j = 0; j < C::TN; ++j) {
-                    const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
-                    const float g = n < count ? scaled(a.dloss[a.rows[n]], e) : 0.f;
-#pragma unroll
-                    for (int i = 0; i < C::TM; ++i) {
-                        const f32x4 x = acc[i][j];
-                        *reinterpret_cast<u32x2 *>(place(j, i)) = u32x2{half_pair(x[0] * g, x[1] * g), half_pair(x[2] * g, x[3] * g)};
-                    }
+                    for (int r = 0; r < 4; ++r) x[r] = (x[r] - (float)top[r]) * kLowScale;
+                    u = u32x2{half_pair(x[0], x[1]), half_pair(x[2], x[3])};
                 }
-                lds_barrier();
-                store_turned(a.turned);
+                *reinterpret_cast<u32x2 *>(to) = u;
+            };
+            const int e = exponent_for(a.count->most.dloss) - 16;
+            float g[C::TN];
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) {
+                const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+                g[j] = n < count && a.turned ? scaled(a.dloss[a.rows[n]], e) : 0.f;
+            }
+            bool first = true;
+#pragma unroll
+            for (int k = 0; k < (MODE == Mode::kHalf ? 1 : 2); ++k) {
+                if (a.dz) {
+                    if (!first) lds_barrier();
+                    first = false;
+#pragma unroll
+                    for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                        for (int i = 0; i < C::TM; ++i) put(place(j, i), acc[i][j], k);
+                    lds_barrier();
+                    store_rows(a.dz + k * a.dz_plane);
+                }
+                if (a.turned) {
+                    if (!first) lds_barrier();
+                    first = false;
+#pragma unroll
+                    for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                        for (int i = 0; i < C::TM; ++i) put(place(j, i), acc[i][j] * g[j], k);
+                    lds_barrier();
+                    store_turned(a.turned + k * a.turned_plane);
+                }
             }
         } else {
 #pragma unroll 1
@@ -826,10 +846,10 @@ struct GradsArgs {
     bool add;                        // not the first piece
 };
 // powers of two that the sums carry
-template <bool HALF> __device__ __forceinline__ int dw_exponent(const Rows &r) {
-    return HALF ? exponent_for(r.most.dloss) - 1 + exponent_for(r.most.h) : kDzExponent;
+__device__ __forceinline__ int dw_exponent(const Rows &r, bool half) {
+    return half ? exponent_for(r.most.dloss) - 1 + exponent_for(r.most.h) : kDzExponent;
 }
-template <bool HALF> __device__ __forceinline__ int dh_exponent(const Rows &r) { return HALF ? 15 + exponent_for(r.most.W) : kDzExponent; }
+__device__ __forceinline__ int dh_exponent(const Rows &r, bool half) { return half ? 15 + exponent_for(r.most.W) : kDzExponent; }
 
 // four consecutive columns of a result row, of which `left` exist; quads: all four or none, aligned
 __device__ __forceinline__ void put4(float *to, f32x4 x, int left, bool quads) {
@@ -854,7 +874,7 @@ __device__ __forceinline__ void put4(bf16_t *to, f32x4 x, int left, bool quads) 
 
 // Units of dW (columns of h x words, over rows) and, behind them, of dh (columns of W x rows, over the piece's words): a lane holds
 // four consecutive columns of a result row.
-template <class C, bool HALF>
+template <class C, Mode MODE>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int count = a.rows->count, words = a.words, D = a.D, tm = (D + C::BM - 1) / C::BM;
@@ -871,9 +891,9 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
         if (!tile_of_block(blockIdx.x, tm, tw * cut.dw, im, in)) return;
         const int part = in / tw, m0 = im * C::BM, n0 = (in - part * tw) * C::BN;
         const int len = ((count + kStepK - 1) / kStepK + cut.dw - 1) / cut.dw * kStepK, k0 = min(count, part * len);
-        tile_product<C, HALF>(acc, a.h_turned, a.dz_turned, m0, n0, k0, min(count, k0 + len), a.pairs, lds);
-        const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4), e = dw_exponent<HALF>(*a.rows);
-        typedef std::conditional_t<HALF, bf16_t, float> grad_t;
+        tile_product<C, half_of(MODE)>(acc, a.h_turned, a.dz_turned, m0, n0, k0, min(count, k0 + len), a.pairs, lds);
+        const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4), e = dw_exponent(*a.rows, half_of(MODE));
+        typedef std::conditional_t<MODE == Mode::kHalf, bf16_t, float> grad_t;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int v = n0 + (wn * C::TN + j) * 16 + (lane & 15);
@@ -892,7 +912,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     const int len = ((words + kStepK - 1) / kStepK + cut.dh - 1) / cut.dh * kStepK, k0 = min(words, part * len);
     Operand dz = a.dz;
     dz.rows = count;
-    tile_product<C, HALF>(acc, a.W_turned, dz, m0, n0, k0, min(words, k0 + len), a.pairs, lds);
+    tile_product<C, half_of(MODE)>(acc, a.W_turned, dz, m0, n0, k0, min(words, k0 + len), a.pairs, lds);
     float *sums = a.dh_sum + part * a.dh_part;
     const int d0 = m0 + wm * C::TM * 16 + 4 * (lane >> 4);
 #pragma unroll
@@ -920,12 +940,12 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
 
 // Parts of dW added in order and scaled back, where there are any.
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict__ rows, const float *__restrict__ sums, size_t part, int words,
+__global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict__ rows, bool half, const float *__restrict__ sums, size_t part, int words,
                                                          int D, T *__restrict__ dW) {
     const int parts = rows->cut.dw, v = blockIdx.x * 4 + wave_id();
     if (parts < 2 || v >= words) return;
     const bool quads = D % 4 == 0;
-    const int e = dw_exponent<sizeof(T) == 2>(*rows);
+    const int e = dw_exponent(*rows, half);
     for (int d = lane_id() * 4; d < D; d += 256) {
         const size_t at = (size_t)v * D + d;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -942,16 +962,16 @@ __global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict_
     }
 }
 
-// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.  bf16: dloss is not in the sums yet.
+// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.  half: dloss is not in the sums yet.
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict__ rows, const float *__restrict__ sums, size_t part,
+__global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict__ rows, bool half, const float *__restrict__ sums, size_t part,
                                                          const int *__restrict__ place, const float *__restrict__ dloss, int N, int D,
                                                          T *__restrict__ dh) {
     const int n = blockIdx.x * 4 + wave_id();
     if (n >= N) return;
-    const int p = place[n], parts = rows->cut.dh, e = dh_exponent<sizeof(T) == 2>(*rows);
+    const int p = place[n], parts = rows->cut.dh, e = dh_exponent(*rows, half);
     const bool quads = D % 4 == 0;
-    const float g = p >= 0 && sizeof(T) == 2 ? dloss[n] : 1.f;
+    const float g = p >= 0 && half ? dloss[n] : 1.f;
     for (int d = lane_id() * 4; d < D; d += 256) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (p >= 0)
@@ -997,7 +1017,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.planes = d.in_dtype == ECHO_F32 ? 3 : 1;
     p.pitch = (int)up(D, 8);
     p.pack_words = d.in_dtype == ECHO_F32 || D % 8 != 0;
-    p.dz_planes = d.out_dtype == ECHO_F32 ? 3 : 1;
+    p.dz_planes = d.in_dtype == ECHO_F32 ? 3 : d.out_dtype == ECHO_F32 ? 2 : 1;
     p.few = !bwd && (d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : few_rows_apply<bf16_t>(d.N, d.D));
     if (p.few) {
         p.tiles = (int)((V + few_words(d.N) - 1) / few_words(d.N));
@@ -1079,7 +1099,7 @@ static bool big_logits(size_t words, size_t N) {
 
 static PlanePairs pairs_of(int a, int b) {             // planes of the operands: nibbles, the small terms first
     if (a == 3 && b == 3) return {6, 0x001021u, 0x010201u};
-    if (a == 1 && b == 3) return {3, 0u, 0x012u};
+    if (a == 1 && b == 2) return {2, 0u, 0x01u};
     return {1, 0u, 0u};
 }
 
@@ -1100,18 +1120,18 @@ template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
     else if (a.N <= 32) k_vocab_few_shared<T, 2><<<a.tiles, 512, 0, st>>>(a);
     else k_vocab_few_shared<T, 4><<<a.tiles, 512, 0, st>>>(a);
 }
-template <class C, Logits MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
+template <class C, Mode MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
-    constexpr bool BWD = MODE != Logits::kForward;
+    constexpr bool BWD = MODE != Mode::kForward;
     return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, MODE>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
                         C::THREADS, a, st);
 }
-template <class C, bool HALF> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
+template <class C, Mode MODE> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long tm = (a.D + C::BM - 1) / C::BM, tw = (a.words + C::BN - 1) / C::BN, th = (N + C::BN - 1) / C::BN;
     const long long blocks = (tm * tw * (a.dW ? cut.most_dw : 0) + 7) / 8 * 8 + tm * th * (a.dh_sum ? cut.most_dh : 0);
-    return launch_tiles("vocab_grads", &k_vocab_grads<C, HALF>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
+    return launch_tiles("vocab_grads", &k_vocab_grads<C, MODE>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
 }
 
 static echo_status_t check_vocab(const echo_vocab_desc_t *d, float eps) {
@@ -1138,7 +1158,7 @@ struct VocabRun {
     hipStream_t st;
     template <typename T> T *at(size_t off) const { return reinterpret_cast<T *>(ws + off); }
 
-    bool half() const { return d.out_dtype == ECHO_BF16; }                    // backward: dz and the turned forms in fp16
+    bool half() const { return d.in_dtype == ECHO_BF16; }                     // backward: dz and the turned forms in fp16
 
     // the rows with a label; turned: in their turned form too
     echo_status_t gather(bool turned, const CutArgs &cut, const LargestArgs &largest) const {
@@ -1233,7 +1253,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
         if (echo_status_t s = x.words(v0, n, false, a.W)) return s;
         a.v0 = v0;
         a.first_tile = tiles;
-        if (echo_status_t s = big ? launch_logits<BigTile, Logits::kForward>(a, N, x.st) : launch_logits<MidTile, Logits::kForward>(a, N, x.st)) return s;
+        if (echo_status_t s = big ? launch_logits<BigTile, Mode::kForward>(a, N, x.st) : launch_logits<MidTile, Mode::kForward>(a, N, x.st)) return s;
         tiles += big ? (n + 255) / 256 : (n + 127) / 128;
     }
     LaunchRecord r = launch_begin("vocab_loss_finish", x.st);
@@ -1284,34 +1304,37 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     g.dw_part = (size_t)p.piece * D;
     g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
     g.dh_part = (size_t)N * D;
-    const size_t out_bytes = x.half() ? 2 : 4;
+    const bool bf16_out = desc->out_dtype == ECHO_BF16;
+    const size_t out_bytes = bf16_out ? 2 : 4;
     const bool big = big_logits(std::min(p.piece, V), N);
     for (int v0 = 0; v0 < V; v0 += p.piece) {
         const int n = std::min(p.piece, V - v0);
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
         echo_status_t s;
-        if (x.half()) s = big ? launch_logits<BigTile, Logits::kHalf>(a, N, x.st) : launch_logits<MidTile, Logits::kHalf>(a, N, x.st);
-        else s = big ? launch_logits<BigTile, Logits::kPlanes>(a, N, x.st) : launch_logits<MidTile, Logits::kPlanes>(a, N, x.st);
+        if (!x.half()) s = big ? launch_logits<BigTile, Mode::kPlanes>(a, N, x.st) : launch_logits<MidTile, Mode::kPlanes>(a, N, x.st);
+        else if (bf16_out) s = big ? launch_logits<BigTile, Mode::kHalf>(a, N, x.st) : launch_logits<MidTile, Mode::kHalf>(a, N, x.st);
+        else s = big ? launch_logits<BigTile, Mode::kHalves>(a, N, x.st) : launch_logits<MidTile, Mode::kHalves>(a, N, x.st);
         if (s) return s;
         g.words = n;
         g.dz_turned = Operand{a.turned, p.dzt_plane, p.turned_pitch, n};
         g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
         g.add = v0 > 0;
-        if (x.half()) s = p.big_grads ? launch_grads<BigTile, true>(g, p.cut, N, x.st) : launch_grads<MidTile, true>(g, p.cut, N, x.st);
-        else s = p.big_grads ? launch_grads<BigTile, false>(g, p.cut, N, x.st) : launch_grads<MidTile, false>(g, p.cut, N, x.st);
+        if (!x.half()) s = p.big_grads ? launch_grads<BigTile, Mode::kPlanes>(g, p.cut, N, x.st) : launch_grads<MidTile, Mode::kPlanes>(g, p.cut, N, x.st);
+        else if (bf16_out) s = p.big_grads ? launch_grads<BigTile, Mode::kHalf>(g, p.cut, N, x.st) : launch_grads<MidTile, Mode::kHalf>(g, p.cut, N, x.st);
+        else s = p.big_grads ? launch_grads<BigTile, Mode::kHalves>(g, p.cut, N, x.st) : launch_grads<MidTile, Mode::kHalves>(g, p.cut, N, x.st);
         if (s) return s;
         if (dW && p.cut.most_dw > 1) {
             LaunchRecord r = launch_begin("vocab_dw_finish", x.st);
-            if (x.half()) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
-            else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
+            if (bf16_out) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
+            else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
             if (echo_status_t s = launch_end(r)) return s;
         }
     }
     if (!dh) return ECHO_OK;
     LaunchRecord r = launch_begin("vocab_dh_finish", x.st);
-    if (x.half()) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
-    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
+    if (bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
+    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
     return launch_end(r);
 }
 

@@ -6,9 +6,10 @@ Tolerances, for every entry, from the arithmetic.  u = 2^-24.
   exp  the argument's product and difference round once each, the exponential is good to 2 u: (2 + 2 |argument|) u relative.
   lse  the largest ez of the row, the exponentials, sums over at most V terms in groups (a running sum of V / 64 + 80 terms), logarithm
        and two sums of fp32 numbers of the size of lse and of the label's logit.
-  dz   p times (ez + e_lse + exponential), three roundings.  bf16 gradients: fp16 rounds it by 2^-11; it has 2^15 at p = 1 (for dh, dloss left
-       out) or at least 2^14 at the largest dloss (for dW), and fp16's last place is 2^-24: 2^-40 of dloss, 2^-39 of the largest dloss.  The
-       other operand, scaled to at least 2^15, is off by at most 2^-40 of its largest value.
+  dz   p times (ez + e_lse + exponential), three roundings.  From bf16 storage it is fp16: one plane (bf16 gradients) rounds it by 2^-11, two
+       (f32 gradients) by 2^-22.  It has 2^15 at p = 1 (for dh, dloss left out) or at least 2^14 at the largest dloss (for dW), and
+       fp16's last place is 2^-24: one plane is off by up to 2^-40 of dloss, or 2^-39 of the largest dloss; the second plane holds 2^11 times
+       what is left, to 2^-11 of that.  The other operand, scaled to at least 2^15, is off by at most 2^-40 of its largest value.
   dh   the errors of dz through |W|, and the sum's own 4 S u of sum |dz| |W|; the rounding of the result.  dW alike.
 """
 import numpy as np
@@ -103,13 +104,13 @@ class Problem:
         g = np.abs(self.dloss.double().numpy()[rows, None])
         p = np.exp(z - lse[rows, None])
         e_dz = g * (p * (ez + e_lse[:, None] + (4 + 2 * np.abs(z - lse[rows, None])) * U) + 3 * U) + 3 * U * np.abs(dz)
-        planes = 3
-        e_dh, e_dW = 0.0, 0.0
-        if self.out == "bf16" and len(rows):
-            planes = 1
-            e_dz = e_dz + 2.0 ** -11 * np.abs(dz)
-            e_dh = 2.0 ** -40 * (g * np.abs(W).sum(0) + np.abs(dz).sum(1, keepdims=True) * np.abs(W).max())
-            e_dW = 2.0 ** -39 * g.max() * np.abs(h_).sum(0) + 2.0 ** -40 * np.abs(dz).sum(0)[:, None] * np.abs(h_).max()
+        planes, e_dh, e_dW = 3, 0.0, 0.0
+        if self.store == "bf16" and len(rows):
+            planes = 1 if self.out == "bf16" else 2
+            e_dz = e_dz + 2.0 ** (-11 * planes) * np.abs(dz)
+            low = 2.0 ** (11 - 11 * planes)
+            e_dh = 2.0 ** -40 * (low * g * np.abs(W).sum(0) + np.abs(dz).sum(1, keepdims=True) * np.abs(W).max())
+            e_dW = 2.0 ** -39 * low * g.max() * np.abs(h_).sum(0) + 2.0 ** -40 * np.abs(dz).sum(0)[:, None] * np.abs(h_).max()
         pairs = 6 if self.store == "f32" else planes
         half = 2.0 ** -8 if self.out == "bf16" else U
         if "dh" in got:
@@ -180,20 +181,22 @@ def test_flat_and_steep_logits(scale):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("power", [0, 60, -60])
-def test_bf16_gradients_of_operands_and_dloss_of_any_size(power):
+def test_bf16_operands_and_dloss_of_any_size(power, out):
     """h up, W down by a power of two leave the logits as they are; the dloss of neighbouring rows differ by up to 2^60."""
     torch, eb, types = _torch()
-    p = Problem(300, 900, 136, "bf16", "bf16", 0.1, seed=12)
+    p = Problem(300, 900, 136, "bf16", out, 0.1, seed=12)
     p.dloss *= torch.exp2(torch.randint(-30, 31, (300,), generator=torch.Generator().manual_seed(13)).float())
     p.h, p.W = p.h * 2.0 ** power, p.W * 2.0 ** -power
     p.check(p.run())
 
 
-def test_bf16_gradient_of_a_dloss_far_below_another():
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_bf16_operands_and_a_dloss_far_below_another(out):
     """2^-34 of it, in a word to which the other row gives nothing: dz in fp16 has 2^-20 there, in steps of 2^-24."""
     torch, eb, types = _torch()
-    p = Problem(2, 64, 64, "bf16", "bf16", 0.0, pad=0.0, seed=15)
+    p = Problem(2, 64, 64, "bf16", out, 0.0, pad=0.0, seed=15)
     p.W[:] = torch.eye(64)
     p.h[:] = 0.0
     p.h[0, 0], p.h[1, 1:] = 120.0, -1.0
@@ -204,9 +207,10 @@ def test_bf16_gradient_of_a_dloss_far_below_another():
     assert got["dW"][1].any()
 
 
-def test_bf16_rows_without_a_label_do_not_reach_the_gradients():
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_bf16_rows_without_a_label_do_not_reach_the_gradients(out):
     torch, eb, types = _torch()
-    p = Problem(150, 300, 72, "bf16", "bf16", 0.1, pad=0.5, seed=3)
+    p = Problem(150, 300, 72, "bf16", out, 0.1, pad=0.5, seed=3)
     none = torch.from_numpy((p.labels < 0) | (p.labels >= 300))
     clean = p.run()
     for h, g in ((float("nan"), float("inf")), (1e30, 1e30), (float("inf"), float("nan"))):
@@ -229,9 +233,10 @@ def test_bf16_gradients_of_nothing():
     assert not got["dh"].any() and not got["dW"].any()
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("scale", [60.0, 1000.0])
-def test_steep_logits_with_bf16_gradients(scale):
-    p = Problem(90, 400, 48, "bf16", "bf16", 0.1, seed=4, scale=scale)
+def test_steep_logits_of_bf16_operands(scale, out):
+    p = Problem(90, 400, 48, "bf16", out, 0.1, seed=4, scale=scale)
     p.check(p.run())
 
 
@@ -267,8 +272,8 @@ def test_infinities_and_nan_reach_their_row(store):
 
 
 def test_one_gradient_alone():
-    for t in ("f32", "bf16"):
-        p = Problem(140, 333, 80, t, t, 0.1, seed=7)
+    for store, out in (("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")):
+        p = Problem(140, 333, 80, store, out, 0.1, seed=7)
         both = p.run()
         assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"])
         assert np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
