@@ -49,24 +49,29 @@ struct CutArgs {
 constexpr int kMostParts = 8;
 constexpr float kUnitSteps = 8.f;                       // steps that a unit's start and end take
 constexpr float kPartSteps = 1.f / 1.1e6f;              // steps (of 1.7 us) that it takes to write and read one number of a part (8 bytes at 5 TB/s)
-__host__ __device__ inline Cut cut_of(const CutArgs &a, int count, float *cost_out = nullptr) {
+constexpr int kCutChoices = 2 * kMostParts;
+__host__ __device__ inline Cut cut_choice(const CutArgs &a, int count, int i, float &cost) {
     const int tm = (a.D + a.tile - 1) / a.tile, tw = tm * ((a.words + a.tile - 1) / a.tile), th = tm * ((count + a.tile - 1) / a.tile);
     const int kw = count > 0 ? (count + 63) / 64 : 1, kh = (a.words + 63) / 64;
-    Cut best = {a.most_dw ? 1 : 0, a.most_dh ? 1 : 0};
-    float least = 3e38f;
-    for (int i = 0; i < 2 * kMostParts; ++i) {
-        const int q = i / 2 + 1, len = ((i % 2 ? kw : kh) + q - 1) / q;
-        Cut c = {(kw + len - 1) / len, (kh + len - 1) / len};
-        c.dw = c.dw < a.most_dw ? c.dw : a.most_dw;
-        c.dh = c.dh < a.most_dh ? c.dh : a.most_dh;
-        const int lw = c.dw ? (kw + c.dw - 1) / c.dw : 0, lh = c.dh ? (kh + c.dh - 1) / c.dh : 0, longest = lw > lh ? lw : lh;
-        const long long units = (long long)tw * c.dw + (long long)th * c.dh;
-        const float rounds = (float)((units + a.slots - 1) / a.slots);
-        const float cost = rounds * ((float)(longest * a.pairs) + kUnitSteps) * a.round +
-                           ((c.dw > 1 ? (float)c.dw * a.words : 0.f) + (c.dh > 1 ? (float)(c.dh - 1) * count : 0.f)) * a.D * kPartSteps;
+    const int q = i / 2 + 1, len = ((i % 2 ? kw : kh) + q - 1) / q;
+    Cut c = {(kw + len - 1) / len, (kh + len - 1) / len};
+    c.dw = c.dw < a.most_dw ? c.dw : a.most_dw;
+    c.dh = c.dh < a.most_dh ? c.dh : a.most_dh;
+    const int lw = c.dw ? (kw + c.dw - 1) / c.dw : 0, lh = c.dh ? (kh + c.dh - 1) / c.dh : 0, longest = lw > lh ? lw : lh;
+    const long long units = (long long)tw * c.dw + (long long)th * c.dh;
+    const float rounds = (float)((units + a.slots - 1) / a.slots);
+    cost = rounds * ((float)(longest * a.pairs) + kUnitSteps) * a.round +
+           ((c.dw > 1 ? (float)c.dw * a.words : 0.f) + (c.dh > 1 ? (float)(c.dh - 1) * count : 0.f)) * a.D * kPartSteps;
+    return c;
+}
+static Cut cut_of(const CutArgs &a, int count, float &least) {
+    Cut best = {1, 1};
+    least = 3e38f;
+    for (int i = 0; i < kCutChoices; ++i) {
+        float cost;
+        const Cut c = cut_choice(a, count, i, cost);
         if (cost < least) least = cost, best = c;
     }
-    if (cost_out) *cost_out = least;
     return best;
 }
 
@@ -116,24 +121,38 @@ __global__ __launch_bounds__(256) void k_vocab_rows(const int *__restrict__ labe
     __syncthreads();
     int at = s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
     constexpr int U = kRowsBlock / 256;
+    __shared__ int s_in[U * 4];
     int t[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) t[u] = begin + u * 256 + (int)threadIdx.x < N ? labels[begin + u * 256 + threadIdx.x] : -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        const unsigned long long m = __ballot((unsigned)t[u] < (unsigned)V);
+        if (lane == 0) s_in[u * 4 + w] = __builtin_popcountll(m);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
         const bool in = (unsigned)t[u] < (unsigned)V;
-        const unsigned long long m = __ballot(in);
-        __syncthreads();
-        if (lane == 0) s_wave[w] = __builtin_popcountll(m);
-        __syncthreads();
-        int p = at + __builtin_popcountll(m & ((1ull << lane) - 1));
-        for (int k = 0; k < w; ++k) p += s_wave[k];
+        int p = at + __builtin_popcountll(__ballot(in) & ((1ull << lane) - 1));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k < w) p += s_in[u * 4 + k];
+            at += s_in[u * 4 + k];
+        }
         const int n = begin + u * 256 + threadIdx.x;
         if (in) rows[p] = n;
         if (n < N) place[n] = in ? p : -1;
-        at += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *out = Rows{at, cut.slots ? cut_of(cut, at) : Cut{0, 0}, Largest{0, 0, 0}};
+    if (blockIdx.x != gridDim.x - 1 || w != 0) return;
+    // a lane per choice: the least cost, the first of equal ones
+    float cost = 3e38f;
+    Cut c = {0, 0};
+    if (cut.slots && lane < kCutChoices) c = cut_choice(cut, at, lane, cost);
+    float least = cost;
+#pragma unroll
+    for (int off = 32; off; off >>= 1) least = fminf(least, __shfl_xor(least, off));
+    if (lane == __builtin_ctzll(__ballot(cost == least))) *out = Rows{at, c, Largest{0, 0, 0}};
 }
 
 // Largest values: blocks in front of h_block0 take the words, the others a row per wave of h, and dloss.  Bound by reading them once.
@@ -187,12 +206,15 @@ __global__ __launch_bounds__(256) void k_vocab_largest(const LargestArgs a) {
     if (threadIdx.x != 0) return;
     m = max(max(s[0][0], s[0][1]), max(s[0][2], s[0][3])) << 16;
     g = max(max(s[1][0], s[1][1]), max(s[1][2], s[1][3]));
-    // a maximum of integers does not depend on the order
+    // A maximum of integers does not depend on the order.  (Only where it raises it: 2000 blocks' atomics in a row took 30 us.)
+    const auto raise = [](unsigned *to, unsigned x) {
+        if (x > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(to, x);
+    };
     if (words) {
-        atomicMax(&a.out->most.W, m);
+        raise(&a.out->most.W, m);
     } else {
-        atomicMax(&a.out->most.h, m);
-        atomicMax(&a.out->most.dloss, g);
+        raise(&a.out->most.h, m);
+        raise(&a.out->most.dloss, g);
     }
 }
 
@@ -1053,7 +1075,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
             // room for what the numbers of rows with a label from a quarter to all of N ask for
             Cut most = {1, 1};
             for (int k = 4; k <= 16; ++k) {
-                const Cut x = cut_of(c, (int)((N * k + 15) / 16), &times[big]);
+                const Cut x = cut_of(c, (int)((N * k + 15) / 16), times[big]);
                 most.dw = std::max(most.dw, x.dw);
                 most.dh = std::max(most.dh, x.dh);
             }
