@@ -46,14 +46,14 @@ struct CutArgs {
     int pairs;
     float round;                     // what a step of a round takes, against one of 256 blocks of 256 x 256
 };
-constexpr int kMostParts = 8;
+constexpr int kMostParts = 64;
 constexpr float kUnitSteps = 8.f;                       // steps that a unit's start and end take
 constexpr float kPartSteps = 1.f / 1.1e6f;              // steps (of 1.7 us) that it takes to write and read one number of a part (8 bytes at 5 TB/s)
-constexpr int kCutChoices = 2 * kMostParts;
+constexpr int kCutChoices = 28;                         // q = 1 .. 8, 12, 16, 24 .. 64 of either axis
 __host__ __device__ inline Cut cut_choice(const CutArgs &a, int count, int i, float &cost) {
     const int tm = (a.D + a.tile - 1) / a.tile, tw = tm * ((a.words + a.tile - 1) / a.tile), th = tm * ((count + a.tile - 1) / a.tile);
     const int kw = count > 0 ? (count + 63) / 64 : 1, kh = (a.words + 63) / 64;
-    const int q = i / 2 + 1, len = ((i % 2 ? kw : kh) + q - 1) / q;
+    const int j = i / 2, q = j < 8 ? j + 1 : (j % 2 ? 16 : 12) << (j - 8) / 2, len = ((i % 2 ? kw : kh) + q - 1) / q;
     Cut c = {(kw + len - 1) / len, (kh + len - 1) / len};
     c.dw = c.dw < a.most_dw ? c.dw : a.most_dw;
     c.dh = c.dh < a.most_dh ? c.dh : a.most_dh;
@@ -242,13 +242,18 @@ template <typename T, bool HALF> __global__ __launch_bounds__(256) void k_vocab_
 #pragma unroll
     for (int j = 0; j < 16; ++j) x[j] = 0.f;
     if (row) {
-        if (a.D % 4 == 0) {
+        if (c + 16 <= a.D) {                     // loads of 16 bytes may begin at any value (2 bytes each: 1536 columns 10 us, 1534 58)
+            struct __attribute__((packed, aligned(sizeof(T)))) Any { u32x4 u; };
+            constexpr int PER = 16 / sizeof(T);
 #pragma unroll
-            for (int j = 0; j < 16; j += 4)
-                if (c + j < a.D) {
-                    const float4 v = ld4(src, c + j);
-                    x[j] = v.x, x[j + 1] = v.y, x[j + 2] = v.z, x[j + 3] = v.w;
+            for (int j = 0; j < 16; j += PER) {
+                const u32x4 u = reinterpret_cast<const Any *>(src + c + j)->u;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if constexpr (PER == 4) x[j + i] = __uint_as_float(u[i]);
+                    else x[j + i] = __uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
                 }
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -873,23 +878,33 @@ __device__ __forceinline__ int dw_exponent(const Rows &r, bool half) {
 }
 __device__ __forceinline__ int dh_exponent(const Rows &r, bool half) { return half ? 15 + exponent_for(r.most.W) : kDzExponent; }
 
-// four consecutive columns of a result row, of which `left` exist; quads: all four or none, aligned
-__device__ __forceinline__ void put4(float *to, f32x4 x, int left, bool quads) {
-    if (quads) {
-        if (left > 0) __builtin_nontemporal_store(x, reinterpret_cast<f32x4 *>(to));
+// Four consecutive columns of a row, of which `left` exist.  Wide loads and stores may begin at any value.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ f32x4 get4(const float *from, int left) {
+    if (left >= 4) return *reinterpret_cast<const f32x4_any *>(from);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+        if (r < left) x[r] = from[r];
+    return x;
+}
+__device__ __forceinline__ void put4(float *to, f32x4 x, int left) {
+    if (left >= 4) {
+        __builtin_nontemporal_store(x, reinterpret_cast<f32x4_any *>(to));
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 3; ++r)
             if (r < left) to[r] = x[r];
     }
 }
-__device__ __forceinline__ void put4(bf16_t *to, f32x4 x, int left, bool quads) {
+__device__ __forceinline__ void put4(bf16_t *to, f32x4 x, int left) {
     const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-    if (quads) {
-        if (left > 0) __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(to));
+    if (left >= 4) {
+        __builtin_nontemporal_store(u, reinterpret_cast<u32x2_any *>(to));
     } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 3; ++r)
             if (r < left) to[r].bits = (unsigned short)(u[r / 2] >> (16 * (r & 1)));
     }
 }
@@ -905,7 +920,6 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     if (!a.dh_sum) cut.dh = 0;
     const int tw = (words + C::BN - 1) / C::BN, th = (count + C::BN - 1) / C::BN;
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN;
-    const bool quads = D % 4 == 0;
     const int dw_blocks = (tm * tw * cut.dw + 7) / 8 * 8;
     f32x4 acc[C::TM][C::TN];
     int im, in;
@@ -923,8 +937,8 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
             const size_t at = (size_t)v * D + d0;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
-                if (cut.dw > 1) put4(a.dw_sum + part * a.dw_part + at + 16 * i, acc[i][j], D - d0 - 16 * i, quads);
-                else put4(static_cast<grad_t *>(a.dW) + at + 16 * i, scaled(acc[i][j], -e), D - d0 - 16 * i, quads);
+                if (cut.dw > 1) put4(a.dw_sum + part * a.dw_part + at + 16 * i, acc[i][j], D - d0 - 16 * i);
+                else put4(static_cast<grad_t *>(a.dW) + at + 16 * i, scaled(acc[i][j], -e), D - d0 - 16 * i);
             }
         }
         return;
@@ -943,19 +957,19 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
         if (n >= count) continue;
         float *to = sums + (size_t)n * D + d0;
         const int left = D - d0;
-        if (quads) {
-            f32x4 old[C::TM];
+        f32x4 old[C::TM];
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i) old[i] = a.add && 16 * i < left ? *reinterpret_cast<const f32x4 *>(to + 16 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < C::TM; ++i) old[i] = a.add ? get4(to + 16 * i, left - 16 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i)
-                if (16 * i < left) *reinterpret_cast<f32x4 *>(to + 16 * i) = old[i] + acc[i][j];
-        } else {
+        for (int i = 0; i < C::TM; ++i) {
+            const f32x4 x = old[i] + acc[i][j];
+            if (left - 16 * i >= 4) {
+                *reinterpret_cast<f32x4_any *>(to + 16 * i) = x;               // read again soon
+            } else {
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (16 * i + r < left) to[16 * i + r] = (a.add ? to[16 * i + r] : 0.f) + acc[i][j][r];
+                for (int r = 0; r < 3; ++r)
+                    if (r < left - 16 * i) to[16 * i + r] = x[r];
+            }
         }
     }
 }
@@ -966,49 +980,32 @@ __global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict_
                                                          int D, T *__restrict__ dW) {
     const int parts = rows->cut.dw, v = blockIdx.x * 4 + wave_id();
     if (parts < 2 || v >= words) return;
-    const bool quads = D % 4 == 0;
     const int e = dw_exponent(*rows, half);
     for (int d = lane_id() * 4; d < D; d += 256) {
         const size_t at = (size_t)v * D + d;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < parts; ++k) {
-            if (quads) {
-                x += *reinterpret_cast<const f32x4 *>(sums + k * part + at);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (d + r < D) x[r] += sums[k * part + at + r];
-            }
-        }
-        put4(dW + at, scaled(x, -e), D - d, quads);
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) x += get4(sums + k * part + at, D - d);
+        put4(dW + at, scaled(x, -e), D - d);
     }
 }
 
-// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per row.  half: dloss is not in the sums yet.
+// dh[n] = sum of the parts of row place[n], scaled back; zeros for rows without a label.  A wave per 256 columns of a row.  half: dloss is not in the sums yet.
 template <typename T>
 __global__ __launch_bounds__(256) void k_vocab_dh_finish(const Rows *__restrict__ rows, bool half, const float *__restrict__ sums, size_t part,
                                                          const int *__restrict__ place, const float *__restrict__ dloss, int N, int D,
                                                          T *__restrict__ dh) {
-    const int n = blockIdx.x * 4 + wave_id();
-    if (n >= N) return;
+    const int n = blockIdx.x * 4 + wave_id(), d = blockIdx.y * 256 + lane_id() * 4;
+    if (n >= N || d >= D) return;
     const int p = place[n], parts = rows->cut.dh, e = dh_exponent(*rows, half);
-    const bool quads = D % 4 == 0;
     const float g = p >= 0 && half ? dloss[n] : 1.f;
-    for (int d = lane_id() * 4; d < D; d += 256) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (p >= 0)
-            for (int k = 0; k < parts; ++k) {
-                const float *from = sums + k * part + (size_t)p * D + d;
-                if (quads) {
-                    x += *reinterpret_cast<const f32x4 *>(from);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (d + r < D) x[r] += from[r];
-                }
-            }
-        put4(dh + (size_t)n * D + d, scaled(x, -e) * g, D - d, quads);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (p >= 0) {
+        const float *from = sums + (size_t)p * D + d;
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) x += get4(from + k * part, D - d);
     }
+    put4(dh + (size_t)n * D + d, scaled(x, -e) * g, D - d);
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------
@@ -1072,9 +1069,9 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
             c = CutArgs{(int)std::min(piece, V), (int)D, 1, 1, big ? 256 : 128, big ? 256 : 512, p.planes == 3 ? 6 : p.dz_planes, big ? 1.f : kMidRound};
             c.most_dw = (int)std::min<size_t>(kMostParts, std::max<size_t>(1, kPartBytes / (piece * D * 4)));
             c.most_dh = (int)std::min<size_t>(kMostParts, std::max<size_t>(1, kPartBytes / (N * D * 4)));
-            // room for what the numbers of rows with a label from a quarter to all of N ask for
+            // room for what some numbers of rows with a label from a quarter to all of N ask for
             Cut most = {1, 1};
-            for (int k = 4; k <= 16; ++k) {
+            for (int k = 4; k <= 16; k += 3) {
                 const Cut x = cut_of(c, (int)((N * k + 15) / 16), times[big]);
                 most.dw = std::max(most.dw, x.dw);
                 most.dh = std::max(most.dh, x.dh);
@@ -1355,8 +1352,8 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     }
     if (!dh) return ECHO_OK;
     LaunchRecord r = launch_begin("vocab_dh_finish", x.st);
-    if (bf16_out) k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
-    else k_vocab_dh_finish<<<(N + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
+    if (bf16_out) k_vocab_dh_finish<<<dim3((N + 3) / 4, (D + 255) / 256), 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
+    else k_vocab_dh_finish<<<dim3((N + 3) / 4, (D + 255) / 256), 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
     return launch_end(r);
 }
 
