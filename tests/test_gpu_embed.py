@@ -42,6 +42,8 @@ def _tokens(kind, N, V, seed):
         t[r.random(N) < 0.05] = V
         t[r.random(N) < 0.02] = -2 ** 31
         t[r.random(N) < 0.02] = 2 ** 31 - 1
+    elif kind == "one class":                           # of the sort's blocks, to which words are dealt in turn
+        t = r.integers(0, max(1, V // 1024), N) * 1024
     elif kind == "sorted":
         t = np.sort(r.integers(0, V, N))
     else:
@@ -68,6 +70,8 @@ CASES = [
     (40000, 2, 8, "bf16", "f32", "uniform"),
     (16, 10, 2100, "f32", "f32", "uniform"),            # rows wider than a wave's four loads
     (70, 10, 4099, "bf16", "bf16", "zipf"),
+    (9000, 50000, 20, "f32", "f32", "one class"),
+    (3000, 3000000, 16, "bf16", "bf16", "one class"),
 ]
 IDS = ["N%d_V%d_D%d_%s_%s_%s" % (c[:5] + (c[5].replace(" ", "_"),)) for c in CASES]
 

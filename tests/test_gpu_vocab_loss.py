@@ -154,6 +154,25 @@ def test_against_the_oracle(case):
 
 
 @pytest.mark.parametrize("store", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [2, 15, 16, 17, 32, 33, 48, 63, 64, 65])
+def test_forward_of_few_rows(N, store):
+    """The words go straight to the matrix cores for up to 64 rows: all sixteens of rows, words that fill no block, widths that fill no step."""
+    for V, D in ((1000, 72), (257, 1032), (64, 8), (4099, 4), (1, 40)):
+        p = Problem(N, V, D, store, "f32", 0.1 if V > 300 else 0.0, seed=N + V)
+        print("few rows", N, V, D, flush=True)
+        p.check(p.run(forward_only=True))
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")], ids="_".join)
+@pytest.mark.parametrize("N,V,D,pad", [(9000, 40, 72, 0.1), (20, 30000, 64, 0.0), (5, 20011, 520, 0.0), (3000, 9001, 36, 0.99), (700, 700, 1000, 0.5),
+                                       (3000, 300, 68, 1.0)])
+def test_gradients_cut_along_either_axis(N, V, D, pad, types):
+    """Many rows and few words and the other way round: sums in up to 64 parts; rows of which few or none have a label."""
+    p = Problem(N, V, D, *types, 0.1, pad=pad, seed=N)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("store", ["f32", "bf16"])
 def test_no_row_has_a_label(store):
     p = Problem(40, 300, 64, store, "f32", 0.1, pad=1.1)
     p.labels[:] = -1
