@@ -72,11 +72,13 @@ template <int ROWS, int WAVES> struct Loader {
 
     __device__ __forceinline__ void init(const Operand &o, int row0, int k_begin, int w, int lane) {
         plane_bytes = o.plane * 2;
-        base0 = reinterpret_cast<const char *>(o.p) + ((size_t)row0 * o.pitch + k_begin) * 2;
+        // from the wave's first row, so that a lane's offset stays below 2^31 for every pitch up to 2^24 (32 rows and less per wave)
+        static_assert(N * 8 <= 32, "offsets");
+        base0 = reinterpret_cast<const char *>(o.p) + ((size_t)(row0 + w * N * 8) * o.pitch + k_begin) * 2;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row_of(i, w, lane);
-            off[i] = row0 + row < o.rows ? (unsigned)(row * o.pitch + k_of(i, w, lane)) * 2u : kOutside;
+            off[i] = row0 + row < o.rows ? (unsigned)((row - w * N * 8) * o.pitch + k_of(i, w, lane)) * 2u : kOutside;
         }
     }
     __device__ __forceinline__ void plane(unsigned p) { base = base0 + p * plane_bytes; }

@@ -1013,6 +1013,7 @@ static size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr size_t kPackBytes = (size_t)128 << 20;      // of f32 words' planes at a time
 constexpr size_t kDzBytes = (size_t)512 << 20;        // of dz and its turned form at a time
+constexpr size_t kTurnedBytes = (size_t)512 << 20;    // of words' turned form at a time (with few rows a piece may be all words)
 constexpr size_t kPartBytes = (size_t)256 << 20;      // of the parts of dW, and of dh
 // A round of 512 blocks of 128 x 128 against one of 256 blocks of 256 x 256, twice its work at 1315 instead of 1130 TFLOP/s.
 constexpr float kMidRound = 0.5f * 1315 / 1130;
@@ -1049,7 +1050,10 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     }
     size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
     if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
-    if (bwd) piece = std::min(piece, std::max<size_t>(kDzBytes / (4 * p.dz_planes * N) / 256 * 256, 256));
+    if (bwd) {
+        piece = std::min(piece, std::max<size_t>(kDzBytes / (4 * p.dz_planes * N) / 256 * 256, 256));
+        piece = std::min(piece, std::max<size_t>(kTurnedBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
+    }
     piece = up((V + (V + piece - 1) / piece - 1) / ((V + piece - 1) / piece), 256);   // pieces of about the same width
     p.piece = (int)piece;
     p.h_plane = N * p.pitch;

@@ -362,3 +362,65 @@ def test_replayed_from_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
+
+
+def _zeros_but(torch, rows, width, filled):
+    x = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
+    for at, value in filled.items():
+        x[at] = torch.from_numpy(value.astype(np.float32)).bfloat16()
+    return x
+
+
+@pytest.mark.parametrize("N", [3, 70])
+def test_words_past_32_bits(N):
+    """4.4 GB of words of zeros but two: the others all have a logit of zero."""
+    torch, eb, types = _torch()
+    V, D = 270000, 8192
+    r = np.random.default_rng(31)
+    words = {V - 1: r.standard_normal(D) / 64, 7: r.standard_normal(D) / 64}
+    W = _zeros_but(torch, V, D, words)
+    h = torch.from_numpy(r.standard_normal((N, D)).astype(np.float32)).bfloat16().cuda()
+    labels = torch.tensor([(V - 1, 7, V - 2)[n % 3] for n in range(N)], dtype=torch.int32, device="cuda")
+    desc = eb.make_vocab_desc(N, V, D, "bf16", "bf16")
+    loss, lse, dloss = torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.rand(N, device="cuda") + 0.5
+    dh, dW = torch.empty(N, D, dtype=torch.bfloat16, device="cuda"), torch.full((V, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(max(eb.echo_vocab_loss_fwd_workspace_bytes(desc), eb.echo_vocab_loss_bwd_workspace_bytes(desc)), dtype=torch.uint8, device="cuda")
+    st = torch.cuda.current_stream()
+    eb.check(eb.echo_vocab_loss_fwd(desc, h, W, labels, 0.0, loss, lse, ws, stream=st))
+    eb.check(eb.echo_vocab_loss_bwd(desc, dloss, lse, h, W, labels, 0.0, dh, dW, ws, stream=st))
+    torch.cuda.synchronize()
+    kept = [7, V - 1, V - 2, 0]
+    h_, W_, g, y = (x.double().cpu().numpy() for x in (h, W[kept], dloss, labels))
+    z = h_ @ W_.T
+    ref = np.log(np.exp(z[:, :2]).sum(1) + V - 2)
+    size = np.abs(h_) @ np.abs(W_).T
+    e = (4 * D // 16 + 4) * U * size.max() + 400 * U + (V / 64 + 80) * U      # ez, the exponentials' arguments, the sums
+    assert np.abs(lse.cpu().numpy() - ref).max() <= e
+    zy = np.where(y == V - 1, z[:, 1], np.where(y == 7, z[:, 0], 0.0))
+    assert np.abs(loss.cpu().numpy() - (ref - zy)).max() <= 2 * e
+    dz = g[:, None] * (np.exp(z - ref[:, None]) - (y[:, None] == np.array(kept)))
+    want = dz.T @ h_
+    bound = (2.0 ** -8 + 1e-5) * np.abs(want) + (2.0 ** -11 + 3 * e) * (np.abs(dz).T @ np.abs(h_))
+    assert (np.abs(dW[kept].double().cpu().numpy() - want) <= bound).all()
+    assert bool(torch.isfinite(dW[1000]).all()) and bool(torch.isfinite(dW[V // 2]).all())
+    want = dz[:, :2] @ W_[:2]                                # (the other words are zeros)
+    bound = (2.0 ** -8 + 1e-5) * np.abs(want) + (2.0 ** -11 + 3 * e) * (np.abs(dz[:, :2]) @ np.abs(W_[:2]))
+    assert (np.abs(dh.double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_more_words_than_32_bit_offsets_of_rows_of_dz(out):
+    """A row of dz of 4.5 million words; its 255 neighbours begin past 2^31 bytes."""
+    torch, eb, types = _torch()
+    N, V, D = 3, 4500003, 8
+    p = Problem(N, V, D, "bf16", out, 0.0, pad=0.0, seed=33)
+    p.check(p.run())
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_more_rows_than_32_bit_offsets_of_words_of_dz(out):
+    """The same of 4.5 million rows, most of them without a label: turned, dz has a row of them per word."""
+    torch, eb, types = _torch()
+    N, V, D = 4500003, 300, 8
+    p = Problem(N, 300, D, "bf16", out, 0.0, pad=0.999, seed=34)
+    p.check(p.run())
