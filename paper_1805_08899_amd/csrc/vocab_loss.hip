@@ -538,18 +538,23 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
-// Up to 64 rows (a decoder step scored, one token): bound by reading the words once.  Every wave takes words straight from memory as operands (f32
-// ones are split in registers) and multiplies them with all rows; no rows are gathered, and a block's maxima, sums and label logits go to part
-// [row][tile].  Up to 16 rows each wave works on its own, the rows coming to it from the caches as operands too.  For more rows that would be more
-// bytes than the caches deliver (64 f32 rows as planes: 256 MB, 36 us), so a block of eight waves passes the rows through LDS as planes.
-constexpr int kFewRows = 64, kFewAlone = 16;
-template <typename T> static bool few_rows_apply(int N, int D) { return N <= kFewRows && D % (16 / (int)sizeof(T)) == 0; }
+// A decoder step scored, one token: bound by reading the words once.  Every wave takes words straight from memory as operands (f32 ones are split in
+// registers) and multiplies them with all rows; no rows are gathered, no words packed, and a block's maxima, sums and label logits go to
+// part [row][tile].  Up to 16 rows each wave works on its own, the rows coming to it from the caches as operands too (one of 32000 x 1024 bf16
+// 13.8 us).  For more rows that would be more bytes than the caches deliver (64 f32 rows as planes: 256 MB, 36 us), so a block of eight waves passes
+// 64 rows through LDS as planes (32000 x 512 f32 23.4 us); several such groups read the words together.
+// Against the tiles (us; 32000 x 1024, 8000 x 512), which pack f32 words first:
+//   f32   128 rows 72 / 212, 23 / 57    256  148 / 216, 26 / 58    384  211 / 223, 43 / 60    512  272 / 249, 45 / 60
+//   bf16  128 rows 30 / 38, 14 / 24     192   42 / 36, 16 / 24     256   51 / 36, 14 / 24
+constexpr int kFewGroup = 64, kFewAlone = 16;
+template <typename T> constexpr int kFewRows = sizeof(T) == 4 ? 384 : 128;
+template <typename T> static bool few_rows_apply(int N, int D) { return N <= kFewRows<T> && D % (16 / (int)sizeof(T)) == 0; }
 constexpr int few_words(int rows) { return rows <= kFewAlone ? 64 : 128; }     // per block of four or eight waves of 16 words
 
 struct FewArgs {
     const void *h, *W;
     const int *labels;
-    int N, V, D, tiles;
+    int N, V, D, tiles, groups;      // groups of 64 rows
     float eps;
     float *part_max, *part_sum, *part_z, *z_label;
 };
@@ -597,7 +602,7 @@ template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 
 
 // The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
 template <int NT, int WAVES>
-__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int v0, float *s_max, float *s_sum, float *s_z) {
+__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z) {
     constexpr int ROWS = 16 * NT;
     const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
 #pragma unroll
@@ -639,7 +644,7 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
         sum += scaled_sum(s_sum[k * ROWS + n], s_max[k * ROWS + n], top);
         z += s_z[k * ROWS + n];
     }
-    const size_t at = (size_t)n * a.tiles + blockIdx.x;
+    const size_t at = (size_t)n * a.tiles + tile;
     a.part_max[at] = top;
     a.part_sum[at] = sum;
     a.part_z[at] = z;
@@ -676,19 +681,29 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
             if (t0 + d + AHEAD < steps) fetch(d, t0 + d + AHEAD);
             acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
         }
-    few_join<1, 4>(a, acc, v0, s_max, s_sum, s_z);
+    few_join<1, 4>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z);
 }
 
 // 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
 constexpr int kFewK = 128, kFewPitch = kFewK * 2 + 16;                         // bytes of a row in LDS: 16 rows of a fragment take all banks
 template <typename T, int NT>
-__global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs a) {
+__global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     constexpr int PLANES = FewFragment<T>::PLANES, SUB = kFewK / 32, ROWS = 16 * NT, WAVES = 8;
     constexpr int GROUPS = ROWS * kFewK / 8, ITEMS = (GROUPS + 64 * WAVES - 1) / (64 * WAVES);      // groups of 8 numbers of the rows, per thread
     constexpr int STAGE = PLANES * ROWS * kFewPitch;
     __shared__ __align__(16) char s_h[2 * STAGE];
     __shared__ float s_max[WAVES * ROWS], s_sum[WAVES * ROWS], s_z[WAVES * ROWS];
-    const int lane = lane_id(), v0 = (blockIdx.x * WAVES + wave_id()) * 16, steps = (a.D + kFewK - 1) / kFewK, k_lane = 8 * (lane >> 4);
+    // the groups' blocks of a tile side by side: its words are read from memory once
+    const int tile = blockIdx.x / all.groups, n0 = (blockIdx.x - tile * all.groups) * kFewGroup;
+    FewArgs a = all;
+    a.N = min(ROWS, all.N - n0);
+    a.h = static_cast<const T *>(all.h) + (size_t)n0 * all.D;
+    a.labels += n0;
+    a.z_label += n0;
+    a.part_max += (size_t)n0 * all.tiles;
+    a.part_sum += (size_t)n0 * all.tiles;
+    a.part_z += (size_t)n0 * all.tiles;
+    const int lane = lane_id(), v0 = (tile * WAVES + wave_id()) * 16, steps = (a.D + kFewK - 1) / kFewK, k_lane = 8 * (lane >> 4);
     const int first = min(v0, a.V - 1);
     const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(a.W) + (size_t)first * a.D), 0, 0x7ffffff0, 0x00020000);
     const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.h), 0, 0x7ffffff0, 0x00020000);
@@ -756,7 +771,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs a) {
         step(t, fw[0]);
         if (t + 1 < steps) step(t + 1, fw[1]);
     }
-    few_join<NT, WAVES>(a, acc, v0, s_max, s_sum, s_z);
+    few_join<NT, WAVES>(a, acc, tile, v0, s_max, s_sum, s_z);
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
@@ -1141,7 +1156,7 @@ static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &grante
 template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
     if (a.N <= kFewAlone) k_vocab_few_alone<T, sizeof(T) == 2 ? 8 : 6><<<a.tiles, 256, 0, st>>>(a);
     else if (a.N <= 32) k_vocab_few_shared<T, 2><<<a.tiles, 512, 0, st>>>(a);
-    else k_vocab_few_shared<T, 4><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<T, 4><<<a.tiles * a.groups, 512, 0, st>>>(a);
 }
 template <class C, Mode MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
@@ -1244,7 +1259,7 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
     const int N = desc->N, V = desc->V;
     if (x.p.few) {
-        const FewArgs a{h, W, labels, N, V, desc->D, x.p.tiles, label_smoothing, x.at<float>(x.p.part_max), x.at<float>(x.p.part_sum),
+        const FewArgs a{h, W, labels, N, V, desc->D, x.p.tiles, (N + kFewGroup - 1) / kFewGroup, label_smoothing, x.at<float>(x.p.part_max), x.at<float>(x.p.part_sum),
                         x.at<float>(x.p.part_z), x.at<float>(x.p.z_label)};
         LaunchRecord r = launch_begin("vocab_few", x.st);
         if (desc->in_dtype == ECHO_F32) launch_few<float>(a, x.st);

@@ -154,9 +154,9 @@ def test_against_the_oracle(case):
 
 
 @pytest.mark.parametrize("store", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [2, 15, 16, 17, 32, 33, 48, 63, 64, 65])
+@pytest.mark.parametrize("N", [2, 15, 16, 17, 32, 33, 48, 63, 64, 65, 127, 128, 129, 320, 383, 384, 385])
 def test_forward_of_few_rows(N, store):
-    """The words go straight to the matrix cores for up to 64 rows: all sixteens of rows, words that fill no block, widths that fill no step."""
+    """The words go straight to the matrix cores for up to 128 rows (f32: 384), in groups of 64: all ends of those, words that fill no block, widths that fill no step."""
     for V, D in ((1000, 72), (257, 1032), (64, 8), (4099, 4), (1, 40)):
         p = Problem(N, V, D, store, "f32", 0.1 if V > 300 else 0.0, seed=N + V)
         print("few rows", N, V, D, flush=True)
