@@ -21,8 +21,8 @@
  * the others are gathered first.
  *
  * What persists from the forward to the backward pass is lse (N floats) in the place of N V logits.  Neither pass holds all of the logits at any
- * time: the forward pass keeps one maximum and sum per row and group of 128 words, the backward pass forms dz for one piece of the
- * vocabulary after another.
+ * time: the forward pass keeps one maximum and sum per row and group of 64, 128 or 256 words, the backward pass forms dz for one piece of
+ * the vocabulary after another (512 MB of dz at most, one piece has 256 words or more).
  *
  * Conventions: as in echoattn.h (caller-owned 16-byte aligned DEVICE memory, row-major and contiguous, work
  * enqueued on `stream`, no synchronisation, no allocation, results bit-identical from run to run, calls that share a workspace
@@ -31,10 +31,14 @@
  *   - in_dtype: storage of E, h and W.  out_dtype: storage of embedded rows and of dout; of dh and dW.  Each is rounded once, to
  *     nearest even, from its fp32 sum.  loss, lse, dloss and dE are fp32.  The loss takes out_dtype ECHO_BF16 with in_dtype
  *     ECHO_BF16 only (ECHO_ERR_DTYPE); the embedding takes all four pairs.
- *   - Products run on the bf16 matrix cores with fp32 sums.  An fp32 operand is taken as the sum of three bf16 numbers, which add up to it
- *     exactly, a product of two of them as the six that matter (error as of fp32 products).  dz is fp32: it enters the
- *     products behind fp32 gradients as three bf16 numbers, those behind bf16 gradients as two (16 of its 24 bits: its rounding
- *     then is 2^-9 of that of the results).  In f32 storage, infinities in h or W, and numbers past 2^127, give NaN.
+ *   - Products run on the matrix cores with fp32 sums.  f32 storage: an operand is taken as the sum of three bf16 numbers, which add up to it
+ *     exactly, a product of two of them as the six that matter (error as of fp32 products), and so is dz; infinities in h or W, and
+ *     numbers past 2^127, give NaN.
+ *   - bf16 storage: the gradients' operands are fp16.  h and W are exact in it, scaled by a power of two, down to 2^-32 of their largest
+ *     finite value (of the rows with a label, of all words), and off by up to 2^-40 of that below.  dz is taken as two fp16 numbers behind
+ *     f32 gradients (off by up to 2^-22 of it) and as one behind bf16 gradients (2^-11, an eighth of what the rounding of
+ *     the result is off by).  Both hold down to 2^-28 of the largest finite |dloss| among the rows with a label for dW, of the row's own
+ *     dloss for dh; a smaller dz is off by up to 2^-50 (two numbers) or 2^-39 (one) of that dloss.
  *   - Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (a limit below; label smoothing outside
  *     [0, 1); a scale that is not finite), ECHO_ERR_ALIGN, ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

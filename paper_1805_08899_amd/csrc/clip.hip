@@ -4,7 +4,8 @@
 //
 // Bound by HBM: the tensors are read once for the norm, once more to be scaled and written once (their norm is a sum over all of them,
 // and nothing on the chip holds more than the 256 MB of the last cache).  The second launch therefore walks the tensors from the end:
-// what the first one read last is still in that cache.
+// what the first one read last is still in that cache.  Measured (400M bf16 values in 40 tensors): 137 + 289 us, 5.8 and 5.5 TB/s; 1.5M f32
+// values in 18 tensors 7 + 8 us, of which a launch of nothing is 2 to 3: a trip for the table, one for the values, one for the sums.
 //
 // Squares and sums are fp64: an exploding gradient (1e20) overflows fp32 squares, which would clip everything to zero.  The vector unit does
 // an fp64 multiply-add per 4 clocks and wave, a tenth of what the loads leave it.

@@ -1,16 +1,20 @@
 // Softmax cross entropy over a vocabulary without kept logits, and its gradients (include/echovocab.h has the formulas).
 //
-//   rows, pack   the rows with a label are gathered (whoever has none takes part in nothing) and stored as bf16 planes; f32 words too, piece by piece
+//   rows, pack   the rows with a label are gathered (whoever has none takes part in nothing); f32 rows and words are stored as bf16 planes, words piece
+//                by piece; for the gradients both are turned as well, so that every product's operands have their rows along k
 //   logits       z = W h^T tile by tile on the matrix cores; a tile never leaves its block:
 //                  forward   maximum and sum of exponentials of its 128 or 256 words but the label, for label smoothing their sum, for every row; the
 //                            label's logit
-//                  backward  dz = dloss (exp(z - lse) - target) of one piece of the vocabulary, as bf16 planes
+//                  backward  dz = dloss (exp(z - lse) - target) of one piece of the vocabulary, as it is and turned, in planes
 //   finish       joins a row's tiles: loss and lse
 //   grads        dW of the piece = dz^T h, dh += dz W, both kinds of tiles in one launch
 //   dh finish    puts the sums of dh into the rows' places
 //
 // Bound by the matrix cores: 2 N V D forward, 8 N V D for both directions (the logits are formed twice, as the tanh map of the attention is: to keep
 // them would take 4 N V bytes written and read twice), times the number of plane pairs (product.hpp, split.hpp).
+// Measured (8192 rows x 100003 words x 2048, bf16): logits 2.45 ms (1370 TFLOP/s), logits and dz 3.1 (the stores of dz and of its turned form, 3.3 GB, are
+// not hidden: a compute unit holds one block), dW and dh 5.9 (1140: by the power limit; pieces whose tiles fill whole rounds gained nothing),
+// all else 0.4.  One of 3520 x 32000 x 1024 with f32 gradients: 0.21, 0.43, 0.85, 0.15.
 #include "../../include/echovocab.h"
 
 #include <hip/hip_runtime.h>
@@ -542,7 +546,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 // registers) and multiplies them with all rows; no rows are gathered, no words packed, and a block's maxima, sums and label logits go to
 // part [row][tile].  Up to 16 rows each wave works on its own, the rows coming to it from the caches as operands too (one of 32000 x 1024 bf16
 // 13.8 us).  For more rows that would be more bytes than the caches deliver (64 f32 rows as planes: 256 MB, 36 us), so a block of eight waves passes
-// 64 rows through LDS as planes (32000 x 512 f32 23.4 us); several such groups read the words together.
+// 64 rows through LDS as planes (32000 x 512 f32 22.4 us); several such groups read the words together.
 // Against the tiles (us; 32000 x 1024, 8000 x 512), which pack f32 words first:
 //   f32   128 rows 72 / 212, 23 / 57    256  148 / 216, 26 / 58    384  211 / 223, 43 / 60    512  272 / 249, 45 / 60
 //   bf16  128 rows 30 / 38, 14 / 24     192   42 / 36, 16 / 24     256   51 / 36, 14 / 24
@@ -685,7 +689,9 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
 }
 
 // 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
-constexpr int kFewK = 128, kFewPitch = kFewK * 2 + 16;                         // bytes of a row in LDS: 16 rows of a fragment take all banks
+// A row takes 256 bytes of LDS, its groups of 16 bytes in the order c ^ (row % 16): the 16 rows of a fragment take all banks, whichever of its lanes are
+// served together (16 more bytes a row instead: 41 % of the LDS time went to conflicts).
+constexpr int kFewK = 128, kFewPitch = kFewK * 2;
 template <typename T, int NT>
 __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     constexpr int PLANES = FewFragment<T>::PLANES, SUB = kFewK / 32, ROWS = 16 * NT, WAVES = 8;
@@ -729,7 +735,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
             if (GROUPS % (64 * WAVES) == 0 || g < GROUPS) {
 #pragma unroll
                 for (int k = 0; k < PLANES; ++k)
-                    *reinterpret_cast<u32x4 *>(s_h + (t & 1) * STAGE + (k * ROWS + g / (kFewK / 8)) * kFewPitch + g % (kFewK / 8) * 16) = p[k];
+                    *reinterpret_cast<u32x4 *>(s_h + (t & 1) * STAGE + (k * ROWS + g / (kFewK / 8)) * kFewPitch + (g % (kFewK / 8) ^ g / (kFewK / 8) % 16) * 16) = p[k];
             }
         }
     };
@@ -755,7 +761,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
         loads_stay();
 #pragma unroll
         for (int s = 0; s < SUB; ++s) {
-            const char *from = s_h + (t & 1) * STAGE + (lane & 15) * kFewPitch + (4 * s + (lane >> 4)) * 16;
+            const char *from = s_h + (t & 1) * STAGE + (lane & 15) * kFewPitch + ((4 * s + (lane >> 4)) ^ (lane & 15)) * 16;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 u32x4 ph[PLANES];
