@@ -442,7 +442,8 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int v = i * 16 + r;
-                    const float p = fast_exp2((acc[i][j][r] - lse) * kLog2e) - (v == y ? off + low : low);
+                    // a probability: a logit of a million has an error of one half, and what that makes of it must not leave fp16
+                    const float e = fast_exp2((acc[i][j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (v == y ? off + low : low);
                     acc[i][j][r] = vw + v < a.V ? p * g : 0.f;
                 }
         }

@@ -364,6 +364,40 @@ def test_replayed_from_a_graph_and_on_another_stream():
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
 
 
+@pytest.mark.parametrize("store,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("scale", [1e6, 1e9])
+def test_logits_whose_rounding_is_larger_than_one(store, out, scale):
+    """The forward pass and the backward pass add a logit's products in another order."""
+    p = Problem(64, 3000, 264, store, out, 0.1, pad=0.1, seed=35, scale=scale)
+    got = p.run()
+    g = np.abs(p.dloss.double().numpy())
+    for k in ("loss", "lse", "dh", "dW"):
+        assert np.isfinite(got[k]).all(), k
+    assert (np.abs(got["dh"]) <= 1.02 * g[:, None] * 3001 * np.abs(p.W.double().numpy()).max()).all()
+
+
+def test_two_calls_at_once_with_workspaces_of_their_own():
+    torch, eb, types = _torch()
+    ps = [Problem(1500, 4000, 128, "bf16", out, 0.1, seed=36) for out in ("f32", "bf16")]
+    want = [p.run() for p in ps]
+    streams, all_out = [torch.cuda.Stream() for _ in ps], []
+    for p, out in zip(ps, ("f32", "bf16")):
+        x = p.h.cuda(), p.W.cuda(), torch.from_numpy(p.labels).cuda()
+        o = [torch.empty(1500, device="cuda"), torch.empty(1500, device="cuda"), torch.empty(1500, 128, dtype=types[out], device="cuda"),
+             torch.empty(4000, 128, dtype=types[out], device="cuda")]
+        ws = [torch.empty(f(p.desc), dtype=torch.uint8, device="cuda") for f in (eb.echo_vocab_loss_fwd_workspace_bytes, eb.echo_vocab_loss_bwd_workspace_bytes)]
+        all_out.append((x, p.dloss.cuda(), o, ws))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, st, (x, g, o, ws) in zip(ps, streams, all_out):
+            eb.check(eb.echo_vocab_loss_fwd(p.desc, *x, 0.1, o[0], o[1], ws[0], stream=st))
+            eb.check(eb.echo_vocab_loss_bwd(p.desc, g, o[1], *x, 0.1, o[2], o[3], ws[1], stream=st))
+    torch.cuda.synchronize()
+    for w, (x, g, o, ws) in zip(want, all_out):
+        for k, got in zip(("loss", "lse", "dh", "dW"), o):
+            assert np.array_equal(got.double().cpu().numpy(), w[k]), k
+
+
 def _zeros_but(torch, rows, width, filled):
     x = torch.zeros(rows, width, dtype=torch.bfloat16, device="cuda")
     for at, value in filled.items():
