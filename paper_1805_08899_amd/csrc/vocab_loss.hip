@@ -444,7 +444,9 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                     const int v = i * 16 + r;
                     // a probability: a logit of a million has an error of one half, and what that makes of it must not leave fp16
                     const float e = fast_exp2((acc[i][j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (v == y ? off + low : low);
-                    acc[i][j][r] = vw + v < a.V ? p * g : 0.f;
+                    float x = vw + v < a.V ? p * g : 0.f;
+                    if constexpr (MODE == Mode::kHalves) asm("" : "+v"(x));       // rounded to fp32 for both planes alike: see below
+                    acc[i][j][r] = x;
                 }
         }
         // dz passes through LDS a plane at a time, [row][word]: each lane writes four words of a row; whole rows leave for dz, and read
@@ -513,7 +515,14 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
                     for (int j = 0; j < C::TN; ++j)
 #pragma unroll
-                        for (int i = 0; i < C::TM; ++i) put(place(j, i), acc[i][j] * g[j], k);
+                        for (int i = 0; i < C::TM; ++i) {
+                        f32x4 x = acc[i][j] * g[j];
+                        // Rounded to fp32 here, for both planes: a product that goes straight to fp16, rounded once, may end at the other one of two
+                        // neighbours than the one whose rest the second plane holds.
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) asm("" : "+v"(x[r]));
+                        put(place(j, i), x, k);
+                    }
                     lds_barrier();
                     store_turned(a.turned + k * a.turned_plane);
                 }

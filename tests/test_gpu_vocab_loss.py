@@ -226,6 +226,25 @@ def test_bf16_operands_and_a_dloss_far_below_another(out):
     assert got["dW"][1].any()
 
 
+def test_two_planes_of_a_dz_add_up():
+    """Few rows, so that one product with a plane off by a place of fp16 (2^-11) stands out of a word's sum; many words, since only a dz within
+    fp32's rounding of halfway between two fp16 numbers (one in 2^13) could be taken for either."""
+    for seed in range(12):
+        p = Problem(4, 20000, 16, "bf16", "f32", 0.0, pad=0.0, seed=40 + seed, scale=0.5)
+        p.W *= 0.25
+        h, W = p.h.double().numpy(), p.W.double().numpy()
+        got = p.run(want_dh=False)
+        # from the lse that was found, so that its error, which all words share, is none of this test's
+        z = h @ W.T
+        q = np.exp(z - got["lse"][:, None])
+        dz = p.dloss.double().numpy()[:, None] * (q - (p.labels[:, None] == np.arange(20000)))
+        size = np.abs(dz).T @ np.abs(h)
+        # z: S = 1; exp: its argument is at most 16 here; dz: three roundings and the planes; the sum: two pairs of one step, the scaling
+        e = 12 * U * (np.abs(h) @ np.abs(W).T).max() + 40 * U + 3 * U + 2.0 ** -22 + 20 * U
+        assert np.abs(z).max() < 6 and (np.abs(got["dW"] - dz.T @ h) <= e * size + 3 * U * np.abs(p.dloss.numpy()).max() * (p.labels[:, None] == np.arange(20000)).T @ np.abs(h)
+                + 2.0 ** -50 * np.abs(h).sum(0)).all(), seed
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_bf16_rows_without_a_label_do_not_reach_the_gradients(out):
     torch, eb, types = _torch()
