@@ -560,6 +560,8 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 // Against the tiles (us; 32000 x 1024, 8000 x 512), which pack f32 words first:
 //   f32   128 rows 72 / 212, 23 / 57    256  148 / 216, 26 / 58    384  211 / 223, 43 / 60    512  272 / 249, 45 / 60
 //   bf16  128 rows 30 / 38, 14 / 24     192   42 / 36, 16 / 24     256   51 / 36, 14 / 24
+// The backward pass of f32 takes the same kernel for dz, with the rows as they were gathered; only the turned words are packed then (forward and
+// backward of 38 rows of 19710 x 1256 454 -> 270 us, of 64 of 32000 x 1024 440 -> 292, of 300 of 60000 x 1500 2546 -> 2196).
 constexpr int kFewGroup = 64, kFewAlone = 16;
 template <typename T> constexpr int kFewRows = sizeof(T) == 4 ? 384 : 128;
 template <typename T> static bool few_rows_apply(int N, int D) { return N <= kFewRows<T> && D % (16 / (int)sizeof(T)) == 0; }
@@ -571,6 +573,14 @@ struct FewArgs {
     int N, V, D, tiles, groups;      // groups of 64 rows
     float eps;
     float *part_max, *part_sum, *part_z, *z_label;
+    // backward (f32): V words from v0 of all_words, rows as gathered, dz and its turned form as three planes
+    int v0, all_words;
+    const Rows *count;
+    const int *rows;
+    const float *lse, *dloss;
+    bf16_t *dz, *turned;
+    size_t dz_plane, turned_plane;
+    int dz_pitch, turned_pitch;
 };
 
 // 16 rows x 32 k of a matrix as an operand: as loaded (lane l: row l % 16, k = 8 (l / 16) .. + 7), and as planes
@@ -664,6 +674,41 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
     a.part_z[at] = z;
 }
 
+// dz of the same: few enough to be stored as the lanes hold it.  Rows n0 .. n0 + a.N, and zeros up to a multiple of 8 and for words past the end
+template <int NT> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0) {
+    const int lane = lane_id(), vw = v0 + 4 * (lane >> 4);
+    const float low = a.eps / (float)a.all_words, off = 1.0f - a.eps;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int n = 16 * j + (lane & 15);
+        if (n >= (a.N + 7) / 8 * 8) continue;
+        const bool row = n < a.N;
+        const int at = a.rows[min(n, a.N - 1)], y = a.labels[at] - a.v0 - vw;
+        const float lse = a.lse[at], g = a.dloss[at] * kDzScale;
+        f32x4 x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float e = fast_exp2((acc[j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (r == y ? off + low : low);
+            x[r] = row && vw + r < a.V ? p * g : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const u32x2 u = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+            x[0] -= __uint_as_float(u.x << 16);
+            x[1] -= __uint_as_float(u.x & 0xffff0000u);
+            x[2] -= __uint_as_float(u.y << 16);
+            x[3] -= __uint_as_float(u.y & 0xffff0000u);
+            if (a.dz && row) *reinterpret_cast<u32x2 *>(a.dz + k * a.dz_plane + (size_t)(n0 + n) * a.dz_pitch + vw) = u;
+            if (a.turned) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (vw + r < a.V)
+                        a.turned[k * a.turned_plane + (size_t)(vw + r) * a.turned_pitch + n0 + n].bits = (unsigned short)(u[r / 2] >> (16 * (r & 1)));
+            }
+        }
+    }
+}
+
 // AHEAD: how many times 32 k are on their way.
 template <typename T, int AHEAD>
 __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
@@ -702,7 +747,7 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
 // A row takes 256 bytes of LDS, its groups of 16 bytes in the order c ^ (row % 16): the 16 rows of a fragment take all banks, whichever of its lanes are
 // served together (16 more bytes a row instead: 41 % of the LDS time went to conflicts).
 constexpr int kFewK = 128, kFewPitch = kFewK * 2;
-template <typename T, int NT>
+template <typename T, int NT, bool BWD>
 __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     constexpr int PLANES = FewFragment<T>::PLANES, SUB = kFewK / 32, ROWS = 16 * NT, WAVES = 8;
     constexpr int GROUPS = ROWS * kFewK / 8, ITEMS = (GROUPS + 64 * WAVES - 1) / (64 * WAVES);      // groups of 8 numbers of the rows, per thread
@@ -712,13 +757,19 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     // the groups' blocks of a tile side by side: its words are read from memory once
     const int tile = blockIdx.x / all.groups, n0 = (blockIdx.x - tile * all.groups) * kFewGroup;
     FewArgs a = all;
-    a.N = min(ROWS, all.N - n0);
-    a.h = static_cast<const T *>(all.h) + (size_t)n0 * all.D;
-    a.labels += n0;
-    a.z_label += n0;
-    a.part_max += (size_t)n0 * all.tiles;
-    a.part_sum += (size_t)n0 * all.tiles;
-    a.part_z += (size_t)n0 * all.tiles;
+    if constexpr (BWD) {
+        a.N = min(ROWS, all.count->count - n0);
+        if (a.N <= 0) return;
+        a.rows += n0;
+    } else {
+        a.N = min(ROWS, all.N - n0);
+        a.h = static_cast<const T *>(all.h) + (size_t)n0 * all.D;
+        a.labels += n0;
+        a.z_label += n0;
+        a.part_max += (size_t)n0 * all.tiles;
+        a.part_sum += (size_t)n0 * all.tiles;
+        a.part_z += (size_t)n0 * all.tiles;
+    }
     const int lane = lane_id(), v0 = (tile * WAVES + wave_id()) * 16, steps = (a.D + kFewK - 1) / kFewK, k_lane = 8 * (lane >> 4);
     const int first = min(v0, a.V - 1);
     const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(a.W) + (size_t)first * a.D), 0, 0x7ffffff0, 0x00020000);
@@ -729,12 +780,15 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
 #pragma unroll
         for (int s = 0; s < SUB; ++s) fw[buf][s].load(words, word_off, t * kFewK + 32 * s + k_lane, a.D);
     };
+    unsigned row_off[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int n = min((i * 64 * WAVES + (int)threadIdx.x) / (kFewK / 8), a.N - 1);
+        row_off[i] = (unsigned)((BWD ? a.rows[n] : n) * a.D) * sizeof(T);
+    }
     auto fetch_rows = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int g = i * 64 * WAVES + threadIdx.x, n = min(g / (kFewK / 8), a.N - 1), k = t * kFewK + g % (kFewK / 8) * 8;
-            fh[i].load(rows, (unsigned)(n * a.D) * sizeof(T), k, a.D);
-        }
+        for (int i = 0; i < ITEMS; ++i) fh[i].load(rows, row_off[i], t * kFewK + (i * 64 * WAVES + (int)threadIdx.x) % (kFewK / 8) * 8, a.D);
     };
     auto put_rows = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
@@ -787,7 +841,8 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
         step(t, fw[0]);
         if (t + 1 < steps) step(t + 1, fw[1]);
     }
-    few_join<NT, WAVES>(a, acc, tile, v0, s_max, s_sum, s_z);
+    if constexpr (BWD) few_dz<NT>(a, acc, n0, v0);
+    else few_join<NT, WAVES>(a, acc, tile, v0, s_max, s_sum, s_z);
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
@@ -1052,7 +1107,7 @@ constexpr size_t kMaxTiles = (size_t)1 << 22;         // of 128 x 128 in a launc
 
 struct VocabPlan {
     int planes, pitch, turned_pitch;                  // of h and, if packed, of W; of h and dz turned
-    bool pack_words, few;                             // few: forward of few rows
+    bool pack_words, few;                             // few: of few rows, whose words are not packed (forward; backward of f32, turned ones are)
     int piece;                                        // words per piece, a multiple of 256
     int dz_planes;
     bool big_grads;
@@ -1067,10 +1122,9 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     const size_t N = d.N, V = d.V, D = d.D;
     p.planes = d.in_dtype == ECHO_F32 ? 3 : 1;
     p.pitch = (int)up(D, 8);
-    p.pack_words = d.in_dtype == ECHO_F32 || D % 8 != 0;
     p.dz_planes = d.in_dtype == ECHO_F32 ? 3 : d.out_dtype == ECHO_F32 ? 2 : 1;
-    p.few = !bwd && (d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : few_rows_apply<bf16_t>(d.N, d.D));
-    if (p.few) {
+    p.few = d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : !bwd && few_rows_apply<bf16_t>(d.N, d.D);
+    if (p.few && !bwd) {
         p.tiles = (int)((V + few_words(d.N) - 1) / few_words(d.N));
         const size_t part = up(N * p.tiles * 4, 256);
         p.part_sum = part;
@@ -1079,6 +1133,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
         p.total = 3 * part + up(N * 4, 256);
         return p;
     }
+    p.pack_words = !p.few && (d.in_dtype == ECHO_F32 || D % 8 != 0);
     size_t piece = std::min(up(V, 256), std::max<size_t>(kMaxTiles * 128 * 128 / N / 256 * 256, 256));
     if (p.pack_words) piece = std::min(piece, std::max<size_t>(kPackBytes / (2 * p.planes * p.pitch) / 256 * 256, 256));
     if (bwd) {
@@ -1126,7 +1181,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.count = take(sizeof(Rows));
     p.rows = take(N * 4);
     p.place = take(N * 4);
-    p.hp = take(p.planes * p.h_plane * 2);
+    if (!p.few) p.hp = take(p.planes * p.h_plane * 2);
     if (p.pack_words) p.wp = take(p.planes * p.w_plane * 2);
     if (!bwd) {
         p.part_max = take(p.tiles * p.part_pitch * 4);
@@ -1171,8 +1226,14 @@ static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &grante
 
 template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
     if (a.N <= kFewAlone) k_vocab_few_alone<T, sizeof(T) == 2 ? 8 : 6><<<a.tiles, 256, 0, st>>>(a);
-    else if (a.N <= 32) k_vocab_few_shared<T, 2><<<a.tiles, 512, 0, st>>>(a);
-    else k_vocab_few_shared<T, 4><<<a.tiles * a.groups, 512, 0, st>>>(a);
+    else if (a.N <= 32) k_vocab_few_shared<T, 2, false><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<T, 4, false><<<a.tiles * a.groups, 512, 0, st>>>(a);
+}
+static echo_status_t launch_few_dz(const FewArgs &a, hipStream_t st) {
+    LaunchRecord r = launch_begin("vocab_few_dz", st);
+    if (a.N <= 32) k_vocab_few_shared<float, 2, true><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<float, 4, true><<<a.tiles * a.groups, 512, 0, st>>>(a);
+    return launch_end(r);
 }
 template <class C, Mode MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
@@ -1229,7 +1290,8 @@ struct VocabRun {
             k_vocab_largest<<<a.h_block0 + (a.h ? std::min((d.N + 3) / 4, 1024) : 0), 256, 0, st>>>(a);
             if (echo_status_t s = launch_end(r)) return s;
         }
-        return pack("vocab_pack_rows", half() && turned, PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<Rows>(p.count), at<bf16_t>(p.hp),
+        if (p.few && !turned) return ECHO_OK;
+        return pack("vocab_pack_rows", half() && turned, PackArgs{h, d.D, 0, d.N, p.pitch, p.turned_pitch, at<int>(p.rows), at<Rows>(p.count), p.few ? nullptr : at<bf16_t>(p.hp),
                                                 turned ? at<bf16_t>(p.ht) : nullptr, p.h_plane, p.ht_plane});
     }
     echo_status_t pack(const char *name, bool half, const PackArgs &a) const {
@@ -1242,6 +1304,7 @@ struct VocabRun {
     }
     // the words of a piece as an operand, and their turned form if it is wanted
     echo_status_t words(int v0, int n, bool turned, Operand &o) const {
+        // (few rows: the operand is not used)
         o = p.pack_words ? Operand{at<bf16_t>(p.wp), p.w_plane, p.pitch, n} : Operand{static_cast<const bf16_t *>(W) + (size_t)v0 * d.D, 0, d.D, n};
         if (!p.pack_words && !turned) return ECHO_OK;
         return pack("vocab_pack_words", half() && turned, PackArgs{W, d.D, v0, n, p.pitch, p.piece, nullptr, at<Rows>(p.count), p.pack_words ? at<bf16_t>(p.wp) : nullptr,
@@ -1249,6 +1312,26 @@ struct VocabRun {
     }
     Operand rows() const { return Operand{at<bf16_t>(p.hp), p.h_plane, p.pitch, d.N}; }
 };
+
+// the few-row form of a backward launch over n words from a.v0
+static FewArgs few_dz_args(const VocabRun &x, const LogitsArgs &a, int n) {
+    FewArgs f{};
+    f.h = x.h;
+    f.W = static_cast<const float *>(x.W) + (size_t)a.v0 * x.d.D;
+    f.labels = a.labels;
+    f.N = x.d.N, f.V = n, f.D = x.d.D;
+    f.tiles = (n + few_words(kFewGroup) - 1) / few_words(kFewGroup);
+    f.groups = (x.d.N + kFewGroup - 1) / kFewGroup;
+    f.eps = a.eps;
+    f.v0 = a.v0, f.all_words = a.V;
+    f.count = a.count;
+    f.rows = a.rows;
+    f.lse = a.lse, f.dloss = a.dloss;
+    f.dz = a.dz, f.turned = a.turned;
+    f.dz_plane = a.dz_plane, f.turned_plane = a.turned_plane;
+    f.dz_pitch = a.dz_pitch, f.turned_pitch = a.turned_pitch;
+    return f;
+}
 
 }  // namespace echo
 
@@ -1366,7 +1449,8 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
         echo_status_t s;
-        if (!x.half()) s = big ? launch_logits<BigTile, Mode::kPlanes>(a, N, x.st) : launch_logits<MidTile, Mode::kPlanes>(a, N, x.st);
+        if (p.few) s = launch_few_dz(few_dz_args(x, a, n), x.st);
+        else if (!x.half()) s = big ? launch_logits<BigTile, Mode::kPlanes>(a, N, x.st) : launch_logits<MidTile, Mode::kPlanes>(a, N, x.st);
         else if (bf16_out) s = big ? launch_logits<BigTile, Mode::kHalf>(a, N, x.st) : launch_logits<MidTile, Mode::kHalf>(a, N, x.st);
         else s = big ? launch_logits<BigTile, Mode::kHalves>(a, N, x.st) : launch_logits<MidTile, Mode::kHalves>(a, N, x.st);
         if (s) return s;

@@ -163,6 +163,23 @@ def test_forward_of_few_rows(N, store):
         p.check(p.run(forward_only=True))
 
 
+@pytest.mark.parametrize("N", [2, 15, 17, 32, 33, 63, 64, 65, 129, 383, 384, 385])
+def test_gradients_of_few_rows(N):
+    """f32 rows straight to the matrix cores, as they are gathered: ends of groups and of their eights, one gradient alone."""
+    for V, D, pad in ((1000, 72, 0.0), (257, 1032, 0.4), (64, 8, 0.9), (4099, 4, 0.2), (1, 40, 0.0)):
+        p = Problem(N, V, D, "f32", "f32", 0.1 if V > 300 else 0.0, pad=pad, seed=N + V)
+        print("few rows", N, V, D, flush=True)
+        both = p.run()
+        p.check(both)
+        assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"]) and np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
+
+
+def test_gradients_of_few_rows_in_pieces():
+    """Words turned in pieces of 512 MB: 5460 words of the widest rows."""
+    p = Problem(70, 6000, 16384, "f32", "f32", 0.1, seed=50)
+    p.check(p.run())
+
+
 @pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")], ids="_".join)
 @pytest.mark.parametrize("N,V,D,pad", [(9000, 40, 72, 0.1), (20, 30000, 64, 0.0), (5, 20011, 520, 0.0), (3000, 9001, 36, 0.99), (700, 700, 1000, 0.5),
                                        (3000, 300, 68, 1.0)])
