@@ -557,14 +557,23 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 // part [row][tile].  Up to 16 rows each wave works on its own, the rows coming to it from the caches as operands too (one of 32000 x 1024 bf16
 // 13.8 us).  For more rows that would be more bytes than the caches deliver (64 f32 rows as planes: 256 MB, 36 us), so a block of eight waves passes
 // 64 rows through LDS as planes (32000 x 512 f32 22.4 us); several such groups read the words together.
-// Against the tiles (us; 32000 x 1024, 8000 x 512), which pack f32 words first:
-//   f32   128 rows 72 / 212, 23 / 57    256  148 / 216, 26 / 58    384  211 / 223, 43 / 60    512  272 / 249, 45 / 60
-//   bf16  128 rows 30 / 38, 14 / 24     192   42 / 36, 16 / 24     256   51 / 36, 14 / 24
+// Against the tiles, which pack f32 words first (us; words x D: 68832 x 696, 32000 x 1024, 8000 x 512):
+//   f32   128 rows 141 / 373,  72 / 212, 23 / 57    256   242 / 408, 148 / 216, 26 / 58    512   447 / 507, 272 / 249, 45 / 60
+//   bf16  128 rows  49 / 57,   30 / 38,  14 / 24    256    78 / 70,   51 / 36,  14 / 24    512   132 / 97,   92 / 45,  20 / 25
+// few_pays() has what these (and 96, 192 and 384 rows) come to in rounds of 256 blocks.
 // The backward pass of f32 takes the same kernel for dz, with the rows as they were gathered; only the turned words are packed then (forward and
 // backward of 38 rows of 19710 x 1256 454 -> 270 us, of 64 of 32000 x 1024 440 -> 292, of 300 of 60000 x 1500 2546 -> 2196).
 constexpr int kFewGroup = 64, kFewAlone = 16;
-template <typename T> constexpr int kFewRows = sizeof(T) == 4 ? 384 : 128;
-template <typename T> static bool few_rows_apply(int N, int D) { return N <= kFewRows<T> && D % (16 / (int)sizeof(T)) == 0; }
+template <typename T> static bool few_pays(size_t N, size_t V, size_t D) {
+    // rows of whole 16-byte groups, and offsets of 31 bits among them
+    if (D % (16 / sizeof(T)) != 0 || N * D * sizeof(T) >= 0x7fff0000u) return false;
+    if (N <= kFewGroup) return true;
+    const auto cover = [](size_t x, size_t a) { return (x + a - 1) / a; };
+    const float few = 6.f + (float)cover(cover(V, 128) * cover(N, kFewGroup), 256) * (sizeof(T) == 4 ? 5.f + 0.03f * D : 3.f + 0.007f * D);
+    const float mid = (float)cover(cover(V, 128) * cover(N, 128), 512) * 1.1f, big = (float)cover(cover(V, 256) * cover(N, 256), 256) * 1.7f;
+    const float steps = (float)cover(D, 64) * (sizeof(T) == 4 ? 6.f : 1.f), pack = sizeof(T) == 4 ? (float)V * D * 2e-6f : 0.f;
+    return few < 15.f + pack + steps * std::min(mid, big);
+}
 constexpr int few_words(int rows) { return rows <= kFewAlone ? 64 : 128; }     // per block of four or eight waves of 16 words
 
 struct FewArgs {
@@ -1123,7 +1132,7 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
     p.planes = d.in_dtype == ECHO_F32 ? 3 : 1;
     p.pitch = (int)up(D, 8);
     p.dz_planes = d.in_dtype == ECHO_F32 ? 3 : d.out_dtype == ECHO_F32 ? 2 : 1;
-    p.few = d.in_dtype == ECHO_F32 ? few_rows_apply<float>(d.N, d.D) : !bwd && few_rows_apply<bf16_t>(d.N, d.D);
+    p.few = d.in_dtype == ECHO_F32 ? few_pays<float>(N, V, D) : !bwd && few_pays<bf16_t>(N, V, D);
     if (p.few && !bwd) {
         p.tiles = (int)((V + few_words(d.N) - 1) / few_words(d.N));
         const size_t part = up(N * p.tiles * 4, 256);

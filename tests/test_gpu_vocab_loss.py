@@ -156,7 +156,7 @@ def test_against_the_oracle(case):
 @pytest.mark.parametrize("store", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [2, 15, 16, 17, 32, 33, 48, 63, 64, 65, 127, 128, 129, 320, 383, 384, 385])
 def test_forward_of_few_rows(N, store):
-    """The words go straight to the matrix cores for up to 128 rows (f32: 384), in groups of 64: all ends of those, words that fill no block, widths that fill no step."""
+    """The words go straight to the matrix cores for few rows, in groups of 64: all ends of those, words that fill no block, widths that fill no step."""
     for V, D in ((1000, 72), (257, 1032), (64, 8), (4099, 4), (1, 40)):
         p = Problem(N, V, D, store, "f32", 0.1 if V > 300 else 0.0, seed=N + V)
         print("few rows", N, V, D, flush=True)
@@ -172,6 +172,14 @@ def test_gradients_of_few_rows(N):
         both = p.run()
         p.check(both)
         assert np.array_equal(p.run(want_dW=False)["dh"], both["dh"]) and np.array_equal(p.run(want_dh=False)["dW"], both["dW"])
+
+
+@pytest.mark.parametrize("N,V,D", [(556, 2180, 936), (1500, 500, 256), (8192, 128, 64), (8193, 120, 32), (1100, 1000, 1024)])
+def test_more_rows_of_few_words(N, V, D):
+    """Where many groups of rows still make few blocks."""
+    for store in ("f32", "bf16"):
+        p = Problem(N, V, D, store, "f32", 0.1, seed=N + 1)
+        p.check(p.run())
 
 
 def test_gradients_of_few_rows_in_pieces():
