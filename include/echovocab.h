@@ -37,8 +37,9 @@
  *   - bf16 storage: the gradients' operands are fp16.  h and W are exact in it, scaled by a power of two, down to 2^-32 of their largest
  *     finite value (of the rows with a label, of all words), and off by up to 2^-40 of that below.  dz is taken as two fp16 numbers behind
  *     f32 gradients (off by up to 2^-22 of it) and as one behind bf16 gradients (2^-11, an eighth of what the rounding of
- *     the result is off by).  Both hold down to 2^-28 of the largest finite |dloss| among the rows with a label for dW, of the row's own
- *     dloss for dh; a smaller dz is off by up to 2^-50 (two numbers) or 2^-39 (one) of that dloss.
+ *     the result is off by).  For dh both hold down to 2^-28 of the row's own dloss; a smaller dz is off by up to 2^-50 (two numbers) or 2^-39
+ *     (one) of that dloss.  For dW they hold down to 2^-10 of the largest |dz| of the word, however small that is (to 2^-130 of the largest
+ *     finite |dloss| among the rows with a label); a smaller dz is off by up to 2^-31 (two numbers) or 2^-20 (one) of that largest |dz|.
  *   - Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (a limit below; label smoothing outside
  *     [0, 1); a scale that is not finite), ECHO_ERR_ALIGN, ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

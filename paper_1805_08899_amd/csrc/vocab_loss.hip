@@ -86,9 +86,15 @@ static Cut cut_of(const CutArgs &a, int count, float &least) {
 //   f32 gradients   two planes, together rounded by up to 2^-22: a dz has larger errors from its logit (three of bf16: 6400 x 32000 x 1024
 //                   2.15 ms, this 1.59).
 // fp16 ends at 2^-24 and 2^16, so the operands are scaled by powers of two: h and W so that their largest value has exponent 15, dz so that the
-// largest dloss times p = 1 has 14.  What of dz (h, W) is below 2^-28 (2^-29) of those is rounded by up to 2^-39 (2^-40) of them
-// instead, with two planes 2^-50; p - 1 itself has an error of 2^-25 in fp32.
-// The rows of dh are scaled each for itself (dloss is multiplied with them at the end), so none suffers from another's large dloss.
+// largest dloss times p = 1 has 14.  What of h or W is below 2^-29 of its largest is rounded by up to 2^-40 of that instead.
+// The rows of dh are scaled each for itself (dloss is multiplied with them at the end), so none suffers from another's large dloss.  What of
+// dz is below 2^-29 of its row's dloss is rounded by up to 2^-40 of that, with two planes 2^-51; p - 1 itself has an error of 2^-25 in fp32.
+// The rows of dW are scaled each for itself as well: a word that is unlikely in every row, or that only rows of small dloss know, has nothing but small dz
+// (at p = 1e-12 everywhere one plane scaled like the others left its row of dW with an error of 26 to 87 %, at 1e-14 there was nothing left of it).
+// A tile of dz is formed where nothing is known of a word's other rows, so it scales its share by 2^(16 k), k by the largest |dz| in it (dz_steps()); where
+// tiles of a word took different k, k_vocab_level brings them to the least one, and the sums are scaled back by that.  Steps of 16, so that hardly any
+// word has tiles that differ; the least k leaves a word's largest |dz| at 2^-4 or above, where fp16's places are 2^-20 of it.  All of it costs 0.5 to
+// 2.5 % of a step (6400 x 32000 x 1024 1628 -> 1670 us, 8192 x 100003 x 2048 12.21 -> 12.30 ms, 300 x 8000 x 512 75 -> 76.5 us).
 struct Largest {                     // bits of |x| as fp32, among the finite values
     unsigned h, W, dloss;            // of the rows with a label; of all words
 };
@@ -99,6 +105,24 @@ __device__ __forceinline__ f32x4 scaled(f32x4 x, int n) { return f32x4{scaled(x[
 __device__ __forceinline__ unsigned half_pair(float a, float b) {
     typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(unsigned, f16x2{(_Float16)a, (_Float16)b});
+}
+
+constexpr unsigned kNoDz = 8;         // steps of a tile in which all dz of a word are zero
+__device__ __forceinline__ unsigned dz_steps(unsigned largest) {              // bits of a magnitude: 2^(16 steps) of it is 2^-4 or more
+    return largest == 0u ? kNoDz : largest >= 123u << 23 ? 0u : min(7u, (138u - (largest >> 23)) / 16u);
+}
+// Of N values per lane the largest of 16 lanes: lane l ends with those of values N / 16 (l % 16) .. in a[0 .. N / 16 - 1].  At each step a lane keeps half of
+// its values and hands the other half on (row_ror:8, row_half_mirror, two quad permutations).
+template <int CTRL, int HALF, int N> __device__ __forceinline__ void row16_max_step(float (&a)[N], bool upper) {
+#pragma unroll
+    for (int k = 0; k < HALF; ++k) a[k] = fmaxf(upper ? a[HALF + k] : a[k], dpp_get<CTRL>(upper ? a[k] : a[HALF + k]));
+}
+template <int N> __device__ __forceinline__ void row16_max(float (&a)[N], int lane) {
+    static_assert(N % 16 == 0, "values for every lane");
+    row16_max_step<0x128, N / 2>(a, lane & 8);
+    row16_max_step<0x141, N / 4>(a, lane & 4);
+    row16_max_step<0x4E, N / 8>(a, lane & 2);
+    row16_max_step<0xB1, N / 16>(a, lane & 1);
 }
 
 // ---- rows with a label ------------------------------------------------------------------------------------------------
@@ -335,6 +359,7 @@ struct LogitsArgs {
     bf16_t *dz, *turned;             // [N][dz_pitch]; [words][turned_pitch]
     size_t dz_plane, turned_plane;
     int dz_pitch, turned_pitch;
+    unsigned char *steps;            // [row tiles][dz_pitch]: dz_steps() of the words of `turned`, of fp16
 };
 // Forward, or backward by what dz is: three bf16 planes (f32 storage), two of fp16 (bf16 storage, f32 gradients), one of fp16 (bf16 gradients)
 enum class Mode { kForward, kPlanes, kHalves, kHalf };
@@ -489,41 +514,84 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 }
                 *reinterpret_cast<u32x2 *>(to) = u;
             };
-            const int e = exponent_for(a.count->most.dloss) - 16;
-            float g[C::TN];
+            constexpr int PLANES = MODE == Mode::kHalf ? 1 : 2;
+            const auto put_all = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < C::TN; ++j) {
-                const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
-                g[j] = n < count && a.turned ? scaled(a.dloss[a.rows[n]], e) : 0.f;
-            }
-            bool first = true;
+                for (int j = 0; j < C::TN; ++j)
 #pragma unroll
-            for (int k = 0; k < (MODE == Mode::kHalf ? 1 : 2); ++k) {
-                if (a.dz) {
-                    if (!first) lds_barrier();
-                    first = false;
+                    for (int i = 0; i < C::TM; ++i) put(place(j, i), acc[i][j], k);
+                lds_barrier();
+            };
+            if (a.dz)
 #pragma unroll
-                    for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-                        for (int i = 0; i < C::TM; ++i) put(place(j, i), acc[i][j], k);
-                    lds_barrier();
+                for (int k = 0; k < PLANES; ++k) {
+                    if (k > 0) lds_barrier();
+                    put_all(k);
                     store_rows(a.dz + k * a.dz_plane);
                 }
-                if (a.turned) {
-                    if (!first) lds_barrier();
-                    first = false;
+            if (a.turned) {
+                const int e = exponent_for(a.count->most.dloss) - 16;
 #pragma unroll
-                    for (int j = 0; j < C::TN; ++j)
+                for (int j = 0; j < C::TN; ++j) {
+                    const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+                    const float g = n < count ? scaled(a.dloss[a.rows[n]], e) : 0.f;
+                    // Rounded to fp32 here, for both planes: a product that goes straight to fp16, rounded once, may end at the other one of two
+                    // neighbours than the one whose rest the second plane holds.
 #pragma unroll
-                        for (int i = 0; i < C::TM; ++i) {
-                        f32x4 x = acc[i][j] * g[j];
-                        // Rounded to fp32 here, for both planes: a product that goes straight to fp16, rounded once, may end at the other one of two
-                        // neighbours than the one whose rest the second plane holds.
+                    for (int i = 0; i < C::TM; ++i) {
+                        acc[i][j] *= g;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) asm("" : "+v"(x[r]));
-                        put(place(j, i), x, k);
+                        for (int r = 0; r < 4; ++r) asm("" : "+v"(acc[i][j][r]));
                     }
-                    lds_barrier();
+                }
+                // Each word's largest |dz| in this tile: over the wave's rows (dealt to the lanes: 30 exchanges where a reduction of each word by itself takes
+                // 128), then over the waves that share its words, one of which works out the steps.
+                constexpr int OWN = C::TM * 4 / 16;                            // words of a lane: from number OWN (lane % 16) of the wave's on
+                float *s_top = reinterpret_cast<float *>(lds + C::BN * PITCH) + wm * C::TM * 16, *s_up = s_top + C::WN * C::BM;
+                const int own = (lane & 15) * OWN, at = own / 4 * 16 + lr + own % 4;
+                float top[C::TM * 4];
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        top[i * 4 + r] = 0.f;
+#pragma unroll
+                        for (int j = 0; j < C::TN; ++j) top[i * 4 + r] = fmaxf(top[i * 4 + r], fabsf(acc[i][j][r]));
+                    }
+                row16_max(top, lane);
+#pragma unroll
+                for (int k = 0; k < OWN; ++k) s_top[wn * C::BM + at + k] = top[k];
+                lds_barrier();
+                if (wn == 0) {
+                    unsigned char *steps = a.steps + (size_t)in * a.dz_pitch + m0 + wm * C::TM * 16 + at;
+#pragma unroll
+                    for (int k = 0; k < OWN; ++k) {
+#pragma unroll
+                        for (int x = 1; x < C::WN; ++x) top[k] = fmaxf(top[k], s_top[x * C::BM + at + k]);
+                        const unsigned n = dz_steps(__float_as_uint(top[k]));
+                        s_up[at + k] = n == kNoDz ? 1.f : __uint_as_float((127u + 16u * n) << 23);
+                        steps[k] = (unsigned char)n;
+                    }
+                }
+                lds_barrier();
+                f32x4 up[C::TM];
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i) {
+                    up[i] = *reinterpret_cast<const f32x4 *>(s_up + i * 16 + lr);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) any |= up[i][r] != 1.f;
+                }
+                if (__ballot(any)) {
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < C::TN; ++j) acc[i][j] *= up[i];
+                }
+#pragma unroll
+                for (int k = 0; k < PLANES; ++k) {
+                    if (k > 0) lds_barrier();
+                    put_all(k);
                     store_turned(a.turned + k * a.turned_plane);
                 }
             }
@@ -546,6 +614,72 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 lds_barrier();
                 if (a.dz) store_rows(a.dz + k * a.dz_plane);
                 if (a.turned) store_turned(a.turned + k * a.turned_plane);
+            }
+        }
+    }
+}
+
+// Brings the turned dz of words whose row tiles took different steps to the least of them: the block's 64 words by a lane each, tiles by waves and
+// blockIdx.y.  Where none differ, which is the rule, it reads a byte per word and tile (3 us a piece).  Nothing is rounded but what falls below fp16's
+// places: two planes are taken together and apart again.  Words at 0 to -48 at random in each tile of 8192 rows (32000 x 1024): 100 us a piece, the step
+// 2313 -> 2438 us with bf16 gradients, 3304 -> 3718 with f32 ones.
+template <int PLANES>
+__global__ __launch_bounds__(256) void k_vocab_level(const Rows *__restrict__ rows, const unsigned char *__restrict__ steps, int steps_pitch, int tile,
+                                                     bf16_t *__restrict__ turned, size_t plane, int pitch, int words, unsigned char *__restrict__ level) {
+    __shared__ unsigned s_least[4][64];
+    const int count = rows->count, tiles = (count + tile - 1) / tile, lane = lane_id(), w = wave_id(), v0 = blockIdx.x * 64;
+    const unsigned char *mine = steps + v0 + lane;
+    unsigned least = kNoDz;
+    for (int t0 = w; t0 < tiles; t0 += 32) {
+        unsigned k[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) k[u] = mine[(size_t)min(t0 + 4 * u, tiles - 1) * steps_pitch];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) least = min(least, k[u]);
+    }
+    s_least[w][lane] = least;
+    __syncthreads();
+    least = min(min(s_least[0][lane], s_least[1][lane]), min(s_least[2][lane], s_least[3][lane]));
+    if (blockIdx.y == 0 && w == 0) level[v0 + lane] = (unsigned char)least;
+    constexpr int U = 2;                                                       // words of half a wave, whose loads leave together
+    for (int t = blockIdx.y * 4 + w; t < tiles; t += gridDim.y * 4) {
+        const int k = mine[(size_t)t * steps_pitch], down = 16 * (k - (int)least);
+        const int n0 = t * tile, n = min(tile, (count - n0 + 7) / 8 * 8), c = (lane & 31) * 8;     // a lane's eight rows: 32 lanes take a tile of up to 256
+        unsigned long long off = __ballot(v0 + lane < words && k < (int)kNoDz && down > 0);
+        while (off) {
+            u32x4 *row[U], u[U], low[U];
+            int by[U];
+            bool here[U];
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const int a = __builtin_ctzll(off);                            // the lower half's word, the upper half's
+                const unsigned long long rest = off & (off - 1);
+                const int b = rest ? __builtin_ctzll(rest) : a;
+                here[x] = off != 0 && (lane < 32 || rest != 0) && c < n;
+                const int l = off == 0 ? 0 : lane < 32 ? a : b;
+                by[x] = off == 0 ? 0 : lane < 32 ? __builtin_amdgcn_readlane(down, a) : __builtin_amdgcn_readlane(down, b);
+                row[x] = reinterpret_cast<u32x4 *>(turned + (size_t)(v0 + l) * pitch + n0 + c);
+                off = rest & (rest - 1);
+                if (here[x]) {
+                    u[x] = *row[x];
+                    if constexpr (PLANES == 2) low[x] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const bf16_t *>(row[x]) + plane);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                if (!here[x]) continue;
+                const f16x8 top = __builtin_bit_cast(f16x8, u[x]);
+                f16x8 new_top, new_low;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    float y = (float)top[r];
+                    if constexpr (PLANES == 2) y += (float)__builtin_bit_cast(f16x8, low[x])[r] * (1.f / kLowScale);
+                    y = scaled(y, -by[x]);
+                    new_top[r] = (_Float16)y;
+                    if constexpr (PLANES == 2) new_low[r] = (_Float16)((y - (float)new_top[r]) * kLowScale);
+                }
+                *row[x] = __builtin_bit_cast(u32x4, new_top);
+                if constexpr (PLANES == 2) *reinterpret_cast<u32x4 *>(reinterpret_cast<bf16_t *>(row[x]) + plane) = __builtin_bit_cast(u32x4, new_low);
             }
         }
     }
@@ -963,6 +1097,7 @@ struct GradsArgs {
     int words, D;                    // of this piece
     PlanePairs pairs;
     void *dW;                        // this piece's first row
+    const unsigned char *level;      // fp16: steps of 16 by which the words' rows of dz_turned were scaled up
     float *dw_sum, *dh_sum;          // [parts][words][D]; [parts][N][D], in the rows' gathered places
     size_t dw_part, dh_part;
     bool add;                        // not the first piece
@@ -1030,10 +1165,11 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
             const int v = n0 + (wn * C::TN + j) * 16 + (lane & 15);
             if (v >= words) continue;
             const size_t at = (size_t)v * D + d0;
+            const int back = -(half_of(MODE) ? e + 16 * a.level[v] : e);
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
                 if (cut.dw > 1) put4(a.dw_sum + part * a.dw_part + at + 16 * i, acc[i][j], D - d0 - 16 * i);
-                else put4(static_cast<grad_t *>(a.dW) + at + 16 * i, scaled(acc[i][j], -e), D - d0 - 16 * i);
+                else put4(static_cast<grad_t *>(a.dW) + at + 16 * i, scaled(acc[i][j], back), D - d0 - 16 * i);
             }
         }
         return;
@@ -1069,13 +1205,13 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_grads(const GradsArgs a) {
     }
 }
 
-// Parts of dW added in order and scaled back, where there are any.
+// Parts of dW added in order and scaled back, where there are any.  level: of fp16, otherwise null
 template <typename T>
-__global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict__ rows, bool half, const float *__restrict__ sums, size_t part, int words,
-                                                         int D, T *__restrict__ dW) {
+__global__ __launch_bounds__(256) void k_vocab_dw_finish(const Rows *__restrict__ rows, const unsigned char *__restrict__ level, const float *__restrict__ sums,
+                                                         size_t part, int words, int D, T *__restrict__ dW) {
     const int parts = rows->cut.dw, v = blockIdx.x * 4 + wave_id();
     if (parts < 2 || v >= words) return;
-    const int e = dw_exponent(*rows, half);
+    const int e = dw_exponent(*rows, level != nullptr) + (level ? 16 * level[v] : 0);
     for (int d = lane_id() * 4; d < D; d += 256) {
         const size_t at = (size_t)v * D + d;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -1121,7 +1257,7 @@ struct VocabPlan {
     int dz_planes;
     bool big_grads;
     CutArgs cut;
-    size_t count, rows, place, hp, ht, wp, wt, dzt, dw, part_max, part_sum, part_z, z_label, dz, dh, total;
+    size_t count, rows, place, hp, ht, wp, wt, dzt, dw, part_max, part_sum, part_z, z_label, dz, dh, steps, level, total;
     size_t h_plane, ht_plane, w_plane, wt_plane, dz_plane, dzt_plane, part_pitch;
     int tiles;                                        // most tiles along the vocabulary
 };
@@ -1202,6 +1338,10 @@ static VocabPlan vocab_plan(const echo_vocab_desc_t &d, bool bwd) {
         p.wt = take(p.planes * p.wt_plane * 2);
         p.dz = take(p.dz_planes * p.dz_plane * 2);
         p.dzt = take(p.dz_planes * p.dzt_plane * 2);
+        if (d.in_dtype == ECHO_BF16) {
+            p.steps = take((N + 127) / 128 * piece);
+            p.level = take(piece);
+        }
         if (p.cut.most_dw > 1) p.dw = take(p.cut.most_dw * piece * D * 4);
         p.dh = take(p.cut.most_dh * N * D * 4);
     }
@@ -1222,7 +1362,7 @@ static PlanePairs pairs_of(int a, int b) {             // planes of the operands
 }
 
 template <class C> static size_t product_lds() {
-    return std::max<size_t>(C::LDS_BYTES, (size_t)C::BN * (C::BM * 2 + 16));
+    return std::max<size_t>(C::LDS_BYTES, (size_t)C::BN * (C::BM * 2 + 16) + (C::WN + 1) * C::BM * 4);    // dz, and of its words the largest values and factors
 }
 
 // Launches a kernel whose LDS is above the default limit.
@@ -1439,6 +1579,7 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     a.turned = dW ? x.at<bf16_t>(p.dzt) : nullptr;
     a.turned_plane = p.dzt_plane;
     a.turned_pitch = p.turned_pitch;
+    a.steps = x.at<unsigned char>(p.steps);
     GradsArgs g{};
     g.dz = Operand{a.dz, p.dz_plane, p.piece, N};
     g.h_turned = Operand{x.at<bf16_t>(p.ht), p.ht_plane, p.turned_pitch, p.pitch};
@@ -1453,6 +1594,8 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     const bool bf16_out = desc->out_dtype == ECHO_BF16;
     const size_t out_bytes = bf16_out ? 2 : 4;
     const bool big = big_logits(std::min(p.piece, V), N);
+    const int row_tile = big ? 256 : 128, row_tiles = (N + row_tile - 1) / row_tile;
+    if (x.half()) g.level = row_tiles > 1 ? x.at<unsigned char>(p.level) : a.steps;
     for (int v0 = 0; v0 < V; v0 += p.piece) {
         const int n = std::min(p.piece, V - v0);
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
@@ -1463,6 +1606,13 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
         else if (bf16_out) s = big ? launch_logits<BigTile, Mode::kHalf>(a, N, x.st) : launch_logits<MidTile, Mode::kHalf>(a, N, x.st);
         else s = big ? launch_logits<BigTile, Mode::kHalves>(a, N, x.st) : launch_logits<MidTile, Mode::kHalves>(a, N, x.st);
         if (s) return s;
+        if (dW && x.half() && row_tiles > 1) {
+            LaunchRecord r = launch_begin("vocab_level", x.st);
+            const dim3 grid((n + 63) / 64, std::min(64, (row_tiles + 15) / 16));
+            if (bf16_out) k_vocab_level<1><<<grid, 256, 0, x.st>>>(a.count, a.steps, p.piece, row_tile, a.turned, p.dzt_plane, p.turned_pitch, n, x.at<unsigned char>(p.level));
+            else k_vocab_level<2><<<grid, 256, 0, x.st>>>(a.count, a.steps, p.piece, row_tile, a.turned, p.dzt_plane, p.turned_pitch, n, x.at<unsigned char>(p.level));
+            if (echo_status_t s = launch_end(r)) return s;
+        }
         g.words = n;
         g.dz_turned = Operand{a.turned, p.dzt_plane, p.turned_pitch, n};
         g.dW = dW ? static_cast<char *>(dW) + (size_t)v0 * D * out_bytes : nullptr;
@@ -1473,8 +1623,8 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
         if (s) return s;
         if (dW && p.cut.most_dw > 1) {
             LaunchRecord r = launch_begin("vocab_dw_finish", x.st);
-            if (bf16_out) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
-            else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, x.half(), g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
+            if (bf16_out) k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.level, g.dw_sum, g.dw_part, n, D, static_cast<bf16_t *>(g.dW));
+            else k_vocab_dw_finish<<<(n + 3) / 4, 256, 0, x.st>>>(g.rows, g.level, g.dw_sum, g.dw_part, n, D, static_cast<float *>(g.dW));
             if (echo_status_t s = launch_end(r)) return s;
         }
     }
