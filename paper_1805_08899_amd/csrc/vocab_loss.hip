@@ -455,6 +455,13 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
         }
     } else {
         const float off = 1.0f - a.eps, low = a.eps / (float)a.V;
+        if (n0 + C::BN > count) {                                              // rows behind the last one have no logits: zero times an infinite word is NaN
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i)
+                    if (n0 + (wn * C::TN + j) * 16 + (lane & 15) >= count) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
