@@ -1,6 +1,7 @@
 """Binding of libechoattn: same names as include/echoattn.h, include/echodropout.h, include/echolstm.h,
 include/echovocab.h and include/echoclip.h, argument marshalling only.  Device buffers are passed as torch tensors (their
-data_ptr() is taken) or as integer addresses; nothing is computed here.
+data_ptr() is taken) or as integer addresses; nothing is computed here.  Tokens, labels and key lengths are torch.int32 tensors:
+other types (torch's default is int64) and shorter ones raise ValueError.
 
 The shared library must have been built (python -m paper_1805_08899_amd.build);
 loading fails loudly otherwise -- there is no fallback path.
@@ -152,6 +153,16 @@ def _ptr(x):
     return c_void_p(x.data_ptr())
 
 
+def _index(x, count):
+    """Device address of at least `count` tokens, labels or key lengths: a torch.int32 tensor, an int, or None."""
+    if hasattr(x, "dtype"):
+        if str(x.dtype) != "torch.int32":
+            raise ValueError("tokens, labels and key lengths must be torch.int32")
+        if x.numel() < count:
+            raise ValueError(f"{x.numel()} tokens, labels or key lengths where the call reads {count}")
+    return _ptr(x)
+
+
 def _stream(stream):
     if stream is None:
         return None
@@ -188,7 +199,7 @@ def _ws_bytes(workspace, workspace_bytes):
 
 
 def echo_attn_fwd(desc, Qp, Kp, V, v, key_len, context, P, workspace, workspace_bytes=None, stream=None) -> int:
-    return lib().echo_attn_fwd(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _ptr(key_len),
+    return lib().echo_attn_fwd(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _index(key_len, desc.B),
                                _ptr(context), _ptr(P), _ptr(workspace), _ws_bytes(workspace, workspace_bytes),
                                _stream(stream))
 
@@ -196,7 +207,7 @@ def echo_attn_fwd(desc, Qp, Kp, V, v, key_len, context, P, workspace, workspace_
 def echo_attn_bwd(desc, dContext, P, Qp, Kp, V, v, key_len, dQp, dKp, dV, dv, workspace, workspace_bytes=None,
                   stream=None) -> int:
     return lib().echo_attn_bwd(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v),
-                               _ptr(key_len), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
+                               _index(key_len, desc.B), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
                                _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -205,25 +216,25 @@ ECHO_ATTN_STATIC_SCRATCH_BYTES = 20 << 20
 
 def echo_attn_bwd_static(desc, dContext, P, Qp, Kp, V, v, key_len, dQp, dKp, dV, dv, stream=None) -> int:
     return lib().echo_attn_bwd_static(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp), _ptr(V),
-                                      _ptr(v), _ptr(key_len), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv),
+                                      _ptr(v), _index(key_len, desc.B), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv),
                                       _stream(stream))
 
 
 def echo_attn_bwd_accumulate(desc, dContext, P, Qp, Kp, V, v, key_len, dQp, dKp, dV, dv, workspace,
                              workspace_bytes=None, stream=None) -> int:
     return lib().echo_attn_bwd_accumulate(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp), _ptr(V),
-                                          _ptr(v), _ptr(key_len), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv),
+                                          _ptr(v), _index(key_len, desc.B), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv),
                                           _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_attn_step_fwd(desc, Qp, Kp, V, v, key_len, context, P, stream=None) -> int:
-    return lib().echo_attn_step_fwd(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _ptr(key_len),
+    return lib().echo_attn_step_fwd(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _index(key_len, desc.B),
                                     _ptr(context), _ptr(P), _stream(stream))
 
 
 def echo_attn_step_bwd(desc, dContext, P, Qp, Kp, V, v, key_len, dQp, dKp, dV, dv_part, stream=None) -> int:
     return lib().echo_attn_step_bwd(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v),
-                                    _ptr(key_len), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv_part), _stream(stream))
+                                    _index(key_len, desc.B), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv_part), _stream(stream))
 
 
 def echo_attn_step_finish(desc, dv_part, dv, stream=None) -> int:
@@ -236,19 +247,19 @@ def echo_attn_steps_ds_bytes(desc) -> int:
 
 def echo_attn_step_bwd_query(desc, step, steps, dContext, P, Qp, Kp, V, v, key_len, dQp, ds_rows, stream=None) -> int:
     return lib().echo_attn_step_bwd_query(ctypes.byref(desc), step, steps, _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp),
-                                          _ptr(V), _ptr(v), _ptr(key_len), _ptr(dQp), _ptr(ds_rows), _stream(stream))
+                                          _ptr(V), _ptr(v), _index(key_len, desc.B), _ptr(dQp), _ptr(ds_rows), _stream(stream))
 
 
 def echo_attn_steps_bwd_keys(desc, dContext, P, Qp, Kp, v, key_len, ds_rows, dKp, dV, dv, workspace,
                              workspace_bytes=None, stream=None) -> int:
     return lib().echo_attn_steps_bwd_keys(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(Qp), _ptr(Kp), _ptr(v),
-                                          _ptr(key_len), _ptr(ds_rows), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
+                                          _index(key_len, desc.B), _ptr(ds_rows), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
                                           _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_attn_fwd_stash(desc, Qp, Kp, V, v, key_len, context, P, tanh_map, workspace, workspace_bytes=None,
                         stream=None) -> int:
-    return lib().echo_attn_fwd_stash(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _ptr(key_len),
+    return lib().echo_attn_fwd_stash(ctypes.byref(desc), _ptr(Qp), _ptr(Kp), _ptr(V), _ptr(v), _index(key_len, desc.B),
                                      _ptr(context), _ptr(P), _ptr(tanh_map), _ptr(workspace),
                                      _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
@@ -256,7 +267,7 @@ def echo_attn_fwd_stash(desc, Qp, Kp, V, v, key_len, context, P, tanh_map, works
 def echo_attn_bwd_stash(desc, dContext, P, tanh_map, V, v, key_len, dQp, dKp, dV, dv, workspace,
                         workspace_bytes=None, stream=None) -> int:
     return lib().echo_attn_bwd_stash(ctypes.byref(desc), _ptr(dContext), _ptr(P), _ptr(tanh_map), _ptr(V), _ptr(v),
-                                     _ptr(key_len), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
+                                     _index(key_len, desc.B), _ptr(dQp), _ptr(dKp), _ptr(dV), _ptr(dv), _ptr(workspace),
                                      _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -326,7 +337,7 @@ def make_vocab_desc(N, V, D, in_dtype="f32", out_dtype="f32") -> echo_vocab_desc
 
 
 def echo_embed_fwd(desc, tokens, table, scale, out, stream=None) -> int:
-    return lib().echo_embed_fwd(ctypes.byref(desc), _ptr(tokens), _ptr(table), scale, _ptr(out), _stream(stream))
+    return lib().echo_embed_fwd(ctypes.byref(desc), _index(tokens, desc.N), _ptr(table), scale, _ptr(out), _stream(stream))
 
 
 def echo_embed_bwd_workspace_bytes(desc) -> int:
@@ -334,12 +345,12 @@ def echo_embed_bwd_workspace_bytes(desc) -> int:
 
 
 def echo_embed_bwd(desc, tokens, dout, scale, dtable, workspace, workspace_bytes=None, stream=None) -> int:
-    return lib().echo_embed_bwd(ctypes.byref(desc), _ptr(tokens), _ptr(dout), scale, _ptr(dtable), _ptr(workspace),
+    return lib().echo_embed_bwd(ctypes.byref(desc), _index(tokens, desc.N), _ptr(dout), scale, _ptr(dtable), _ptr(workspace),
                                 _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_embed_bwd_accumulate(desc, tokens, dout, scale, dtable, workspace, workspace_bytes=None, stream=None) -> int:
-    return lib().echo_embed_bwd_accumulate(ctypes.byref(desc), _ptr(tokens), _ptr(dout), scale, _ptr(dtable),
+    return lib().echo_embed_bwd_accumulate(ctypes.byref(desc), _index(tokens, desc.N), _ptr(dout), scale, _ptr(dtable),
                                            _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -349,7 +360,7 @@ def echo_vocab_loss_fwd_workspace_bytes(desc) -> int:
 
 def echo_vocab_loss_fwd(desc, h, W, labels, label_smoothing, loss, lse, workspace, workspace_bytes=None,
                         stream=None) -> int:
-    return lib().echo_vocab_loss_fwd(ctypes.byref(desc), _ptr(h), _ptr(W), _ptr(labels), label_smoothing, _ptr(loss),
+    return lib().echo_vocab_loss_fwd(ctypes.byref(desc), _ptr(h), _ptr(W), _index(labels, desc.N), label_smoothing, _ptr(loss),
                                      _ptr(lse), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
@@ -359,7 +370,7 @@ def echo_vocab_loss_bwd_workspace_bytes(desc) -> int:
 
 def echo_vocab_loss_bwd(desc, dloss, lse, h, W, labels, label_smoothing, dh, dW, workspace, workspace_bytes=None,
                         stream=None) -> int:
-    return lib().echo_vocab_loss_bwd(ctypes.byref(desc), _ptr(dloss), _ptr(lse), _ptr(h), _ptr(W), _ptr(labels),
+    return lib().echo_vocab_loss_bwd(ctypes.byref(desc), _ptr(dloss), _ptr(lse), _ptr(h), _ptr(W), _index(labels, desc.N),
                                      label_smoothing, _ptr(dh), _ptr(dW), _ptr(workspace),
                                      _ws_bytes(workspace, workspace_bytes), _stream(stream))
 

@@ -7,8 +7,8 @@
 // backward pass 18.6 -> 14.5 us (its three launches are 7 of them), of a 50-step decoder sentence 609 -> 468 us.
 //
 // Arguments are matched by position or keyword; a device pointer is a torch tensor (contiguous), an integer address, None, or
-// any object (tensor subclasses among them) with is_contiguous() and data_ptr().  The interpreter lock is released around the library call, as ctypes
-// does.
+// any object (tensor subclasses among them) with is_contiguous() and data_ptr().  Tokens, labels and key lengths that have a type must be int32, and
+// as many as the call reads.  The interpreter lock is released around the library call, as ctypes does.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -29,7 +29,7 @@ namespace {
 PyTypeObject *g_desc_type = nullptr;                       // binding.echo_attn_desc_t
 PyTypeObject *g_vocab_desc_type = nullptr;                 // binding.echo_vocab_desc_t
 PyTypeObject *g_grad_type = nullptr;                       // binding.echo_grad_t
-PyObject *g_s_type, *g_s_data_ptr, *g_s_is_contiguous, *g_s_cuda_stream, *g_s_numel, *g_s_element_size;
+PyObject *g_s_type, *g_s_data_ptr, *g_s_is_contiguous, *g_s_cuda_stream, *g_s_numel, *g_s_element_size, *g_s_dtype;
 
 bool int_value(PyObject *o, unsigned long long &out) {     // two's complement bits of any integer, as ctypes takes them
     if (!PyLong_Check(o)) {
@@ -123,6 +123,35 @@ template <typename T> struct Ptr {
         return yes > 0 && address_from_attribute(o, g_s_data_ptr, true, p);
     }
     C value() const { return static_cast<C>(p); }
+};
+struct Index : Ptr<const int32_t> {                        // tokens, labels, key lengths: as many as the descriptor's first number says
+    bool resolve(PyObject *o, int32_t count) {
+        if (o == Py_None || PyLong_Check(o)) return true;
+        bool is_int = false;
+        unsigned long long n = 0;
+        if (THPVariable_CheckExact(o)) {                    // Ptr::read has accepted it
+            const at::Tensor &t = THPVariable_Unpack(o);
+            is_int = t.scalar_type() == at::kInt;
+            n = static_cast<unsigned long long>(t.numel());
+        } else {
+            PyObject *type = PyObject_GetAttr(o, g_s_dtype);
+            if (!type) {                                    // no tensor: an address under another name
+                PyErr_Clear();
+                return true;
+            }
+            PyObject *name = PyObject_Str(type);
+            is_int = name && PyUnicode_CompareWithASCIIString(name, "torch.int32") == 0;
+            Py_DECREF(type);
+            Py_XDECREF(name);
+            void *numel = nullptr;
+            if (!name || !address_from_attribute(o, g_s_numel, true, numel)) return false;
+            n = reinterpret_cast<uintptr_t>(numel);
+        }
+        if (!is_int) PyErr_SetString(PyExc_ValueError, "tokens, labels and key lengths must be torch.int32");
+        else if (count > 0 && n < static_cast<unsigned long long>(count))
+            PyErr_Format(PyExc_ValueError, "%llu tokens, labels or key lengths where the call reads %d", n, (int)count);
+        return !PyErr_Occurred();
+    }
 };
 struct Stream {
     using C = void *;
@@ -249,15 +278,18 @@ bool collect(Names &n, PyObject *const *args, Py_ssize_t nargs, PyObject *kwname
     return true;
 }
 
-template <typename P> bool resolve_bytes(P &, PyObject *) { return true; }
-bool resolve_bytes(Bytes &b, PyObject *ws) { return b.resolve(ws); }
-bool resolve_bytes(Count &n, PyObject *array) { return n.resolve(array); }
+// What depends on other parameters: the one in front of it, the descriptor
+template <typename P, typename First> bool resolve(P &, PyObject *const *, const First &) { return true; }
+template <typename First> bool resolve(Bytes &b, PyObject *const *slot, const First &) { return b.resolve(slot[-1]); }
+template <typename First> bool resolve(Count &n, PyObject *const *slot, const First &) { return n.resolve(slot[-1]); }
+bool resolve(Index &x, PyObject *const *slot, const Desc &d) { return x.resolve(slot[0], d.value()->B); }
+bool resolve(Index &x, PyObject *const *slot, const VocabDesc &d) { return x.resolve(slot[0], d.value()->N); }
 
 template <typename... K, size_t... I>
 PyObject *call_with(Names &n, PyObject **slot, std::index_sequence<I...>) {
     std::tuple<K...> a;
     if (!(std::get<I>(a).read(slot[I]) && ...)) return nullptr;
-    if (!(resolve_bytes(std::get<I>(a), slot[I > 0 ? I - 1 : 0]) && ...)) return nullptr;
+    if (!(resolve(std::get<I>(a), slot + I, std::get<0>(a)) && ...)) return nullptr;
     const auto fn = reinterpret_cast<echo_status_t (*)(typename K::C...)>(n.target);
     echo_status_t st;
     Py_BEGIN_ALLOW_THREADS
@@ -277,7 +309,6 @@ template <int ID, typename... K> struct Call {
 
 using In = Ptr<const void>;
 using InF = Ptr<const float>;
-using Len = Ptr<const int32_t>;
 using OutF = Ptr<float>;
 using Work = Ptr<void>;
 using I32 = Int<int32_t>;
@@ -286,28 +317,28 @@ using U64 = Int<uint64_t>;
 using Size = Int<size_t>;
 
 // every launching call of the headers
-using Fwd = Call<0, Desc, In, In, In, In, Len, OutF, OutF, Work, Bytes, Stream>;
-using Bwd = Call<1, Desc, InF, InF, In, In, In, In, Len, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
-using BwdStatic = Call<2, Desc, InF, InF, In, In, In, In, Len, OutF, OutF, OutF, OutF, Stream>;
-using BwdAccumulate = Call<3, Desc, InF, InF, In, In, In, In, Len, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
-using StepFwd = Call<4, Desc, In, In, In, In, Len, OutF, OutF, Stream>;
-using StepBwd = Call<5, Desc, InF, InF, In, In, In, In, Len, OutF, OutF, OutF, OutF, Stream>;
+using Fwd = Call<0, Desc, In, In, In, In, Index, OutF, OutF, Work, Bytes, Stream>;
+using Bwd = Call<1, Desc, InF, InF, In, In, In, In, Index, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
+using BwdStatic = Call<2, Desc, InF, InF, In, In, In, In, Index, OutF, OutF, OutF, OutF, Stream>;
+using BwdAccumulate = Call<3, Desc, InF, InF, In, In, In, In, Index, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
+using StepFwd = Call<4, Desc, In, In, In, In, Index, OutF, OutF, Stream>;
+using StepBwd = Call<5, Desc, InF, InF, In, In, In, In, Index, OutF, OutF, OutF, OutF, Stream>;
 using StepFinish = Call<6, Desc, InF, OutF, Stream>;
-using StepBwdQuery = Call<7, Desc, I32, I32, InF, InF, In, In, In, In, Len, OutF, Work, Stream>;
-using StepsBwdKeys = Call<8, Desc, InF, InF, In, In, In, Len, In, OutF, OutF, OutF, Work, Bytes, Stream>;
-using FwdStash = Call<9, Desc, In, In, In, In, Len, OutF, OutF, OutF, Work, Bytes, Stream>;
-using BwdStash = Call<10, Desc, InF, InF, InF, In, In, Len, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
+using StepBwdQuery = Call<7, Desc, I32, I32, InF, InF, In, In, In, In, Index, OutF, Work, Stream>;
+using StepsBwdKeys = Call<8, Desc, InF, InF, In, In, In, Index, In, OutF, OutF, OutF, Work, Bytes, Stream>;
+using FwdStash = Call<9, Desc, In, In, In, In, Index, OutF, OutF, OutF, Work, Bytes, Stream>;
+using BwdStash = Call<10, Desc, InF, InF, InF, In, In, Index, OutF, OutF, OutF, OutF, Work, Bytes, Stream>;
 using DropoutFwd = Call<11, InF, Size, Float, U64, U64, OutF, Ptr<uint32_t>, Stream>;
 using DropoutBwd = Call<12, InF, Ptr<const uint32_t>, Size, Float, OutF, Stream>;
 using LstmFwd = Call<13, I64, I64, InF, InF, InF, OutF, OutF, OutF, Stream>;
 using LstmBwd = Call<14, I64, I64, InF, InF, InF, InF, OutF, OutF, Stream>;
 using LstmFwdStash = Call<15, I64, I64, InF, InF, InF, OutF, OutF, OutF, OutF, Stream>;
 using LstmBwdStash = Call<16, I64, I64, InF, InF, InF, InF, InF, OutF, OutF, Stream>;
-using EmbedFwd = Call<17, VocabDesc, Len, In, Float, Work, Stream>;
-using EmbedBwd = Call<18, VocabDesc, Len, In, Float, OutF, Work, Bytes, Stream>;
-using EmbedBwdAccumulate = Call<19, VocabDesc, Len, In, Float, OutF, Work, Bytes, Stream>;
-using VocabLossFwd = Call<20, VocabDesc, In, In, Len, Float, OutF, OutF, Work, Bytes, Stream>;
-using VocabLossBwd = Call<21, VocabDesc, InF, InF, In, In, Len, Float, Work, Work, Work, Bytes, Stream>;
+using EmbedFwd = Call<17, VocabDesc, Index, In, Float, Work, Stream>;
+using EmbedBwd = Call<18, VocabDesc, Index, In, Float, OutF, Work, Bytes, Stream>;
+using EmbedBwdAccumulate = Call<19, VocabDesc, Index, In, Float, OutF, Work, Bytes, Stream>;
+using VocabLossFwd = Call<20, VocabDesc, In, In, Index, Float, OutF, OutF, Work, Bytes, Stream>;
+using VocabLossBwd = Call<21, VocabDesc, InF, InF, In, In, Index, Float, Work, Work, Work, Bytes, Stream>;
 using GradNorm = Call<22, Grads, Count, OutF, Work, Bytes, Stream>;
 using GradClip = Call<23, Grads, Count, Float, OutF, Work, Bytes, Stream>;
 
@@ -400,6 +431,7 @@ PyMODINIT_FUNC PyInit__py_calls() {
     g_s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     g_s_numel = PyUnicode_InternFromString("numel");
     g_s_element_size = PyUnicode_InternFromString("element_size");
-    if (!g_s_type || !g_s_data_ptr || !g_s_is_contiguous || !g_s_cuda_stream || !g_s_numel || !g_s_element_size) return nullptr;
+    g_s_dtype = PyUnicode_InternFromString("dtype");
+    if (!g_s_type || !g_s_data_ptr || !g_s_is_contiguous || !g_s_cuda_stream || !g_s_numel || !g_s_element_size || !g_s_dtype) return nullptr;
     return PyModule_Create(&g_module);
 }
