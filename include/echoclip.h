@@ -8,8 +8,8 @@
  *   g    = g * max_norm / norm     if norm > max_norm, otherwise g as it is
  *
  * Squares and sums are fp64: they neither overflow nor lose small entries, whatever the number of elements.  A norm that is
- * not finite (an infinity or a NaN among the gradients) clips nothing: the gradients stay as they are, and `norm` says so to
- * whoever reads it.  `norm` is the norm before clipping, rounded to fp32.
+ * not finite (an infinity or a NaN among the gradients, or finite ones whose norm is past fp32's largest number) clips nothing: the
+ * gradients stay as they are, and `norm` says so to whoever reads it.  `norm` is the norm before clipping, rounded to fp32.
  *
  * Conventions: `grads` is HOST memory, read before the call returns (a HIP graph that captures the call keeps what it held).  The data
  * pointers in it are caller-owned DEVICE memory, contiguous and 16-byte aligned; `clipped` may be the very pointer `grad`

@@ -66,5 +66,5 @@ def grad_norm(grads):
 
 def grad_clip(grads, max_norm):
     norm = grad_norm(grads)
-    f = max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0
+    f = max_norm / norm if max_norm < norm < 2.0 ** 128 - 2.0 ** 103 else 1.0      # from there on fp32 rounds a norm to infinity
     return norm, [np.asarray(g, np.float64) * f for g in grads]

@@ -148,9 +148,13 @@ __global__ __launch_bounds__(kClipThreads) void k_grad_scale(const ClipTable tab
     if (any && s.whole()) s.load(v);
     const double x = grad_norm_of(parts, n_parts, s_sum);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)x;
-    // false for NaN; an infinite norm clips nothing either
-    const bool clip = x > (double)max_norm && x < __builtin_inf();
-    const float f = clip ? (float)((double)max_norm / x) : 1.0f;
+    // false for NaN; a norm that fp32 rounds to infinity, which is what the caller reads, clips nothing either
+    const bool clip = x > (double)max_norm && (float)x < __builtin_inff();
+    // f 2^k: a factor below 2^-100 (down to 2^-277) would lose digits in fp32; f has [1/2, 1) then, so that no product overflows
+    const double factor = clip ? (double)max_norm / x : 1.;
+    const int k = factor < 0x1p-100 ? (int)(__builtin_bit_cast(unsigned long long, factor) >> 52) - 1022 : 0;
+    const float f = (float)__builtin_amdgcn_ldexp(factor, -k);
+    const auto scaled = [&](float v) { return __builtin_amdgcn_ldexpf(v * f, k); };
     for (long long r = blockIdx.x; r < tab.spans; r += gridDim.x) {
         if (r > blockIdx.x) {
             s.find(tab, tab.spans - 1 - r);
@@ -160,10 +164,10 @@ __global__ __launch_bounds__(kClipThreads) void k_grad_scale(const ClipTable tab
         if (s.whole()) {
             if (clip) {
 #pragma unroll
-                for (int k = 0; k < kSpanLoads; ++k)
+                for (int l = 0; l < kSpanLoads; ++l)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        v[k][j] = s.bf16 ? bf16_round2(bf_lo(v[k][j]) * f, bf_hi(v[k][j]) * f) : __float_as_uint(__uint_as_float(v[k][j]) * f);
+                        v[l][j] = s.bf16 ? bf16_round2(scaled(bf_lo(v[l][j])), scaled(bf_hi(v[l][j]))) : __float_as_uint(scaled(__uint_as_float(v[l][j])));
             }
 #pragma unroll
             for (int k = 0; k < kSpanLoads; ++k)
@@ -172,10 +176,10 @@ __global__ __launch_bounds__(kClipThreads) void k_grad_scale(const ClipTable tab
             for (int i = threadIdx.x; i < (int)s.left; i += kClipThreads) {
                 if (s.bf16) {
                     const unsigned short u = reinterpret_cast<const unsigned short *>(s.src)[i];
-                    reinterpret_cast<unsigned short *>(s.dst)[i] = clip ? bf16_round(__uint_as_float((unsigned)u << 16) * f) : u;
+                    reinterpret_cast<unsigned short *>(s.dst)[i] = clip ? bf16_round(scaled(__uint_as_float((unsigned)u << 16))) : u;
                 } else {
                     const float u = reinterpret_cast<const float *>(s.src)[i];
-                    reinterpret_cast<float *>(s.dst)[i] = clip ? u * f : u;
+                    reinterpret_cast<float *>(s.dst)[i] = clip ? scaled(u) : u;
                 }
             }
         }
