@@ -1395,14 +1395,15 @@ template <class C, Mode MODE> static echo_status_t launch_logits(const LogitsArg
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
     constexpr bool BWD = MODE != Mode::kForward;
-    return launch_tiles(BWD ? "vocab_dlogits" : "vocab_logits", &k_vocab_logits<C, MODE>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
+    constexpr const char *name = C::BM == 256 ? (BWD ? "vocab_dlogits_256" : "vocab_logits_256") : (BWD ? "vocab_dlogits_128" : "vocab_logits_128");
+    return launch_tiles(name, &k_vocab_logits<C, MODE>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
                         C::THREADS, a, st);
 }
 template <class C, Mode MODE> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long tm = (a.D + C::BM - 1) / C::BM, tw = (a.words + C::BN - 1) / C::BN, th = (N + C::BN - 1) / C::BN;
     const long long blocks = (tm * tw * (a.dW ? cut.most_dw : 0) + 7) / 8 * 8 + tm * th * (a.dh_sum ? cut.most_dh : 0);
-    return launch_tiles("vocab_grads", &k_vocab_grads<C, MODE>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
+    return launch_tiles(C::BM == 256 ? "vocab_grads_256" : "vocab_grads_128", &k_vocab_grads<C, MODE>, granted, C::LDS_BYTES, blocks, C::THREADS, a, st);
 }
 
 static echo_status_t check_vocab(const echo_vocab_desc_t *d, float eps) {

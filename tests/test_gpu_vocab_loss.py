@@ -140,8 +140,8 @@ CASES = [
     (700, 1500, 260, "f32", "f32", 0.0),
     (2500, 70, 136, "bf16", "f32", 0.1),       # more rows than words
     (8, 2000, 16384, "f32", "f32", 0.0),       # words of f32 storage in two pieces; the widest rows
-    (4100, 8200, 64, "bf16", "bf16", 0.1),     # tiles of 256 x 256
-    (4100, 11000, 40, "f32", "f32", 0.0),      # the same, dz in two pieces
+    (4100, 8200, 64, "bf16", "bf16", 0.1),     # tiles of 128 x 128 (those of 256 x 256: test_gpu_vocab_tiles.py)
+    (4100, 11000, 40, "f32", "f32", 0.0),      # logits in tiles of 256 x 256, dz in two pieces
 ]
 IDS = ["N%d_V%d_D%d_%s_%s_%g" % c for c in CASES]
 
