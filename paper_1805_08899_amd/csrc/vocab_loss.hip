@@ -996,12 +996,14 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
-// -log p of the label: log(1 + sum over the other words of exp(z - z_label)), which keeps the digits of a sure label's loss
+// -log p of the label: log(1 + sum over the other words of exp(z - z_label)), which keeps the digits of a sure label's loss.  lse from whichever of the label's
+// logit and the maximum is larger: the digits of a label far below (from -infinity, a word that is shut out) are not in it.
 __device__ __forceinline__ void loss_of_row(float top, float sum, float z, float zl, int V, float eps, float &loss, float &lse) {
     const float t = top - zl;
-    const float nll = t > 0.f ? t + logf(sum + expf(-t)) : log1pf(sum * expf(t));
-    lse = zl + nll;
-    loss = nll;
+    const float rest = t > 0.f ? logf(sum + expf(-t)) : log1pf(sum * expf(t));
+    lse = (t > 0.f ? top : zl) + rest;
+    loss = t > 0.f ? t + rest : rest;
+    if (zl == __builtin_inff()) loss = __builtin_nanf("");
     if (eps > 0.f) loss += eps * (zl - z / (float)V);
 }
 
