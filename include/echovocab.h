@@ -32,8 +32,9 @@
  *     nearest even, from its fp32 sum.  loss, lse, dloss and dE are fp32.  The loss takes out_dtype ECHO_BF16 with in_dtype
  *     ECHO_BF16 only (ECHO_ERR_DTYPE); the embedding takes all four pairs.
  *   - Products run on the matrix cores with fp32 sums.  f32 storage: an operand is taken as the sum of three bf16 numbers, which add up to it
- *     exactly, a product of two of them as the six that matter (error as of fp32 products), and so is dz; infinities in h or W, and
- *     numbers past 2^127, give NaN.
+ *     exactly (below 2^-110 they are off by up to 2^-134), a product of two of them as the six that matter (error as of fp32 products), and
+ *     so is dz, with a factor of 2^24 until the sums are done; infinities in h or W, numbers past 2^127, and dloss, dh or dW from 2^104
+ *     on give NaN or infinities.
  *   - bf16 storage: the gradients' operands are fp16.  h and W are exact in it, scaled by a power of two, down to 2^-32 of their largest
  *     finite value (of the rows with a label, of all words), and off by up to 2^-40 of that below.  dz is taken as two fp16 numbers behind
  *     f32 gradients (off by up to 2^-22 of it) and as one behind bf16 gradients (2^-11, an eighth of what the rounding of
