@@ -45,7 +45,7 @@ struct Cut {
 };
 struct CutArgs {
     int words, D;                    // of a whole piece: the last one, which may be narrower, is cut into as many parts
-    int most_dw, most_dh;            // parts there is room for; 0: that gradient is not wanted
+    int most_dw, most_dh;            // parts there is room for, of either gradient whether it is wanted or not: each is the same beside the other and alone
     int tile, slots;                 // tile x tile; blocks that run at once
     int pairs;
     float round;                     // what a step of a round takes, against one of 256 blocks of 256 x 256
@@ -61,7 +61,7 @@ __host__ __device__ inline Cut cut_choice(const CutArgs &a, int count, int i, fl
     Cut c = {(kw + len - 1) / len, (kh + len - 1) / len};
     c.dw = c.dw < a.most_dw ? c.dw : a.most_dw;
     c.dh = c.dh < a.most_dh ? c.dh : a.most_dh;
-    const int lw = c.dw ? (kw + c.dw - 1) / c.dw : 0, lh = c.dh ? (kh + c.dh - 1) / c.dh : 0, longest = lw > lh ? lw : lh;
+    const int lw = (kw + c.dw - 1) / c.dw, lh = (kh + c.dh - 1) / c.dh, longest = lw > lh ? lw : lh;
     const long long units = (long long)tw * c.dw + (long long)th * c.dh;
     const float rounds = (float)((units + a.slots - 1) / a.slots);
     cost = rounds * ((float)(longest * a.pairs) + kUnitSteps) * a.round +
