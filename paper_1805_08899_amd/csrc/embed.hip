@@ -10,9 +10,10 @@
 //   k_embed_sum    a wave per word with up to kRun tokens adds their rows in order; a wave per kRun sorted tokens adds what of them belongs to
 //                  longer runs (the commonest word of Zipf's law has a tenth of all tokens, padding more) into parts.
 //   k_embed_join   adds the parts of a long run in order.
-// Measured: forward 12800 bf16 rows of 512 7 us, one of 64 f32 rows 2.6.  Backward, V = 32000, 12800 f32 rows of 512, 40 % padding: 8.5 + 12.6 (66 MB
+// Measured: forward 12800 bf16 rows of 1024 7 us, one of 64 f32 rows 2.6.  Backward, V = 32000, 12800 f32 rows of 512, 40 % padding: 8.5 + 12.6 (66 MB
 // written at 5.7 TB/s) + 5.1 us; V = 50021, 9601 bf16 rows of 1020 added: 8.5 + 16.3 + 5.8.  The first and the last are trips to memory one after
-// the other (tokens, counters, positions; first of a run, parts, row), not bytes.
+// the other (tokens, counters, positions; first of a run, parts, row), not bytes.  Rows that are no multiple of four are taken value by value, twice the time where bf16
+// ones come from the caches (12800 rows of 1001 values instead of 1000: forward bf16 7.9 -> 15.7, f32 16.9 -> 18.1 us; backward 40.5 -> 62.7, 39.7 -> 58.7).
 #include "../../include/echovocab.h"
 
 #include <hip/hip_runtime.h>

@@ -12,9 +12,9 @@
 //
 // Bound by the matrix cores: 2 N V D forward, 8 N V D for both directions (the logits are formed twice, as the tanh map of the attention is: to keep
 // them would take 4 N V bytes written and read twice), times the number of plane pairs (product.hpp, split.hpp).
-// Measured (8192 rows x 100003 words x 2048, bf16): logits 2.45 ms (1370 TFLOP/s), logits and dz 3.1 (the stores of dz and of its turned form, 3.3 GB, are
-// not hidden: a compute unit holds one block), dW and dh 5.9 (1140: by the power limit; pieces whose tiles fill whole rounds gained nothing),
-// all else 0.4.  One of 3520 x 32000 x 1024 with f32 gradients: 0.21, 0.43, 0.85, 0.15.
+// Measured (8192 rows x 100003 words x 2048, bf16): logits 2.5 ms (1340 TFLOP/s), logits and dz 3.25 (the stores of dz and of its turned form, 3.3 GB, are
+// not hidden: a compute unit holds one block), dW and dh 6.1 (1100: by the power limit; pieces whose tiles fill whole rounds gained nothing),
+// all else 0.4.  One of 3520 x 32000 x 1024 with f32 gradients: 0.23, 0.45, 0.88, 0.12.
 #include "../../include/echovocab.h"
 
 #include <hip/hip_runtime.h>
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 }
 
 // Brings the turned dz of words whose row tiles took different steps to the least of them: the block's 64 words by a lane each, tiles by waves and
-// blockIdx.y.  Where none differ, which is the rule, it reads a byte per word and tile (3 us a piece).  Nothing is rounded but what falls below fp16's
+// blockIdx.y.  Where none differ, which is the rule, it reads a byte per word and tile (5 us a piece).  Nothing is rounded but what falls below fp16's
 // places: two planes are taken together and apart again.  Words at 0 to -48 at random in each tile of 8192 rows (32000 x 1024): 100 us a piece, the step
 // 2313 -> 2438 us with bf16 gradients, 3304 -> 3718 with f32 ones.
 template <int PLANES>
@@ -703,7 +703,8 @@ __global__ __launch_bounds__(256) void k_vocab_level(const Rows *__restrict__ ro
 //   bf16  128 rows  49 / 57,   30 / 38,  14 / 24    256    78 / 70,   51 / 36,  14 / 24    512   132 / 97,   92 / 45,  20 / 25
 // few_pays() has what these (and 96, 192 and 384 rows) come to in rounds of 256 blocks.
 // The backward pass of f32 takes the same kernel for dz, with the rows as they were gathered; only the turned words are packed then (forward and
-// backward of 38 rows of 19710 x 1256 454 -> 270 us, of 64 of 32000 x 1024 440 -> 292, of 300 of 60000 x 1500 2546 -> 2196).
+// backward of 38 rows of 19710 x 1256 454 -> 270 us, of 64 of 32000 x 1024 440 -> 292, of 300 of 60000 x 1500 2546 -> 2196).  Where it does is decided by
+// the forward's rule, which knows neither the packed rows nor the 2-byte stores of the turned dz: measured at these sizes and 556 of 2180 x 936 only.
 constexpr int kFewGroup = 64, kFewAlone = 16;
 template <typename T> static bool few_pays(size_t N, size_t V, size_t D) {
     // rows of whole 16-byte groups, and offsets of 31 bits among them
