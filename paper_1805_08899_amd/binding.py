@@ -1,6 +1,6 @@
 """Binding of libechoattn: same names as include/echoattn.h, include/echodropout.h, include/echolstm.h,
-include/echovocab.h and include/echoclip.h, argument marshalling only.  Device buffers are passed as torch tensors (their
-data_ptr() is taken) or as integer addresses; nothing is computed here.  Tokens, labels and key lengths are torch.int32 tensors:
+include/echovocab.h, include/echoclip.h, include/echoscan.h, include/echodistill.h and include/echodraft.h, argument marshalling only.  Device buffers are passed as torch tensors (their
+data_ptr() is taken) or as integer addresses; nothing is computed here.  Words, labels and lengths are torch.int32 tensors:
 other types (torch's default is int64) and shorter ones raise ValueError.
 
 The shared library must have been built (python -m paper_1805_08899_amd.build);
@@ -35,6 +35,18 @@ ECHO_VOCAB_MAX_ROWS, ECHO_VOCAB_MAX_D, ECHO_GRAD_MAX_COUNT = 1 << 24, 16384, 163
 
 class echo_vocab_desc_t(ctypes.Structure):
     _fields_ = [("N", c_int32), ("V", c_int32), ("D", c_int32), ("in_dtype", c_int32), ("out_dtype", c_int32)]
+
+
+class echo_scan_desc_t(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("T", c_int32), ("H", c_int32), ("dtype", c_int32), ("reverse", c_int32)]
+
+
+class echo_draft_desc_t(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("K", c_int32), ("V", c_int32), ("dtype", c_int32)]
+
+
+ECHO_SCAN_MAX_ROWS, ECHO_SCAN_MAX_H, ECHO_SCAN_CHUNK = 1 << 24, 1 << 20, 128
+ECHO_DISTILL_MAX_K, ECHO_DRAFT_MAX_B, ECHO_DRAFT_MAX_K, ECHO_DRAFT_MAX_V = 128, 1 << 20, 1024, 1 << 24
 
 
 class echo_grad_t(ctypes.Structure):
@@ -94,6 +106,19 @@ EXPORTS = {
     "echo_grad_workspace_bytes": (c_size_t, [POINTER(echo_grad_t), c_int32]),
     "echo_grad_norm": (c_int, [POINTER(echo_grad_t), c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
     "echo_grad_clip": (c_int, [POINTER(echo_grad_t), c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "echo_scan_states_bytes": (c_size_t, [POINTER(echo_scan_desc_t)]),
+    "echo_scan_fwd_workspace_bytes": (c_size_t, [POINTER(echo_scan_desc_t)]),
+    "echo_scan_fwd": (c_int, [POINTER(echo_scan_desc_t)] + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "echo_scan_bwd_workspace_bytes": (c_size_t, [POINTER(echo_scan_desc_t)]),
+    "echo_scan_bwd": (c_int, [POINTER(echo_scan_desc_t)] + [c_void_p] * 8 + [c_size_t, c_void_p]),
+    "echo_distill_fwd_workspace_bytes": (c_size_t, [POINTER(echo_vocab_desc_t), c_int32]),
+    "echo_distill_fwd": (c_int, [POINTER(echo_vocab_desc_t)] + [c_void_p] * 4 + [c_int32, c_float] + [c_void_p] * 3 +
+                         [c_size_t, c_void_p]),
+    "echo_distill_bwd_workspace_bytes": (c_size_t, [POINTER(echo_vocab_desc_t), c_int32]),
+    "echo_distill_bwd": (c_int, [POINTER(echo_vocab_desc_t)] + [c_void_p] * 6 + [c_int32, c_float] + [c_void_p] * 3 +
+                         [c_size_t, c_void_p]),
+    "echo_draft_verify_workspace_bytes": (c_size_t, [POINTER(echo_draft_desc_t)]),
+    "echo_draft_verify": (c_int, [POINTER(echo_draft_desc_t)] + [c_void_p] * 9 + [c_size_t, c_void_p]),
     "echo_status_string": (c_char_p, [c_int]),
     "echo_last_error_detail": (c_char_p, []),
     "echo_version": (c_char_p, []),
@@ -134,7 +159,7 @@ def _install_native_calls(L) -> None:
     if not os.path.exists(PY_CALLS_PATH):
         raise FileNotFoundError(f"{PY_CALLS_PATH} is missing: build it with `python -m paper_1805_08899_amd.build`")
     from . import _py_calls
-    _py_calls.bind(echo_attn_desc_t, echo_vocab_desc_t, echo_grad_t,
+    _py_calls.bind((echo_attn_desc_t, echo_vocab_desc_t, echo_grad_t, echo_scan_desc_t, echo_draft_desc_t),
                    {name: ctypes.cast(getattr(L, name), c_void_p).value for name in EXPORTS})
     for name in EXPORTS:
         native = getattr(_py_calls, name, None)
@@ -412,6 +437,69 @@ def echo_grad_norm(grads, count, norm, workspace, workspace_bytes=None, stream=N
 def echo_grad_clip(grads, count, max_norm, norm, workspace, workspace_bytes=None, stream=None) -> int:
     return lib().echo_grad_clip(grads, _count(grads, count), max_norm, _ptr(norm), _ptr(workspace),
                                 _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def make_scan_desc(B, T, H, dtype="f32", reverse=False) -> echo_scan_desc_t:
+    return echo_scan_desc_t(B, T, H, DTYPES[dtype] if isinstance(dtype, str) else int(dtype), int(reverse))
+
+
+def echo_scan_states_bytes(desc) -> int:
+    return lib().echo_scan_states_bytes(ctypes.byref(desc))
+
+
+def echo_scan_fwd_workspace_bytes(desc) -> int:
+    return lib().echo_scan_fwd_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_scan_fwd(desc, G, c0, len, h, c_last, states, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_scan_fwd(ctypes.byref(desc), _ptr(G), _ptr(c0), _index(len, desc.B), _ptr(h), _ptr(c_last), _ptr(states),
+                               _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_scan_bwd_workspace_bytes(desc) -> int:
+    return lib().echo_scan_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_scan_bwd(desc, dh, dc_last, G, len, states, dG, dc0, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_scan_bwd(ctypes.byref(desc), _ptr(dh), _ptr(dc_last), _ptr(G), _index(len, desc.B), _ptr(states), _ptr(dG),
+                               _ptr(dc0), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def _words(x, rows, each):
+    return _index(x, rows * each if rows > 0 and each > 0 else 0)
+
+
+def echo_distill_fwd_workspace_bytes(desc, K) -> int:
+    return lib().echo_distill_fwd_workspace_bytes(ctypes.byref(desc), K)
+
+
+def echo_distill_fwd(desc, h, W, words, logits, K, T, loss, lse, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_distill_fwd(ctypes.byref(desc), _ptr(h), _ptr(W), _words(words, desc.N, K), _ptr(logits), K, T, _ptr(loss),
+                                  _ptr(lse), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def echo_distill_bwd_workspace_bytes(desc, K) -> int:
+    return lib().echo_distill_bwd_workspace_bytes(ctypes.byref(desc), K)
+
+
+def echo_distill_bwd(desc, dloss, lse, h, W, words, logits, K, T, dh, dW, workspace, workspace_bytes=None, stream=None) -> int:
+    return lib().echo_distill_bwd(ctypes.byref(desc), _ptr(dloss), _ptr(lse), _ptr(h), _ptr(W), _words(words, desc.N, K), _ptr(logits),
+                                  K, T, _ptr(dh), _ptr(dW), _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
+
+
+def make_draft_desc(B, K, V, dtype="f32") -> echo_draft_desc_t:
+    return echo_draft_desc_t(B, K, V, DTYPES[dtype] if isinstance(dtype, str) else int(dtype))
+
+
+def echo_draft_verify_workspace_bytes(desc) -> int:
+    return lib().echo_draft_verify_workspace_bytes(ctypes.byref(desc))
+
+
+def echo_draft_verify(desc, drafted, n_drafted, draft, target, u, r, tokens, taken, workspace, workspace_bytes=None,
+                      stream=None) -> int:
+    return lib().echo_draft_verify(ctypes.byref(desc), _words(drafted, desc.B, desc.K), _index(n_drafted, desc.B), _ptr(draft),
+                                   _ptr(target), _ptr(u), _ptr(r), _ptr(tokens), _ptr(taken), _ptr(workspace),
+                                   _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_status_string(status: int) -> str:

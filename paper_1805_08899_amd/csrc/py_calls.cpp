@@ -20,8 +20,11 @@
 #include <utility>
 
 #include "../../include/echoclip.h"
+#include "../../include/echodistill.h"
+#include "../../include/echodraft.h"
 #include "../../include/echodropout.h"
 #include "../../include/echolstm.h"
+#include "../../include/echoscan.h"
 #include "../../include/echovocab.h"
 
 namespace {
@@ -29,6 +32,8 @@ namespace {
 PyTypeObject *g_desc_type = nullptr;                       // binding.echo_attn_desc_t
 PyTypeObject *g_vocab_desc_type = nullptr;                 // binding.echo_vocab_desc_t
 PyTypeObject *g_grad_type = nullptr;                       // binding.echo_grad_t
+PyTypeObject *g_scan_desc_type = nullptr;                  // binding.echo_scan_desc_t
+PyTypeObject *g_draft_desc_type = nullptr;                 // binding.echo_draft_desc_t
 PyObject *g_s_type, *g_s_data_ptr, *g_s_is_contiguous, *g_s_cuda_stream, *g_s_numel, *g_s_element_size, *g_s_dtype;
 
 bool int_value(PyObject *o, unsigned long long &out) {     // two's complement bits of any integer, as ctypes takes them
@@ -68,6 +73,8 @@ template <typename T, PyTypeObject *&TYPE> struct Struct {  // a ctypes structur
 };
 using Desc = Struct<echo_attn_desc_t, g_desc_type>;
 using VocabDesc = Struct<echo_vocab_desc_t, g_vocab_desc_type>;
+using ScanDesc = Struct<echo_scan_desc_t, g_scan_desc_type>;
+using DraftDesc = Struct<echo_draft_desc_t, g_draft_desc_type>;
 struct Grads {                                             // a ctypes array of echo_grad_t
     using C = const echo_grad_t *;
     Py_buffer view{};
@@ -125,7 +132,7 @@ template <typename T> struct Ptr {
     C value() const { return static_cast<C>(p); }
 };
 struct Index : Ptr<const int32_t> {                        // tokens, labels, key lengths: as many as the descriptor's first number says
-    bool resolve(PyObject *o, int32_t count) {
+    bool resolve(PyObject *o, int64_t count) {
         if (o == Py_None || PyLong_Check(o)) return true;
         bool is_int = false;
         unsigned long long n = 0;
@@ -149,10 +156,11 @@ struct Index : Ptr<const int32_t> {                        // tokens, labels, ke
         }
         if (!is_int) PyErr_SetString(PyExc_ValueError, "tokens, labels and key lengths must be torch.int32");
         else if (count > 0 && n < static_cast<unsigned long long>(count))
-            PyErr_Format(PyExc_ValueError, "%llu tokens, labels or key lengths where the call reads %d", n, (int)count);
+            PyErr_Format(PyExc_ValueError, "%llu tokens, labels or key lengths where the call reads %lld", n, (long long)count);
         return !PyErr_Occurred();
     }
 };
+struct Words : Index {};                                   // so many per row: the number behind the next argument, or the descriptor's K
 struct Stream {
     using C = void *;
     void *p = nullptr;
@@ -284,6 +292,15 @@ template <typename First> bool resolve(Bytes &b, PyObject *const *slot, const Fi
 template <typename First> bool resolve(Count &n, PyObject *const *slot, const First &) { return n.resolve(slot[-1]); }
 bool resolve(Index &x, PyObject *const *slot, const Desc &d) { return x.resolve(slot[0], d.value()->B); }
 bool resolve(Index &x, PyObject *const *slot, const VocabDesc &d) { return x.resolve(slot[0], d.value()->N); }
+bool resolve(Index &x, PyObject *const *slot, const ScanDesc &d) { return x.resolve(slot[0], d.value()->B); }
+bool resolve(Index &x, PyObject *const *slot, const DraftDesc &d) { return x.resolve(slot[0], d.value()->B); }
+// (numbers that the library refuses ask for nothing here)
+int64_t both(int64_t rows, int64_t each) { return rows > 0 && each > 0 ? rows * each : 0; }
+bool resolve(Words &x, PyObject *const *slot, const VocabDesc &d) {
+    unsigned long long k = 0;
+    return int_value(slot[2], k) && x.resolve(slot[0], both(d.value()->N, static_cast<int32_t>(k)));
+}
+bool resolve(Words &x, PyObject *const *slot, const DraftDesc &d) { return x.resolve(slot[0], both(d.value()->B, d.value()->K)); }
 
 template <typename... K, size_t... I>
 PyObject *call_with(Names &n, PyObject **slot, std::index_sequence<I...>) {
@@ -341,6 +358,11 @@ using VocabLossFwd = Call<20, VocabDesc, In, In, Index, Float, OutF, OutF, Work,
 using VocabLossBwd = Call<21, VocabDesc, InF, InF, In, In, Index, Float, Work, Work, Work, Bytes, Stream>;
 using GradNorm = Call<22, Grads, Count, OutF, Work, Bytes, Stream>;
 using GradClip = Call<23, Grads, Count, Float, OutF, Work, Bytes, Stream>;
+using ScanFwd = Call<24, ScanDesc, In, InF, Index, Work, OutF, OutF, Work, Bytes, Stream>;
+using ScanBwd = Call<25, ScanDesc, In, InF, In, Index, InF, Work, OutF, Work, Bytes, Stream>;
+using DistillFwd = Call<26, VocabDesc, In, In, Words, InF, I32, Float, OutF, OutF, Work, Bytes, Stream>;
+using DistillBwd = Call<27, VocabDesc, InF, InF, In, In, Words, InF, I32, Float, Work, Work, Work, Bytes, Stream>;
+using DraftVerify = Call<28, DraftDesc, Words, Index, In, In, InF, InF, Ptr<int32_t>, Ptr<int32_t>, Work, Bytes, Stream>;
 
 #define NAMES(CALL, FN, REQUIRED, ...) template <> Names CALL::names = {FN, {__VA_ARGS__, nullptr}, REQUIRED, {}, 0, nullptr}
 NAMES(Fwd, "echo_attn_fwd", 9, "desc", "Qp", "Kp", "V", "v", "key_len", "context", "P", "workspace", "workspace_bytes", "stream");
@@ -378,18 +400,29 @@ NAMES(VocabLossBwd, "echo_vocab_loss_bwd", 10, "desc", "dloss", "lse", "h", "W",
       "workspace_bytes", "stream");
 NAMES(GradNorm, "echo_grad_norm", 4, "grads", "count", "norm", "workspace", "workspace_bytes", "stream");
 NAMES(GradClip, "echo_grad_clip", 5, "grads", "count", "max_norm", "norm", "workspace", "workspace_bytes", "stream");
+NAMES(ScanFwd, "echo_scan_fwd", 8, "desc", "G", "c0", "len", "h", "c_last", "states", "workspace", "workspace_bytes", "stream");
+NAMES(ScanBwd, "echo_scan_bwd", 9, "desc", "dh", "dc_last", "G", "len", "states", "dG", "dc0", "workspace", "workspace_bytes", "stream");
+NAMES(DistillFwd, "echo_distill_fwd", 10, "desc", "h", "W", "words", "logits", "K", "T", "loss", "lse", "workspace", "workspace_bytes",
+      "stream");
+NAMES(DistillBwd, "echo_distill_bwd", 12, "desc", "dloss", "lse", "h", "W", "words", "logits", "K", "T", "dh", "dW", "workspace",
+      "workspace_bytes", "stream");
+NAMES(DraftVerify, "echo_draft_verify", 10, "desc", "drafted", "n_drafted", "draft", "target", "u", "r", "tokens", "taken", "workspace",
+      "workspace_bytes", "stream");
 #undef NAMES
 
 Names *const kAll[] = {&Fwd::names, &Bwd::names, &BwdStatic::names, &BwdAccumulate::names, &StepFwd::names, &StepBwd::names,
                        &StepFinish::names, &StepBwdQuery::names, &StepsBwdKeys::names, &FwdStash::names, &BwdStash::names,
                        &DropoutFwd::names, &DropoutBwd::names, &LstmFwd::names, &LstmBwd::names, &LstmFwdStash::names,
                        &LstmBwdStash::names, &EmbedFwd::names, &EmbedBwd::names, &EmbedBwdAccumulate::names,
-                       &VocabLossFwd::names, &VocabLossBwd::names, &GradNorm::names, &GradClip::names};
+                       &VocabLossFwd::names, &VocabLossBwd::names, &GradNorm::names, &GradClip::names,
+                       &ScanFwd::names, &ScanBwd::names, &DistillFwd::names, &DistillBwd::names, &DraftVerify::names};
 
-// bind(desc_type, vocab_desc_type, grad_type, {name: address of the loaded library's function}): the names that are not in the dict raise when called
+// bind((desc_type, vocab_desc_type, grad_type, scan_desc_type, draft_desc_type), {name: address of the loaded library's function}): the names that are not in the dict raise when called
 PyObject *bind(PyObject *, PyObject *args) {
-    PyObject *type[3] = {}, *addresses = nullptr;
-    if (!PyArg_ParseTuple(args, "O!O!O!O!", &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2], &PyDict_Type, &addresses))
+    constexpr int TYPES = 5;
+    PyObject *type[TYPES] = {}, *addresses = nullptr;
+    if (!PyArg_ParseTuple(args, "(O!O!O!O!O!)O!", &PyType_Type, &type[0], &PyType_Type, &type[1], &PyType_Type, &type[2], &PyType_Type, &type[3],
+                          &PyType_Type, &type[4], &PyDict_Type, &addresses))
         return nullptr;
     for (Names *n : kAll) {
         PyObject *a = PyDict_GetItemString(addresses, n->fn);        // borrowed
@@ -397,8 +430,8 @@ PyObject *bind(PyObject *, PyObject *args) {
         if (a && !int_value(a, x)) return nullptr;
         n->target = reinterpret_cast<void *>(x);
     }
-    PyTypeObject **const to[3] = {&g_desc_type, &g_vocab_desc_type, &g_grad_type};
-    for (int i = 0; i < 3; ++i) {
+    PyTypeObject **const to[TYPES] = {&g_desc_type, &g_vocab_desc_type, &g_grad_type, &g_scan_desc_type, &g_draft_desc_type};
+    for (int i = 0; i < TYPES; ++i) {
         Py_INCREF(type[i]);
         Py_XDECREF(reinterpret_cast<PyObject *>(*to[i]));
         *to[i] = reinterpret_cast<PyTypeObject *>(type[i]);
@@ -412,7 +445,8 @@ PyMethodDef g_methods[] = {METHOD(Fwd), METHOD(Bwd), METHOD(BwdStatic), METHOD(B
                            METHOD(StepFinish), METHOD(StepBwdQuery), METHOD(StepsBwdKeys), METHOD(FwdStash), METHOD(BwdStash),
                            METHOD(DropoutFwd), METHOD(DropoutBwd), METHOD(LstmFwd), METHOD(LstmBwd), METHOD(LstmFwdStash),
                            METHOD(LstmBwdStash), METHOD(EmbedFwd), METHOD(EmbedBwd), METHOD(EmbedBwdAccumulate),
-                           METHOD(VocabLossFwd), METHOD(VocabLossBwd), METHOD(GradNorm), METHOD(GradClip), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                           METHOD(VocabLossFwd), METHOD(VocabLossBwd), METHOD(GradNorm), METHOD(GradClip), METHOD(ScanFwd),
+                           METHOD(ScanBwd), METHOD(DistillFwd), METHOD(DistillBwd), METHOD(DraftVerify), {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef METHOD
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_py_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -15,7 +15,7 @@
 // Measured (8192 rows x 100003 words x 2048, bf16): logits 2.5 ms (1340 TFLOP/s), logits and dz 3.25 (the stores of dz and of its turned form, 3.3 GB, are
 // not hidden: a compute unit holds one block), dW and dh 6.1 (1100: by the power limit; pieces whose tiles fill whole rounds gained nothing),
 // all else 0.4.  One of 3520 x 32000 x 1024 with f32 gradients: 0.23, 0.45, 0.88, 0.12.
-#include "../../include/echovocab.h"
+#include "../../include/echodistill.h"
 
 #include <hip/hip_runtime.h>
 
@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "distill.hpp"
 #include "kernels.hpp"
 #include "launch.hpp"
 #include "product.hpp"
@@ -350,6 +351,7 @@ struct LogitsArgs {
     const int *rows, *labels;
     int V, v0;                       // words of the vocabulary; this piece's first word
     float eps;                       // label smoothing
+    Teacher teacher;                 // in the place of labels
     // forward: [tiles][pitch] maximum, sum, sum of logits; the label's logit
     float *part_max, *part_sum, *part_z, *z_label;
     int first_tile;
@@ -370,7 +372,8 @@ __device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
     return from == to ? sum : sum * fast_exp2((from - to) * kLog2e);
 }
 
-template <class C, Mode MODE>
+// TEACHER: the target is a row's shares among the teacher's words (distill.hpp) instead of its label, and logits are divided by the temperature.
+template <class C, Mode MODE, bool TEACHER = false>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int count = a.count->count;
@@ -384,14 +387,34 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
     const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
+    typedef TeacherTile<C::TM * 16> Shares;
+    if constexpr (TEACHER) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) acc[i][j] *= a.teacher.inv_t;
+    }
     if constexpr (MODE == Mode::kForward) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
+        static_assert(3 * C::WM * C::BN * 4 + C::WAVES * Shares::BYTES <= C::LDS_BYTES, "room for the shares");
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int nt = (wn * C::TN + j) * 16 + (lane & 15), n = n0 + nt;
-            const int y = n < count ? a.labels[a.rows[n]] - vw : -1;
+            const int y = !TEACHER && n < count ? a.labels[a.rows[n]] - vw : -1;
             float z = 0.f;
-            if (a.eps > 0.f) {
+            if constexpr (TEACHER) {
+                shares.put(n < count ? a.rows[n] : -1);
+#pragma unroll
+                for (int i = 0; i < C::TM; ++i) {
+                    const f32x4 q = shares.get(i * 16 + lr);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z += q[r] != 0.f ? q[r] * acc[i][j][r] : 0.f;      // a logit of a word past the end may be anything
+                }
+                shares.clear();
+                z += __shfl_xor(z, 16);
+                z += __shfl_xor(z, 32);
+            } else if (a.eps > 0.f) {
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -399,7 +422,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 z += __shfl_xor(z, 16);
                 z += __shfl_xor(z, 32);
             }
-            if (__ballot(y >= 0 && y < C::TM * 16 && y % 16 < 4)) {   // the label's logit: the lane that holds it writes it and leaves it out of maximum and sum
+            if (!TEACHER && __ballot(y >= 0 && y < C::TM * 16 && y % 16 < 4)) {   // the label's logit: the lane that holds it writes it and leaves it out of maximum and sum
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -451,7 +474,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
             const size_t at = (size_t)(a.first_tile + im) * a.pitch + n0 + nt;
             a.part_max[at] = top;
             a.part_sum[at] = sum;
-            if (a.eps > 0.f) a.part_z[at] = z;
+            if (TEACHER || a.eps > 0.f) a.part_z[at] = z;
         }
     } else {
         const float off = 1.0f - a.eps, low = a.eps / (float)a.V;
@@ -462,25 +485,34 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 for (int i = 0; i < C::TM; ++i)
                     if (n0 + (wn * C::TN + j) * 16 + (lane & 15) >= count) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds), vw - lr, TEACHER);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
             const bool row = n < count;
             const int at = row ? a.rows[n] : 0;
-            const int y = row ? a.labels[at] - vw : -1;
+            const int y = !TEACHER && row ? a.labels[at] - vw : -1;
+            if constexpr (TEACHER) shares.put(row ? at : -1);
             const float lse = row ? a.lse[at] : 0.f, g = !row ? 0.f : half_of(MODE) ? 0x1p15f : a.dloss[at] * kDzScale;
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i)
+            for (int i = 0; i < C::TM; ++i) {
+                f32x4 q;
+                if constexpr (TEACHER) q = shares.get(i * 16 + lr);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int v = i * 16 + r;
                     // a probability: a logit of a million has an error of one half, and what that makes of it must not leave fp16
-                    const float e = fast_exp2((acc[i][j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (v == y ? off + low : low);
+                    const float e = fast_exp2((acc[i][j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (TEACHER ? q[r] : v == y ? off + low : low);
                     float x = vw + v < a.V ? p * g : 0.f;
-                    if constexpr (MODE == Mode::kHalves) asm("" : "+v"(x));       // rounded to fp32 for both planes alike: see below
+                    // kHalves: rounded to fp32 for both planes alike, see below.  TEACHER: computed here, between the shares' way into LDS and out of it
+                    // (put off to the stores, it takes more registers than there are)
+                    if constexpr (MODE == Mode::kHalves || TEACHER) asm("" : "+v"(x));
                     acc[i][j][r] = x;
                 }
+            }
+            if constexpr (TEACHER) shares.clear();
         }
+        if constexpr (TEACHER) lds_barrier();                                  // the shares' place is the other waves' for dz
         // dz passes through LDS a plane at a time, [row][word]: each lane writes four words of a row; whole rows leave for dz, and read
         // with the transposing load 16 words x 32 rows leave for its turned form
         constexpr int PITCH = C::BM * 2 + 16;                                  // bytes; 16 more per row spread the rows over the banks
@@ -732,6 +764,7 @@ struct FewArgs {
     bf16_t *dz, *turned;
     size_t dz_plane, turned_plane;
     int dz_pitch, turned_pitch;
+    Teacher teacher;
 };
 
 // 16 rows x 32 k of a matrix as an operand: as loaded (lane l: row l % 16, k = 8 (l / 16) .. + 7), and as planes
@@ -776,20 +809,25 @@ template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 
 }
 
 // The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
-template <int NT, int WAVES>
+template <int NT, int WAVES, bool TEACHER>
 __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z) {
     constexpr int ROWS = 16 * NT;
     const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int n = 16 * j + (lane & 15), y = n < a.N ? a.labels[n] - vw : -1;
+        const int n = 16 * j + (lane & 15), y = !TEACHER && n < a.N ? a.labels[n] - vw : -1;
+        f32x4 q = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (TEACHER) {
+            acc[j] *= a.teacher.inv_t;
+            q = teacher_shares(a.teacher, n < a.N ? n : -1, vw);
+        }
         float z = 0.f, top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             if (vw + r >= a.V) {
                 acc[j][r] = -__builtin_inff();
             } else {
-                z += acc[j][r];
+                z += !TEACHER ? acc[j][r] : q[r] != 0.f ? q[r] * acc[j][r] : 0.f;
                 if (y == r) {                                                  // the label's logit is left out of maximum and sum
                     a.z_label[n] = acc[j][r];
                     acc[j][r] = -__builtin_inff();
@@ -826,7 +864,7 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
 }
 
 // dz of the same: few enough to be stored as the lanes hold it.  Rows n0 .. n0 + a.N, and zeros up to a multiple of 8 and for words past the end
-template <int NT> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0) {
+template <int NT, bool TEACHER> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0) {
     const int lane = lane_id(), vw = v0 + 4 * (lane >> 4);
     const float low = a.eps / (float)a.all_words, off = 1.0f - a.eps;
 #pragma unroll
@@ -834,12 +872,17 @@ template <int NT> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4
         const int n = 16 * j + (lane & 15);
         if (n >= (a.N + 7) / 8 * 8) continue;
         const bool row = n < a.N;
-        const int at = a.rows[min(n, a.N - 1)], y = a.labels[at] - a.v0 - vw;
+        const int at = a.rows[min(n, a.N - 1)], y = TEACHER ? -1 : a.labels[at] - a.v0 - vw;
+        f32x4 q = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (TEACHER) {
+            acc[j] *= a.teacher.inv_t;
+            q = teacher_shares(a.teacher, row ? at : -1, a.v0 + vw);
+        }
         const float lse = a.lse[at], g = a.dloss[at] * kDzScale;
         f32x4 x;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float e = fast_exp2((acc[j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (r == y ? off + low : low);
+            const float e = fast_exp2((acc[j][r] - lse) * kLog2e), p = (e > 1.f ? 1.f : e) - (TEACHER ? q[r] : r == y ? off + low : low);
             x[r] = row && vw + r < a.V ? p * g : 0.f;
         }
 #pragma unroll
@@ -861,7 +904,7 @@ template <int NT> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4
 }
 
 // AHEAD: how many times 32 k are on their way.
-template <typename T, int AHEAD>
+template <typename T, int AHEAD, bool TEACHER>
 __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
     constexpr int PLANES = FewFragment<T>::PLANES;
     __shared__ float s_max[64], s_sum[64], s_z[64];
@@ -891,14 +934,14 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
             if (t0 + d + AHEAD < steps) fetch(d, t0 + d + AHEAD);
             acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
         }
-    few_join<1, 4>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z);
+    few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z);
 }
 
 // 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
 // A row takes 256 bytes of LDS, its groups of 16 bytes in the order c ^ (row % 16): the 16 rows of a fragment take all banks, whichever of its lanes are
 // served together (16 more bytes a row instead: 41 % of the LDS time went to conflicts).
 constexpr int kFewK = 128, kFewPitch = kFewK * 2;
-template <typename T, int NT, bool BWD>
+template <typename T, int NT, bool BWD, bool TEACHER>
 __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     constexpr int PLANES = FewFragment<T>::PLANES, SUB = kFewK / 32, ROWS = 16 * NT, WAVES = 8;
     constexpr int GROUPS = ROWS * kFewK / 8, ITEMS = (GROUPS + 64 * WAVES - 1) / (64 * WAVES);      // groups of 8 numbers of the rows, per thread
@@ -915,8 +958,12 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     } else {
         a.N = min(ROWS, all.N - n0);
         a.h = static_cast<const T *>(all.h) + (size_t)n0 * all.D;
-        a.labels += n0;
-        a.z_label += n0;
+        if constexpr (TEACHER) {
+            a.teacher.from_row(n0);
+        } else {
+            a.labels += n0;
+            a.z_label += n0;
+        }
         a.part_max += (size_t)n0 * all.tiles;
         a.part_sum += (size_t)n0 * all.tiles;
         a.part_z += (size_t)n0 * all.tiles;
@@ -992,8 +1039,8 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
         step(t, fw[0]);
         if (t + 1 < steps) step(t + 1, fw[1]);
     }
-    if constexpr (BWD) few_dz<NT>(a, acc, n0, v0);
-    else few_join<NT, WAVES>(a, acc, tile, v0, s_max, s_sum, s_z);
+    if constexpr (BWD) few_dz<NT, TEACHER>(a, acc, n0, v0);
+    else few_join<NT, WAVES, TEACHER>(a, acc, tile, v0, s_max, s_sum, s_z);
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
@@ -1008,7 +1055,14 @@ __device__ __forceinline__ void loss_of_row(float top, float sum, float z, float
     if (eps > 0.f) loss += eps * (zl - z / (float)V);
 }
 
+// The same against a teacher: z is the sum of the logits by their shares, `own` the sum of share log share.
+__device__ __forceinline__ void loss_of_row(float top, float sum, float z, const Teacher &t, int n, float &loss, float &lse) {
+    lse = top + logf(sum);
+    loss = t.temperature * t.temperature * (t.own[n] + (lse - z));
+}
+
 // A block per row.
+template <bool TEACHER>
 __global__ __launch_bounds__(256) void k_vocab_few_finish(const FewArgs a, float *__restrict__ loss, float *__restrict__ lse) {
     __shared__ float s_max[4], s_sum[4], s_z[4];
     const int n = blockIdx.x, lane = lane_id(), w = wave_id(), y = a.labels[n];
@@ -1043,14 +1097,16 @@ __global__ __launch_bounds__(256) void k_vocab_few_finish(const FewArgs a, float
     sum = 0.f, z = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum += scaled_sum(s_sum[k], s_max[k], top), z += s_z[k];
-    loss_of_row(top, sum, z, a.z_label[n], a.V, a.eps, loss[n], lse[n]);
+    if constexpr (TEACHER) loss_of_row(top, sum, z, a.teacher, n, loss[n], lse[n]);
+    else loss_of_row(top, sum, z, a.z_label[n], a.V, a.eps, loss[n], lse[n]);
 }
 
 // Joins the tiles of 64 rows: four waves take a quarter of the tiles each, lanes are rows.  Rows without a label get zeros.
+template <bool TEACHER>
 __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restrict__ part_max, const float *__restrict__ part_sum,
                                                            const float *__restrict__ part_z, const float *__restrict__ z_label,
                                                            const int *__restrict__ place, int N, int V, int tiles, size_t pitch,
-                                                           float eps, float *__restrict__ loss, float *__restrict__ lse) {
+                                                           float eps, const Teacher teacher, float *__restrict__ loss, float *__restrict__ lse) {
     __shared__ float s_max[4][64], s_sum[4][64], s_z[4][64];
     const int lane = lane_id(), w = wave_id(), n = blockIdx.x * 64 + lane, p = n < N ? place[n] : -1;
     const int share = (tiles + 3) / 4, t0 = w * share, t1 = min(tiles, t0 + share);
@@ -1063,7 +1119,7 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
                 const size_t at = (size_t)min(t + u, t1 - 1) * pitch + p;
                 m[u] = part_max[at];
                 s[u] = part_sum[at];
-                zz[u] = eps > 0.f ? part_z[at] : 0.f;
+                zz[u] = TEACHER || eps > 0.f ? part_z[at] : 0.f;
             }
             float next = top;
 #pragma unroll
@@ -1093,7 +1149,8 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
             sum += scaled_sum(s_sum[k][lane], s_max[k][lane], all);
             z += s_z[k][lane];
         }
-        loss_of_row(all, sum, z, z_label[p], V, eps, l, e);
+        if constexpr (TEACHER) loss_of_row(all, sum, z, teacher, n, l, e);
+        else loss_of_row(all, sum, z, z_label[p], V, eps, l, e);
     }
     loss[n] = l;
     lse[n] = e;
@@ -1383,23 +1440,23 @@ static echo_status_t launch_tiles(const char *name, K *kernel, LdsGrants &grante
     return launch_end(r);
 }
 
-template <typename T> static void launch_few(const FewArgs &a, hipStream_t st) {
-    if (a.N <= kFewAlone) k_vocab_few_alone<T, sizeof(T) == 2 ? 8 : 6><<<a.tiles, 256, 0, st>>>(a);
-    else if (a.N <= 32) k_vocab_few_shared<T, 2, false><<<a.tiles, 512, 0, st>>>(a);
-    else k_vocab_few_shared<T, 4, false><<<a.tiles * a.groups, 512, 0, st>>>(a);
+template <typename T, bool TEACHER> static void launch_few(const FewArgs &a, hipStream_t st) {
+    if (a.N <= kFewAlone) k_vocab_few_alone<T, sizeof(T) == 2 ? 8 : 6, TEACHER><<<a.tiles, 256, 0, st>>>(a);
+    else if (a.N <= 32) k_vocab_few_shared<T, 2, false, TEACHER><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<T, 4, false, TEACHER><<<a.tiles * a.groups, 512, 0, st>>>(a);
 }
-static echo_status_t launch_few_dz(const FewArgs &a, hipStream_t st) {
+template <bool TEACHER> static echo_status_t launch_few_dz(const FewArgs &a, hipStream_t st) {
     LaunchRecord r = launch_begin("vocab_few_dz", st);
-    if (a.N <= 32) k_vocab_few_shared<float, 2, true><<<a.tiles, 512, 0, st>>>(a);
-    else k_vocab_few_shared<float, 4, true><<<a.tiles * a.groups, 512, 0, st>>>(a);
+    if (a.N <= 32) k_vocab_few_shared<float, 2, true, TEACHER><<<a.tiles, 512, 0, st>>>(a);
+    else k_vocab_few_shared<float, 4, true, TEACHER><<<a.tiles * a.groups, 512, 0, st>>>(a);
     return launch_end(r);
 }
-template <class C, Mode MODE> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
+template <class C, Mode MODE, bool TEACHER> static echo_status_t launch_logits(const LogitsArgs &a, int N, hipStream_t st) {
     static LdsGrants granted{};
     const long long blocks = (long long)((a.W.rows + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
     constexpr bool BWD = MODE != Mode::kForward;
     constexpr const char *name = C::BM == 256 ? (BWD ? "vocab_dlogits_256" : "vocab_logits_256") : (BWD ? "vocab_dlogits_128" : "vocab_logits_128");
-    return launch_tiles(name, &k_vocab_logits<C, MODE>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
+    return launch_tiles(name, &k_vocab_logits<C, MODE, TEACHER>, granted, BWD ? product_lds<C>() : (size_t)C::LDS_BYTES, blocks,
                         C::THREADS, a, st);
 }
 template <class C, Mode MODE> static echo_status_t launch_grads(const GradsArgs &a, const CutArgs &cut, int N, hipStream_t st) {
@@ -1490,42 +1547,24 @@ static FewArgs few_dz_args(const VocabRun &x, const LogitsArgs &a, int n) {
     f.dz = a.dz, f.turned = a.turned;
     f.dz_plane = a.dz_plane, f.turned_plane = a.turned_plane;
     f.dz_pitch = a.dz_pitch, f.turned_pitch = a.turned_pitch;
+    f.teacher = a.teacher;
     return f;
 }
 
-}  // namespace echo
-
-extern "C" {
-
-size_t echo_vocab_loss_fwd_workspace_bytes(const echo_vocab_desc_t *desc) {
-    if (echo::check_vocab(desc, 0.f)) return 0;
-    return echo::vocab_plan(*desc, false).total;
-}
-
-size_t echo_vocab_loss_bwd_workspace_bytes(const echo_vocab_desc_t *desc) {
-    if (echo::check_vocab(desc, 0.f)) return 0;
-    return echo::vocab_plan(*desc, true).total;
-}
-
-echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, const void *W, const int32_t *labels,
-                                  float label_smoothing, float *loss, float *lse, void *workspace, size_t workspace_bytes,
-                                  void *stream) {
-    using namespace echo;
-    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
-    if (!h || !W || !labels || !loss || !lse || !workspace) return ECHO_ERR_NULL;
-    if (unaligned({h, W, labels, loss, lse, workspace})) return ECHO_ERR_ALIGN;
-    const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
-    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
-    const int N = desc->N, V = desc->V;
+// TEACHER: x.labels holds a word of every row that takes part, which is what the rows are gathered by; eps is 0
+template <bool TEACHER>
+static echo_status_t run_forward(const VocabRun &x, float eps, const Teacher &teacher, float *loss, float *lse) {
+    const int N = x.d.N, V = x.d.V;
     if (x.p.few) {
-        const FewArgs a{h, W, labels, N, V, desc->D, x.p.tiles, (N + kFewGroup - 1) / kFewGroup, label_smoothing, x.at<float>(x.p.part_max), x.at<float>(x.p.part_sum),
+        FewArgs a{x.h, x.W, x.labels, N, V, x.d.D, x.p.tiles, (N + kFewGroup - 1) / kFewGroup, eps, x.at<float>(x.p.part_max), x.at<float>(x.p.part_sum),
                         x.at<float>(x.p.part_z), x.at<float>(x.p.z_label)};
+        a.teacher = teacher;
         LaunchRecord r = launch_begin("vocab_few", x.st);
-        if (desc->in_dtype == ECHO_F32) launch_few<float>(a, x.st);
-        else launch_few<bf16_t>(a, x.st);
+        if (x.d.in_dtype == ECHO_F32) launch_few<float, TEACHER>(a, x.st);
+        else launch_few<bf16_t, TEACHER>(a, x.st);
         if (echo_status_t s = launch_end(r)) return s;
         r = launch_begin("vocab_few_finish", x.st);
-        k_vocab_few_finish<<<N, 256, 0, x.st>>>(a, loss, lse);
+        k_vocab_few_finish<TEACHER><<<N, 256, 0, x.st>>>(a, loss, lse);
         return launch_end(r);
     }
     if (echo_status_t s = x.gather(false, CutArgs{}, LargestArgs{})) return s;
@@ -1535,9 +1574,10 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
     a.pairs = pairs_of(x.p.planes, x.p.planes);
     a.count = x.at<Rows>(x.p.count);
     a.rows = x.at<int>(x.p.rows);
-    a.labels = labels;
+    a.labels = x.labels;
     a.V = V;
-    a.eps = label_smoothing;
+    a.eps = eps;
+    a.teacher = teacher;
     a.part_max = x.at<float>(x.p.part_max);
     a.part_sum = x.at<float>(x.p.part_sum);
     a.part_z = x.at<float>(x.p.part_z);
@@ -1550,28 +1590,21 @@ echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, 
         if (echo_status_t s = x.words(v0, n, false, a.W)) return s;
         a.v0 = v0;
         a.first_tile = tiles;
-        if (echo_status_t s = big ? launch_logits<BigTile, Mode::kForward>(a, N, x.st) : launch_logits<MidTile, Mode::kForward>(a, N, x.st)) return s;
+        if (echo_status_t s = big ? launch_logits<BigTile, Mode::kForward, TEACHER>(a, N, x.st) : launch_logits<MidTile, Mode::kForward, TEACHER>(a, N, x.st)) return s;
         tiles += big ? (n + 255) / 256 : (n + 127) / 128;
     }
     LaunchRecord r = launch_begin("vocab_loss_finish", x.st);
-    k_vocab_loss_finish<<<(N + 63) / 64, 256, 0, x.st>>>(a.part_max, a.part_sum, a.part_z, a.z_label, x.at<int>(x.p.place), N, V, tiles, a.pitch,
-                                                         label_smoothing, loss, lse);
+    k_vocab_loss_finish<TEACHER><<<(N + 63) / 64, 256, 0, x.st>>>(a.part_max, a.part_sum, a.part_z, a.z_label, x.at<int>(x.p.place), N, V, tiles, a.pitch,
+                                                                  eps, teacher, loss, lse);
     return launch_end(r);
 }
 
-echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dloss, const float *lse, const void *h, const void *W,
-                                  const int32_t *labels, float label_smoothing, void *dh, void *dW, void *workspace,
-                                  size_t workspace_bytes, void *stream) {
-    using namespace echo;
-    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
-    if (!dloss || !lse || !h || !W || !labels || (!dh && !dW) || !workspace) return ECHO_ERR_NULL;
-    if (unaligned({dloss, lse, h, W, labels, dh, dW, workspace})) return ECHO_ERR_ALIGN;
-    const VocabRun x{*desc, vocab_plan(*desc, true), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
-    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
-    const int N = desc->N, V = desc->V, D = desc->D;
+template <bool TEACHER>
+static echo_status_t run_backward(const VocabRun &x, float eps, const Teacher &teacher, const float *dloss, const float *lse, void *dh, void *dW) {
+    const int N = x.d.N, V = x.d.V, D = x.d.D;
     const VocabPlan &p = x.p;
     LargestArgs l{};
-    if (x.half()) l = LargestArgs{dW ? static_cast<const bf16_t *>(h) : nullptr, dh ? static_cast<const bf16_t *>(W) : nullptr, dloss, labels, N, V, D};
+    if (x.half()) l = LargestArgs{dW ? static_cast<const bf16_t *>(x.h) : nullptr, dh ? static_cast<const bf16_t *>(x.W) : nullptr, dloss, x.labels, N, V, D};
     if (echo_status_t s = x.gather(dW != nullptr, x.p.cut, l)) return s;
     LogitsArgs a{};
     a.h = x.rows();
@@ -1579,9 +1612,10 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     a.pairs = pairs_of(p.planes, p.planes);
     a.count = x.at<Rows>(p.count);
     a.rows = x.at<int>(p.rows);
-    a.labels = labels;
+    a.labels = x.labels;
     a.V = V;
-    a.eps = label_smoothing;
+    a.eps = eps;
+    a.teacher = teacher;
     a.lse = lse;
     a.dloss = dloss;
     a.dz = dh ? x.at<bf16_t>(p.dz) : nullptr;
@@ -1602,7 +1636,7 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     g.dw_part = (size_t)p.piece * D;
     g.dh_sum = dh ? x.at<float>(p.dh) : nullptr;
     g.dh_part = (size_t)N * D;
-    const bool bf16_out = desc->out_dtype == ECHO_BF16;
+    const bool bf16_out = x.d.out_dtype == ECHO_BF16;
     const size_t out_bytes = bf16_out ? 2 : 4;
     const bool big = big_logits(std::min(p.piece, V), N);
     const int row_tile = big ? 256 : 128, row_tiles = (N + row_tile - 1) / row_tile;
@@ -1612,10 +1646,10 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
         if (echo_status_t s = x.words(v0, n, dh != nullptr, a.W)) return s;
         a.v0 = v0;
         echo_status_t s;
-        if (p.few) s = launch_few_dz(few_dz_args(x, a, n), x.st);
-        else if (!x.half()) s = big ? launch_logits<BigTile, Mode::kPlanes>(a, N, x.st) : launch_logits<MidTile, Mode::kPlanes>(a, N, x.st);
-        else if (bf16_out) s = big ? launch_logits<BigTile, Mode::kHalf>(a, N, x.st) : launch_logits<MidTile, Mode::kHalf>(a, N, x.st);
-        else s = big ? launch_logits<BigTile, Mode::kHalves>(a, N, x.st) : launch_logits<MidTile, Mode::kHalves>(a, N, x.st);
+        if (p.few) s = launch_few_dz<TEACHER>(few_dz_args(x, a, n), x.st);
+        else if (!x.half()) s = big ? launch_logits<BigTile, Mode::kPlanes, TEACHER>(a, N, x.st) : launch_logits<MidTile, Mode::kPlanes, TEACHER>(a, N, x.st);
+        else if (bf16_out) s = big ? launch_logits<BigTile, Mode::kHalf, TEACHER>(a, N, x.st) : launch_logits<MidTile, Mode::kHalf, TEACHER>(a, N, x.st);
+        else s = big ? launch_logits<BigTile, Mode::kHalves, TEACHER>(a, N, x.st) : launch_logits<MidTile, Mode::kHalves, TEACHER>(a, N, x.st);
         if (s) return s;
         if (dW && x.half() && row_tiles > 1) {
             LaunchRecord r = launch_begin("vocab_level", x.st);
@@ -1644,6 +1678,128 @@ echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dl
     if (bf16_out) k_vocab_dh_finish<<<dim3((N + 3) / 4, (D + 255) / 256), 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<bf16_t *>(dh));
     else k_vocab_dh_finish<<<dim3((N + 3) / 4, (D + 255) / 256), 256, 0, x.st>>>(g.rows, x.half(), g.dh_sum, g.dh_part, x.at<int>(p.place), dloss, N, D, static_cast<float *>(dh));
     return launch_end(r);
+}
+
+// ---- distillation: the workspace of the loss, and behind it what the teacher's lists are made into ---------------------------
+struct TeacherPlan {
+    int marks;
+    size_t labels, own, dloss, words, shares, start, total;
+};
+static TeacherPlan teacher_plan(const echo_vocab_desc_t &d, int K, size_t at) {
+    TeacherPlan p{};
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes, 256);
+        return here;
+    };
+    const size_t N = d.N;
+    p.marks = (d.V + kMarkWords - 1) / kMarkWords + 1;
+    p.labels = take(N * 4);
+    p.own = take(N * 4);
+    p.dloss = take(N * 4);
+    p.words = take(N * K * 4);
+    p.shares = take(N * K * 4);
+    p.start = take(N * p.marks);
+    p.total = at;
+    return p;
+}
+static echo_status_t check_distill(const echo_vocab_desc_t *d, int K, float T) {
+    if (echo_status_t s = check_vocab(d, 0.f)) return s;
+    return K < 1 || K > ECHO_DISTILL_MAX_K || !(T >= 0x1p-64f && T <= 0x1p64f) ? ECHO_ERR_SHAPE : ECHO_OK;
+}
+// the lists, sorted, and the run that works on them
+static echo_status_t distill_begin(VocabRun &x, const TeacherPlan &p, const int *words, const float *logits, int K, float T, const float *dloss,
+                                   Teacher &teacher) {
+    TeacherLists l{};
+    l.words = words, l.logits = logits, l.dloss = dloss;
+    l.N = x.d.N, l.V = x.d.V, l.K = K, l.marks = p.marks;
+    l.temperature = T;
+    l.labels = x.at<int>(p.labels);
+    l.own = x.at<float>(p.own);
+    l.dloss_out = x.at<float>(p.dloss);
+    l.words_out = x.at<int>(p.words);
+    l.shares = x.at<float>(p.shares);
+    l.start = x.at<unsigned char>(p.start);
+    x.labels = l.labels;
+    teacher = Teacher{l.words_out, l.shares, l.start, l.own, K, p.marks, 1.f / T, T};
+    return launch_teacher_lists(l, x.st);
+}
+
+}  // namespace echo
+
+extern "C" {
+
+size_t echo_vocab_loss_fwd_workspace_bytes(const echo_vocab_desc_t *desc) {
+    if (echo::check_vocab(desc, 0.f)) return 0;
+    return echo::vocab_plan(*desc, false).total;
+}
+
+size_t echo_vocab_loss_bwd_workspace_bytes(const echo_vocab_desc_t *desc) {
+    if (echo::check_vocab(desc, 0.f)) return 0;
+    return echo::vocab_plan(*desc, true).total;
+}
+
+echo_status_t echo_vocab_loss_fwd(const echo_vocab_desc_t *desc, const void *h, const void *W, const int32_t *labels,
+                                  float label_smoothing, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                                  void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
+    if (!h || !W || !labels || !loss || !lse || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({h, W, labels, loss, lse, workspace})) return ECHO_ERR_ALIGN;
+    const VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
+    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
+    return run_forward<false>(x, label_smoothing, Teacher{}, loss, lse);
+}
+
+echo_status_t echo_vocab_loss_bwd(const echo_vocab_desc_t *desc, const float *dloss, const float *lse, const void *h, const void *W,
+                                  const int32_t *labels, float label_smoothing, void *dh, void *dW, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_vocab(desc, label_smoothing)) return s;
+    if (!dloss || !lse || !h || !W || !labels || (!dh && !dW) || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({dloss, lse, h, W, labels, dh, dW, workspace})) return ECHO_ERR_ALIGN;
+    const VocabRun x{*desc, vocab_plan(*desc, true), static_cast<char *>(workspace), h, W, labels, static_cast<hipStream_t>(stream)};
+    if (workspace_bytes < x.p.total) return ECHO_ERR_WORKSPACE;
+    return run_backward<false>(x, label_smoothing, Teacher{}, dloss, lse, dh, dW);
+}
+
+size_t echo_distill_fwd_workspace_bytes(const echo_vocab_desc_t *desc, int32_t K) {
+    if (echo::check_distill(desc, K, 1.f)) return 0;
+    return echo::teacher_plan(*desc, K, echo::vocab_plan(*desc, false).total).total;
+}
+
+size_t echo_distill_bwd_workspace_bytes(const echo_vocab_desc_t *desc, int32_t K) {
+    if (echo::check_distill(desc, K, 1.f)) return 0;
+    return echo::teacher_plan(*desc, K, echo::vocab_plan(*desc, true).total).total;
+}
+
+echo_status_t echo_distill_fwd(const echo_vocab_desc_t *desc, const void *h, const void *W, const int32_t *words, const float *logits,
+                               int32_t K, float T, float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_distill(desc, K, T)) return s;
+    if (!h || !W || !words || !logits || !loss || !lse || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({h, W, words, logits, loss, lse, workspace})) return ECHO_ERR_ALIGN;
+    VocabRun x{*desc, vocab_plan(*desc, false), static_cast<char *>(workspace), h, W, nullptr, static_cast<hipStream_t>(stream)};
+    const TeacherPlan p = teacher_plan(*desc, K, x.p.total);
+    if (workspace_bytes < p.total) return ECHO_ERR_WORKSPACE;
+    Teacher teacher;
+    if (echo_status_t s = distill_begin(x, p, words, logits, K, T, nullptr, teacher)) return s;
+    return run_forward<true>(x, 0.f, teacher, loss, lse);
+}
+
+echo_status_t echo_distill_bwd(const echo_vocab_desc_t *desc, const float *dloss, const float *lse, const void *h, const void *W,
+                               const int32_t *words, const float *logits, int32_t K, float T, void *dh, void *dW, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    using namespace echo;
+    if (echo_status_t s = check_distill(desc, K, T)) return s;
+    if (!dloss || !lse || !h || !W || !words || !logits || (!dh && !dW) || !workspace) return ECHO_ERR_NULL;
+    if (unaligned({dloss, lse, h, W, words, logits, dh, dW, workspace})) return ECHO_ERR_ALIGN;
+    VocabRun x{*desc, vocab_plan(*desc, true), static_cast<char *>(workspace), h, W, nullptr, static_cast<hipStream_t>(stream)};
+    const TeacherPlan p = teacher_plan(*desc, K, x.p.total);
+    if (workspace_bytes < p.total) return ECHO_ERR_WORKSPACE;
+    Teacher teacher;
+    if (echo_status_t s = distill_begin(x, p, words, logits, K, T, dloss, teacher)) return s;
+    return run_backward<true>(x, 0.f, teacher, x.at<float>(p.dloss), lse, dh, dW);
 }
 
 }  // extern "C"
