@@ -10,6 +10,9 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -42,6 +45,7 @@ template <typename T> struct Lanes<T, 1> {
     __device__ __forceinline__ void load(const T *p) { raw = RawElem<T>::load(p, 0); }
     __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = RawElem<T>::value(raw); }
 };
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16_hw;
 __device__ __forceinline__ unsigned bf16_bits(float x) { return __builtin_bit_cast(unsigned short, (bf16_hw)x); }
 __device__ __forceinline__ void put_one(float *p, float x) { *p = x; }
@@ -72,172 +76,302 @@ struct ScanArgs {
     const float *first;              // c0; dc_last
     const int *len;
     int B, T, H, reverse, chunks, groups_h;   // groups_h: units along the channels
-    long long units;                 // B groups_h
+    long long chains, units;         // B groups_h; chains by chunks
     void *out;                       // h; dG
     float *last;                     // c_last; dc0
     float *states;
+    unsigned long long *words, *ticket;       // [units][3][WIDTH]; the next unit to be taken
 };
 
-// What a thread is
+// What a thread is in a unit
 template <int VEC, int GROUPS> struct Place {
     static constexpr int SUBS = kScanThreads / 16 / GROUPS, WIDTH = 16 * VEC;
-    int lane16, group, sub, b, ch, slot;
-    int skip;                        // of its VEC channels, those in front that are the neighbour's
+    int group, sub, slot, b, base, ch, skip, chunk, s0;    // skip: of its VEC channels, those in front that are the neighbour's
     bool on;                         // it has channels of its own
     int n;                           // steps of the sequence
-    __device__ __forceinline__ Place(const ScanArgs &a) {
-        lane16 = threadIdx.x & 15;
+    long long chain;
+    __device__ __forceinline__ Place(const ScanArgs &a, long long unit, int chunk_) : chunk(chunk_) {
+        const int lane16 = threadIdx.x & 15;
         group = (threadIdx.x >> 4) % GROUPS;
         sub = (threadIdx.x >> 4) / GROUPS;
-        const long long unit = (long long)blockIdx.x * SUBS + sub, u = unit < a.units ? unit : a.units - 1;
-        b = (int)(u / a.groups_h);
-        const int c = (int)(u - (long long)b * a.groups_h) * WIDTH + lane16 * VEC;
-        on = unit < a.units && c < a.H;
-        ch = min(c, a.H - VEC);                            // the last lane steps back to a whole group of channels
-        skip = c - ch;
+        chain = min(unit + sub, a.chains - 1);
+        b = (int)(chain / a.groups_h);
+        base = (int)(chain - (long long)b * a.groups_h) * WIDTH;
         slot = lane16 * VEC;
+        on = unit + sub < a.chains && base + slot < a.H;
+        ch = min(base + slot, a.H - VEC);                  // the last lane steps back to a whole group of channels
+        skip = base + slot - ch;
         n = a.len ? clamp_len(a.len[b], a.T) : a.T;
+        s0 = (chunk * GROUPS + group) * kSteps;
     }
-    // position of step s; steps from n on stand at their own number
-    __device__ __forceinline__ int position(const ScanArgs &a, int s) const { return a.reverse && s < n ? n - 1 - s : s; }
+    __device__ __forceinline__ bool in(int i) const { return s0 + i < n; }
+    // position of the thread's step i; steps from n on stand at their own number
+    __device__ __forceinline__ int position(const ScanArgs &a, int i) const { return a.reverse && in(i) ? n - 1 - s0 - i : s0 + i; }
 };
 
-template <typename T, int VEC, int GROUPS>
-__global__ __launch_bounds__(kScanThreads) void k_scan_fwd(const ScanArgs a) {
+// What a lane is where a wave folds the maps of unit w: a channel each
+template <int VEC, int GROUPS> struct Folder {
     typedef Place<VEC, GROUPS> P;
-    __shared__ float s_a[GROUPS > 1 ? P::SUBS : 1][GROUPS][P::WIDTH], s_b[GROUPS > 1 ? P::SUBS : 1][GROUPS][P::WIDTH];
-    const P p(a);
-    const size_t row = (size_t)p.b * a.T;
-    const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
-    T *h = static_cast<T *>(a.out) + row * a.H + p.ch;
-    float carry[VEC];                                      // the state in front of the chunk: of every thread's own channels
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) carry[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
-    for (int chunk = 0; chunk < a.chunks; ++chunk) {
-        const int s0 = chunk * GROUPS * kSteps + p.group * kSteps;
-        if (a.states && p.group == 0 && p.on) {
-#pragma unroll
-            for (int v = 0; v < VEC; ++v)
-                if (v >= p.skip) a.states[((size_t)p.b * a.chunks + chunk) * a.H + p.ch + v] = carry[v];
+    int lane, ch;
+    bool on, own;
+    size_t row, state;               // of c0 and c_last; of the kept states
+    long long chain;
+    __device__ __forceinline__ Folder(const ScanArgs &a, long long unit, int w, int chunk) {
+        lane = lane_id();
+        chain = min(unit + w, a.chains - 1);
+        const int b = (int)(chain / a.groups_h), c = (int)(chain - (long long)b * a.groups_h) * P::WIDTH + lane / VEC * VEC;
+        on = w < P::SUBS && lane < P::WIDTH;
+        ch = max(0, min(c, a.H - VEC)) + lane % VEC;
+        own = on && unit + w < a.chains && c < a.H && ch >= c;
+        row = (size_t)b * a.H + ch;
+        state = ((size_t)b * a.chunks + chunk) * a.H + ch;
+    }
+};
+
+// ---- chains ---------------------------------------------------------------------------------------------------------------
+// The chunks of a sequence's channels are a chain: each hands the state behind it to the next.  A chunk publishes its map (A, b) as soon as it has it, and the
+// state behind it (C) as soon as it knows the one in front of it; the next one takes C from the chunk in front, or from one up to kLookBack in front and applies
+// the maps of those between, in order, with the same operation that each of them applies to its own: results do not depend on how far it looked.
+// A value goes out in one 64-bit word with a mark, so that nothing has to be waited for in between; the words are cleared in front of the launch.
+// Units are taken by ticket, chunk after chunk: whoever waits, waits for a unit that has been taken already and waits for lower tickets only.
+constexpr unsigned kMark = 1;
+__device__ __forceinline__ unsigned long long marked(float x) { return (unsigned long long)kMark << 32 | __float_as_uint(x); }
+__device__ __forceinline__ bool is_marked(unsigned long long w) { return (unsigned)(w >> 32) == kMark; }
+__device__ __forceinline__ float value_of(unsigned long long w) { return __uint_as_float((unsigned)w); }
+
+// A wave, a lane per channel: `mine` this unit's words of the lane (A, b, C: `pitch` apart), `back` words from a chunk's to those of the one in front; `first`: there is
+// none.  Returns the state in front of this chunk (`start` if it is the first) and publishes the one behind it.
+template <int kLookBack> __device__ __forceinline__ float chain_carry(unsigned long long *mine, int pitch, long long back, int ahead, bool on, float start, float A, float b) {
+    float carry = start;
+    if (ahead > 0) {
+        bool got = !on;
+        unsigned long long c = 0;
+        if (on) {
+            c = load_agent(mine - back + 2 * pitch);
+            got = is_marked(c);
         }
+        if (__all(got)) {
+            carry = value_of(c);
+        } else {
+            if (on) {
+                store_agent(mine, marked(A));
+                store_agent(mine + pitch, marked(b));
+            }
+            const long long t0 = wall_clock64();
+            for (;;) {
+                unsigned long long w[kLookBack][3];
+#pragma unroll
+                for (int d = 0; d < kLookBack; ++d)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) w[d][k] = on && d < ahead ? load_agent(mine - (d + 1) * back + k * pitch) : 0;
+                // the nearest chunk whose C is there, the maps of all nearer ones being there
+                int from = -1;
+                bool maps = true;
+#pragma unroll
+                for (int d = 0; d < kLookBack; ++d) {
+                    if (from < 0 && maps && __all(!on || is_marked(w[d][2]))) from = d;
+                    maps = maps && __all(!on || (is_marked(w[d][0]) && is_marked(w[d][1])));
+                }
+                if (from >= 0) {
+#pragma unroll
+                    for (int d = kLookBack - 1; d >= 0; --d) {
+                        if (d == from) carry = value_of(w[d][2]);
+                        else if (d < from) carry = __builtin_fmaf(value_of(w[d][0]), carry, value_of(w[d][1]));
+                    }
+                    break;
+                }
+                if (wall_clock64() - t0 > kSpinLimitTicks) {
+                    carry = __builtin_nanf("");            // make the failure visible
+                    break;
+                }
+                __builtin_amdgcn_s_sleep(1);
+            }
+        }
+    }
+    if (on) store_agent(mine + 2 * pitch, marked(__builtin_fmaf(A, carry, b)));
+    return carry;
+}
+
+__global__ __launch_bounds__(256) void k_scan_clear(u32x4_any *p, long long n) {
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = u32x4_any{0u, 0u, 0u, 0u};
+}
+
+template <typename T, int VEC, int GROUPS, bool CHAIN>
+__global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) {
+    typedef Place<VEC, GROUPS> P;
+    __shared__ float s_a[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH], s_b[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH];
+    __shared__ long long s_unit[2];
+    const int w = wave_id();
+    long long unit = (long long)blockIdx.x * P::SUBS;
+    int buf = 0;
+    if constexpr (CHAIN) {
+        if (threadIdx.x == 0) s_unit[1] = (long long)atomicAdd(a.ticket, 1ull);
+        __syncthreads();
+        unit = s_unit[1];
+    }
+    for (;;) {
+        if (CHAIN && unit >= a.units) break;
+        const int chunk = CHAIN ? (int)(unit / a.chains) : 0;
+        const long long first_chain = CHAIN ? unit - chunk * a.chains : unit;
+        unsigned long long next = 0;
+        if (CHAIN && threadIdx.x == kScanThreads - 64) next = atomicAdd(a.ticket, 1ull);
+        const P p(a, first_chain, chunk);
+        const size_t row = (size_t)p.b * a.T;
+        const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
+        T *h = static_cast<T *>(a.out) + row * a.H + p.ch;
         Lanes<T, VEC> x[kSteps][3];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const size_t at = (size_t)(s0 + i < p.n ? p.position(a, s0 + i) : 0) * 3 * a.H;
+            const size_t at = (size_t)(p.in(i) ? p.position(a, i) : 0) * 3 * a.H;
 #pragma unroll
             for (int k = 0; k < 3; ++k) x[i][k].load(G + at + (size_t)k * a.H);
+        }
+        float c[VEC];
+        if constexpr (GROUPS == 1) {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) c[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
+            if (a.states && p.on) {
+#pragma unroll
+                for (int v = 0; v < VEC; ++v)
+                    if (v >= p.skip) a.states[(size_t)p.b * a.H + p.ch + v] = c[v];
+            }
         }
         float u[kSteps][VEC], g[kSteps][VEC];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const bool in = s0 + i < p.n;
             float y[VEC];
             x[i][0].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) u[i][v] = in ? forget_rest(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
             x[i][1].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) g[i][v] = in ? candidate(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
         }
-        float c[VEC];
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) c[v] = carry[v];
         if constexpr (GROUPS > 1) {
+            float A[VEC], b[VEC];
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
-                float A = 1.f, b = 0.f;
+                A[v] = 1.f, b[v] = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
-                    A = __builtin_fmaf(-u[i][v], A, A);
+                    b[v] = __builtin_fmaf(u[i][v], g[i][v] - b[v], b[v]);
+                    A[v] = __builtin_fmaf(-u[i][v], A[v], A[v]);
                 }
-                s_a[p.sub][p.group][p.slot + v] = A;
-                s_b[p.sub][p.group][p.slot + v] = b;
+                s_a[buf][p.sub][p.group][p.slot + v] = A[v];
+                s_b[buf][p.sub][p.group][p.slot + v] = b[v];
             }
-            __syncthreads();
-            // every thread folds the maps of the groups in front of it, and goes on to the end for the next chunk's start
+            lds_barrier();
+            if (w < P::SUBS) {
+                const Folder<VEC, GROUPS> f(a, first_chain, w, chunk);
+                if (f.on) {
+                    float(&fa)[GROUPS][P::WIDTH] = s_a[buf][w], (&fb)[GROUPS][P::WIDTH] = s_b[buf][w];
+                    float state = (!CHAIN || chunk == 0) && a.first ? a.first[f.row] : 0.f;
+                    if constexpr (CHAIN) {
+                        float all = 1.f, sum = 0.f;
+#pragma unroll 8
+                        for (int k = 0; k < GROUPS; ++k) {
+                            sum = __builtin_fmaf(fa[k][f.lane], sum, fb[k][f.lane]);
+                            all *= fa[k][f.lane];
+                        }
+                        unsigned long long *mine = a.words + (chunk * a.chains + f.chain) * (3 * P::WIDTH) + f.lane;
+                        state = chain_carry<4>(mine, P::WIDTH, a.chains * (3 * P::WIDTH), chunk, true, state, all, sum);
+                    }
+                    if (a.states && f.own) a.states[f.state] = state;
+#pragma unroll 8
+                    for (int k = 0; k < GROUPS; ++k) {
+                        const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
+                        fb[k][f.lane] = state;
+                        state = x;
+                    }
+                    if (a.last && f.own && chunk == a.chunks - 1) a.last[f.row] = state;
+                }
+            }
+            if (CHAIN && threadIdx.x == kScanThreads - 64) s_unit[buf] = (long long)next;
+            lds_barrier();
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                float state = carry[v];
-#pragma unroll 4
-                for (int k = 0; k < GROUPS; ++k) {
-                    if (k == p.group) c[v] = state;
-                    state = __builtin_fmaf(s_a[p.sub][k][p.slot + v], state, s_b[p.sub][k][p.slot + v]);
-                }
-                carry[v] = state;
-            }
-            __syncthreads();
+            for (int v = 0; v < VEC; ++v) c[v] = s_b[buf][p.sub][p.group][p.slot + v];
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const bool in = s0 + i < p.n;
             float y[VEC];
             x[i][2].get(y);
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
-                y[v] = in ? gate(y[v]) * c[v] : 0.f;
+                y[v] = p.in(i) ? gate(y[v]) * c[v] : 0.f;
             }
-            if (p.on && s0 + i < a.T) put_from<T, VEC>(h + (size_t)p.position(a, s0 + i) * a.H, y, p.skip);
+            if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h + (size_t)p.position(a, i) * a.H, y, p.skip);
         }
         if constexpr (GROUPS == 1) {
+            if (a.last && p.on) {
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) carry[v] = c[v];
+                for (int v = 0; v < VEC; ++v)
+                    if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = c[v];
+            }
         }
-    }
-    if (a.last && p.group == 0 && p.on) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v)
-            if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = carry[v];
+        if constexpr (!CHAIN) break;
+        unit = s_unit[buf];
+        buf ^= 1;
     }
 }
 
-template <typename T, int VEC, int GROUPS>
-__global__ __launch_bounds__(kScanThreads) void k_scan_bwd(const ScanArgs a) {
+template <typename T, int VEC, int GROUPS, bool CHAIN>
+__global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) {
     typedef Place<VEC, GROUPS> P;
-    constexpr int SUBS = GROUPS > 1 ? P::SUBS : 1;
-    __shared__ float s_a[SUBS][GROUPS][P::WIDTH], s_b[SUBS][GROUPS][P::WIDTH], s_r[SUBS][GROUPS][P::WIDTH];
-    const P p(a);
-    const size_t row = (size_t)p.b * a.T;
-    const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
-    const T *dh = static_cast<const T *>(a.dh) + row * a.H + p.ch;
-    T *dG = static_cast<T *>(a.out) + row * 3 * a.H + p.ch;
-    float carry[VEC];                                      // f r of the step behind the chunk
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) carry[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
-    for (int chunk = a.chunks - 1; chunk >= 0; --chunk) {
-        const int s0 = chunk * GROUPS * kSteps + p.group * kSteps;
+    constexpr int BUFS = CHAIN ? 2 : 1;
+    __shared__ float s_a[BUFS][P::SUBS][GROUPS][P::WIDTH], s_b[BUFS][P::SUBS][GROUPS][P::WIDTH], s_r[BUFS][P::SUBS][GROUPS][P::WIDTH];
+    __shared__ long long s_unit[2];
+    const int w = wave_id();
+    long long unit = (long long)blockIdx.x * P::SUBS;
+    int buf = 0;
+    if constexpr (CHAIN) {
+        if (threadIdx.x == 0) s_unit[1] = (long long)atomicAdd(a.ticket, 1ull);
+        __syncthreads();
+        unit = s_unit[1];
+    }
+    for (;;) {
+        if (CHAIN && unit >= a.units) break;
+        const int link = CHAIN ? (int)(unit / a.chains) : 0, chunk = CHAIN ? a.chunks - 1 - link : 0;     // from the last chunk on
+        const long long first_chain = CHAIN ? unit - link * a.chains : unit;
+        unsigned long long next = 0;
+        if (CHAIN && threadIdx.x == kScanThreads - 64) next = atomicAdd(a.ticket, 1ull);
+        const P p(a, first_chain, chunk);
+        const size_t row = (size_t)p.b * a.T;
+        const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
+        const T *dh = static_cast<const T *>(a.dh) + row * a.H + p.ch;
+        T *dG = static_cast<T *>(a.out) + row * 3 * a.H + p.ch;
         Lanes<T, VEC> x[kSteps][3], up[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const size_t at = s0 + i < p.n ? p.position(a, s0 + i) : 0;
+            const size_t at = p.in(i) ? p.position(a, i) : 0;
 #pragma unroll
             for (int k = 0; k < 3; ++k) x[i][k].load(G + (at * 3 + k) * a.H);
             up[i].load(dh + at * a.H);
         }
         float c[VEC], q[VEC];
+        if constexpr (GROUPS == 1) {
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            c[v] = a.states[((size_t)p.b * a.chunks + chunk) * a.H + p.ch + v];
-            q[v] = carry[v];
+            for (int v = 0; v < VEC; ++v) {
+                c[v] = a.states[(size_t)p.b * a.H + p.ch + v];
+                q[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
+            }
         }
         float u[kSteps][VEC], g[kSteps][VEC], o[kSteps][VEC], d[kSteps][VEC];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const bool in = s0 + i < p.n;
             float y[VEC];
             x[i][0].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) u[i][v] = in ? forget_rest(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
             x[i][1].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) g[i][v] = in ? candidate(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
             x[i][2].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) o[i][v] = in ? gate(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) o[i][v] = p.in(i) ? gate(y[v]) : 0.f;
             up[i].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) d[i][v] = in ? y[v] : 0.f;
+            for (int v = 0; v < VEC; ++v) d[i][v] = p.in(i) ? y[v] : 0.f;
         }
         if constexpr (GROUPS > 1) {
 #pragma unroll
@@ -251,25 +385,53 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_bwd(const ScanArgs a) {
                     const float r = __builtin_fmaf(d[k][v], o[k][v], R);
                     R = __builtin_fmaf(-u[k][v], r, r);
                 }
-                s_a[p.sub][p.group][p.slot + v] = A;
-                s_b[p.sub][p.group][p.slot + v] = b;
-                s_r[p.sub][p.group][p.slot + v] = R;
+                s_a[buf][p.sub][p.group][p.slot + v] = A;
+                s_b[buf][p.sub][p.group][p.slot + v] = b;
+                s_r[buf][p.sub][p.group][p.slot + v] = R;
             }
-            __syncthreads();
+            lds_barrier();
+            // the states in front of the groups, and behind them f r of the next step: two waves' work in a chain, otherwise one's
+            if (w < (CHAIN ? 2 : P::SUBS)) {
+                const int sub = CHAIN ? 0 : w;
+                const Folder<VEC, GROUPS> f(a, first_chain, sub, chunk);
+                float(&fa)[GROUPS][P::WIDTH] = s_a[buf][sub], (&fb)[GROUPS][P::WIDTH] = s_b[buf][sub], (&fr)[GROUPS][P::WIDTH] = s_r[buf][sub];
+                if (f.on && (!CHAIN || w == 0)) {
+                    float state = a.states[f.state];
+#pragma unroll 8
+                    for (int k = 0; k < GROUPS; ++k) {
+                        const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
+                        fb[k][f.lane] = state;
+                        state = x;
+                    }
+                }
+                if (f.on && (!CHAIN || w == 1)) {
+                    float back = (!CHAIN || link == 0) && a.first ? a.first[f.row] : 0.f;
+                    if constexpr (CHAIN) {
+                        float all = 1.f, sum = 0.f;
+#pragma unroll 8
+                        for (int k = GROUPS - 1; k >= 0; --k) {
+                            sum = __builtin_fmaf(fa[k][f.lane], sum, fr[k][f.lane]);
+                            all *= fa[k][f.lane];
+                        }
+                        unsigned long long *mine = a.words + (link * a.chains + f.chain) * (3 * P::WIDTH) + f.lane;
+                        back = chain_carry<2>(mine, P::WIDTH, a.chains * (3 * P::WIDTH), link, true, back, all, sum);
+                    }
+#pragma unroll 8
+                    for (int k = GROUPS - 1; k >= 0; --k) {
+                        const float x = __builtin_fmaf(fa[k][f.lane], back, fr[k][f.lane]);
+                        fr[k][f.lane] = back;
+                        back = x;
+                    }
+                    if (a.last && f.own && chunk == 0) a.last[f.row] = back;
+                }
+            }
+            if (CHAIN && threadIdx.x == kScanThreads - 64) s_unit[buf] = (long long)next;
+            lds_barrier();
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
-                float state = c[v], back = carry[v];
-#pragma unroll 4
-                for (int k = 0; k < GROUPS; ++k) {
-                    const int j = GROUPS - 1 - k;
-                    if (k == p.group) c[v] = state;
-                    if (j == p.group) q[v] = back;
-                    state = __builtin_fmaf(s_a[p.sub][k][p.slot + v], state, s_b[p.sub][k][p.slot + v]);
-                    back = __builtin_fmaf(s_a[p.sub][j][p.slot + v], back, s_r[p.sub][j][p.slot + v]);
-                }
-                carry[v] = back;
+                c[v] = s_b[buf][p.sub][p.group][p.slot + v];
+                q[v] = s_r[buf][p.sub][p.group][p.slot + v];
             }
-            __syncthreads();
         }
         float before[kSteps][VEC];
 #pragma unroll
@@ -293,22 +455,23 @@ __global__ __launch_bounds__(kScanThreads) void k_scan_bwd(const ScanArgs a) {
                 c[v] = before[i][v];
                 q[v] = r - ru;
             }
-            if (p.on && s0 + i < a.T) {
-                T *to = dG + (size_t)p.position(a, s0 + i) * 3 * a.H;
+            if (p.on && p.s0 + i < a.T) {
+                T *to = dG + (size_t)p.position(a, i) * 3 * a.H;
                 put_from<T, VEC>(to, df, p.skip);
                 put_from<T, VEC>(to + a.H, dg, p.skip);
                 put_from<T, VEC>(to + 2 * (size_t)a.H, dout, p.skip);
             }
         }
         if constexpr (GROUPS == 1) {
+            if (a.last && p.on) {
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) carry[v] = q[v];
+                for (int v = 0; v < VEC; ++v)
+                    if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = q[v];
+            }
         }
-    }
-    if (a.last && p.group == 0 && p.on) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v)
-            if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = carry[v];
+        if constexpr (!CHAIN) break;
+        unit = s_unit[buf];
+        buf ^= 1;
     }
 }
 
@@ -327,28 +490,51 @@ static bool unaligned_scan(std::initializer_list<const void *> ps) {
     return (m & 15u) != 0;
 }
 
-template <typename T, int VEC, int GROUPS> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
+// Words and ticket of the chains.  Nothing where all steps are one chunk's.
+struct ScanPlan {
+    int vec, groups_h, chunks;
+    long long chains, units;
+    size_t bytes;
+};
+static ScanPlan scan_plan(const echo_scan_desc_t &d) {
+    ScanPlan p{};
+    p.vec = d.H < 4 ? 1 : 4;
+    p.groups_h = (d.H + 16 * p.vec - 1) / (16 * p.vec);
+    p.chunks = (int)scan_chunks(d);
+    p.chains = (long long)d.B * p.groups_h;
+    p.units = p.chains * p.chunks;
+    if (p.chunks > 1) p.bytes = 256 + (size_t)p.units * 3 * 16 * p.vec * 8;
+    return p;
+}
+
+template <typename T, int VEC, int GROUPS, bool CHAIN> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
     constexpr int SUBS = Place<VEC, GROUPS>::SUBS;
-    const unsigned blocks = (unsigned)((a.units + SUBS - 1) / SUBS);
+    const long long blocks = CHAIN ? std::min<long long>(a.units, 512) : (a.chains + SUBS - 1) / SUBS;
     LaunchRecord r = launch_begin(bwd ? "scan_bwd" : "scan_fwd", st);
-    if (bwd) k_scan_bwd<T, VEC, GROUPS><<<blocks, kScanThreads, 0, st>>>(a);
-    else k_scan_fwd<T, VEC, GROUPS><<<blocks, kScanThreads, 0, st>>>(a);
+    if (bwd) k_scan_bwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
+    else k_scan_fwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
     return launch_end(r);
 }
 template <typename T, int VEC> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
-    if (a.T <= kSteps) return launch_scan<T, VEC, 1>(a, bwd, st);
-    if (a.T <= 4 * kSteps) return launch_scan<T, VEC, 4>(a, bwd, st);
-    if (a.T <= 16 * kSteps) return launch_scan<T, VEC, 16>(a, bwd, st);
-    return launch_scan<T, VEC, kChunkGroups>(a, bwd, st);
+    if (a.chunks > 1) return launch_scan<T, VEC, kChunkGroups, true>(a, bwd, st);
+    if (a.T <= kSteps) return launch_scan<T, VEC, 1, false>(a, bwd, st);
+    if (a.T <= 4 * kSteps) return launch_scan<T, VEC, 4, false>(a, bwd, st);
+    if (a.T <= 16 * kSteps) return launch_scan<T, VEC, 16, false>(a, bwd, st);
+    return launch_scan<T, VEC, kChunkGroups, false>(a, bwd, st);
 }
-static echo_status_t run_scan(const echo_scan_desc_t &d, ScanArgs a, bool bwd, hipStream_t st) {
-    const int vec = d.H < 4 ? 1 : 4;
+static echo_status_t run_scan(const echo_scan_desc_t &d, const ScanPlan &p, ScanArgs a, bool bwd, void *workspace, hipStream_t st) {
     a.B = d.B, a.T = d.T, a.H = d.H, a.reverse = d.reverse;
-    a.chunks = (int)scan_chunks(d);
-    a.groups_h = (d.H + 16 * vec - 1) / (16 * vec);
-    a.units = (long long)d.B * a.groups_h;
-    if (d.dtype == ECHO_F32) return vec == 4 ? launch_scan<float, 4>(a, bwd, st) : launch_scan<float, 1>(a, bwd, st);
-    return vec == 4 ? launch_scan<bf16_t, 4>(a, bwd, st) : launch_scan<bf16_t, 1>(a, bwd, st);
+    a.chunks = p.chunks, a.groups_h = p.groups_h, a.chains = p.chains, a.units = p.units;
+    if (p.bytes) {
+        a.ticket = static_cast<unsigned long long *>(workspace);
+        a.words = a.ticket + 32;
+        const long long n = (long long)(p.bytes / 16);
+        LaunchRecord r = launch_begin("scan_clear", st);
+        k_scan_clear<<<(unsigned)std::min<long long>((n + 255) / 256, 2048), 256, 0, st>>>(static_cast<u32x4_any *>(workspace), n);
+        if (echo_status_t s = launch_end(r)) return s;
+    }
+    if (d.dtype == ECHO_F32) return p.vec == 4 ? launch_scan<float, 4>(a, bwd, st) : launch_scan<float, 1>(a, bwd, st);
+    return p.vec == 4 ? launch_scan<bf16_t, 4>(a, bwd, st) : launch_scan<bf16_t, 1>(a, bwd, st);
 }
 
 }  // namespace echo
@@ -359,29 +545,33 @@ size_t echo_scan_states_bytes(const echo_scan_desc_t *desc) {
     if (echo::check_scan(desc)) return 0;
     return (size_t)desc->B * echo::scan_chunks(*desc) * desc->H * 4;
 }
-size_t echo_scan_fwd_workspace_bytes(const echo_scan_desc_t *desc) { return 0; }
-size_t echo_scan_bwd_workspace_bytes(const echo_scan_desc_t *desc) { return 0; }
+size_t echo_scan_fwd_workspace_bytes(const echo_scan_desc_t *desc) { return echo::check_scan(desc) ? 0 : echo::scan_plan(*desc).bytes; }
+size_t echo_scan_bwd_workspace_bytes(const echo_scan_desc_t *desc) { return echo_scan_fwd_workspace_bytes(desc); }
 
 echo_status_t echo_scan_fwd(const echo_scan_desc_t *desc, const void *G, const float *c0, const int32_t *len, void *h, float *c_last,
                             float *states, void *workspace, size_t workspace_bytes, void *stream) {
     using namespace echo;
     if (echo_status_t s = check_scan(desc)) return s;
-    if (!G || !h) return ECHO_ERR_NULL;
+    const ScanPlan p = scan_plan(*desc);
+    if (!G || !h || (p.bytes && !workspace)) return ECHO_ERR_NULL;
     if (unaligned_scan({G, c0, len, h, c_last, states, workspace})) return ECHO_ERR_ALIGN;
+    if (workspace_bytes < p.bytes) return ECHO_ERR_WORKSPACE;
     ScanArgs a{};
     a.G = G, a.first = c0, a.len = len, a.out = h, a.last = c_last, a.states = states;
-    return run_scan(*desc, a, false, static_cast<hipStream_t>(stream));
+    return run_scan(*desc, p, a, false, workspace, static_cast<hipStream_t>(stream));
 }
 
 echo_status_t echo_scan_bwd(const echo_scan_desc_t *desc, const void *dh, const float *dc_last, const void *G, const int32_t *len,
                             const float *states, void *dG, float *dc0, void *workspace, size_t workspace_bytes, void *stream) {
     using namespace echo;
     if (echo_status_t s = check_scan(desc)) return s;
-    if (!dh || !G || !states || !dG) return ECHO_ERR_NULL;
+    const ScanPlan p = scan_plan(*desc);
+    if (!dh || !G || !states || !dG || (p.bytes && !workspace)) return ECHO_ERR_NULL;
     if (unaligned_scan({dh, dc_last, G, len, states, dG, dc0, workspace})) return ECHO_ERR_ALIGN;
+    if (workspace_bytes < p.bytes) return ECHO_ERR_WORKSPACE;
     ScanArgs a{};
     a.G = G, a.dh = dh, a.first = dc_last, a.len = len, a.out = dG, a.last = dc0, a.states = const_cast<float *>(states);
-    return run_scan(*desc, a, true, static_cast<hipStream_t>(stream));
+    return run_scan(*desc, p, a, true, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
