@@ -19,7 +19,9 @@
 namespace echo {
 
 constexpr int kSteps = 4;
-constexpr int kScanThreads = 512;
+template <int GROUPS> constexpr int kThreads = GROUPS > 16 ? 512 : 256;
+constexpr int kBlocks = 2;            // to a compute unit
+constexpr int kQueues = 32, kTicketStride = 16;            // (words of 8 bytes: a cache line)
 constexpr int kChunkGroups = ECHO_SCAN_CHUNK / kSteps;
 constexpr float kLog2eS = 1.4426950408889634f;
 
@@ -50,20 +52,29 @@ typedef __bf16 bf16_hw;
 __device__ __forceinline__ unsigned bf16_bits(float x) { return __builtin_bit_cast(unsigned short, (bf16_hw)x); }
 __device__ __forceinline__ void put_one(float *p, float x) { *p = x; }
 __device__ __forceinline__ void put_one(bf16_t *p, float x) { p->bits = (unsigned short)bf16_bits(x); }
-template <int VEC> __device__ __forceinline__ void put(float *p, const float (&x)[VEC]) {
-    if constexpr (VEC == 4) __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4_any *>(p));
-    else store_streaming(p, x[0]);
+// whole: the rows consist of whole groups of 16 bytes
+template <int VEC> __device__ __forceinline__ void put(float *p, const float (&x)[VEC], bool whole) {
+    if constexpr (VEC == 4) {
+        const f32x4 v = {x[0], x[1], x[2], x[3]};
+        if (whole) __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(p));
+        else *reinterpret_cast<f32x4_any *>(p) = v;
+    } else {
+        *p = x[0];
+    }
 }
-template <int VEC> __device__ __forceinline__ void put(bf16_t *p, const float (&x)[VEC]) {
-    if constexpr (VEC == 4)
-        __builtin_nontemporal_store(u32x2{bf16_bits(x[0]) | bf16_bits(x[1]) << 16, bf16_bits(x[2]) | bf16_bits(x[3]) << 16}, reinterpret_cast<u32x2_any *>(p));
-    else p->bits = (unsigned short)bf16_bits(x[0]);
+template <int VEC> __device__ __forceinline__ void put(bf16_t *p, const float (&x)[VEC], bool whole) {
+    if constexpr (VEC == 4) {
+        const u32x2 v = {bf16_bits(x[0]) | bf16_bits(x[1]) << 16, bf16_bits(x[2]) | bf16_bits(x[3]) << 16};
+        if (whole) __builtin_nontemporal_store(v, reinterpret_cast<u32x2 *>(p));
+        else *reinterpret_cast<u32x2_any *>(p) = v;
+    } else {
+        p->bits = (unsigned short)bf16_bits(x[0]);
+    }
 }
-
 // x[skip ..]: what a lane's neighbour has in front of that is not its own
-template <typename T, int VEC> __device__ __forceinline__ void put_from(T *p, const float (&x)[VEC], int skip) {
+template <typename T, int VEC> __device__ __forceinline__ void put_from(T *p, const float (&x)[VEC], int skip, bool whole) {
     if (skip == 0) {
-        put<VEC>(p, x);
+        put<VEC>(p, x, whole);
     } else {
 #pragma unroll
         for (int v = 1; v < VEC; ++v)
@@ -76,16 +87,18 @@ struct ScanArgs {
     const float *first;              // c0; dc_last
     const int *len;
     int B, T, H, reverse, chunks, groups_h;   // groups_h: units along the channels
-    long long chains, units;         // B groups_h; chains by chunks
+    long long chains, units, chain0; // B groups_h; chains by chunks; the launch's first
     void *out;                       // h; dG
     float *last;                     // c_last; dc0
     float *states;
-    unsigned long long *words, *ticket;       // [units][3][WIDTH]; the next unit to be taken
+    unsigned long long *words, *tickets;      // [units][WIDTH]; [queues], kTicketStride apart: the next to be taken
+    int queues;
+    bool whole;                      // rows are whole groups of 16 bytes
 };
 
 // What a thread is in a unit
 template <int VEC, int GROUPS> struct Place {
-    static constexpr int SUBS = kScanThreads / 16 / GROUPS, WIDTH = 16 * VEC;
+    static constexpr int SUBS = kThreads<GROUPS> / 16 / GROUPS, WIDTH = 16 * VEC;
     int group, sub, slot, b, base, ch, skip, chunk, s0;    // skip: of its VEC channels, those in front that are the neighbour's
     bool on;                         // it has channels of its own
     int n;                           // steps of the sequence
@@ -132,63 +145,73 @@ template <int VEC, int GROUPS> struct Folder {
 // The chunks of a sequence's channels are a chain: each hands the state behind it to the next.  A chunk publishes its map (A, b) as soon as it has it, and the
 // state behind it (C) as soon as it knows the one in front of it; the next one takes C from the chunk in front, or from one up to kLookBack in front and applies
 // the maps of those between, in order, with the same operation that each of them applies to its own: results do not depend on how far it looked.
-// A value goes out in one 64-bit word with a mark, so that nothing has to be waited for in between; the words are cleared in front of the launch.
-// Units are taken by ticket, chunk after chunk: whoever waits, waits for a unit that has been taken already and waits for lower tickets only.
-constexpr unsigned kMark = 1;
-__device__ __forceinline__ unsigned long long marked(float x) { return (unsigned long long)kMark << 32 | __float_as_uint(x); }
-__device__ __forceinline__ bool is_marked(unsigned long long w) { return (unsigned)(w >> 32) == kMark; }
-__device__ __forceinline__ float value_of(unsigned long long w) { return __uint_as_float((unsigned)w); }
+// Map and state go out in one 64-bit word, b or C below and above it A, which is 0 to 1 and leaves the upper two bits for what it is (A that is NaN comes with
+// a b that is), so that nothing has to be waited for in between; the words are cleared in front of the launch.
+// Units are taken by ticket, chunk after chunk: whoever waits, waits for a unit that has been taken already and waits for lower tickets only.  The chains are
+// dealt to up to kQueues queues with a ticket counter and blocks each: one counter for all gives out a ticket every 15 to 20 ns, no matter who asks
+// (4 x 16384 x 1280 bf16, forward: 181 us of 10240 tickets).
+struct Queue {
+    unsigned *ticket;
+    long long first;                 // chain; neighbours are one queue's, and with it one XCD's: they share cache lines where rows are not whole ones
+    int chains;
+    __device__ __forceinline__ Queue(const ScanArgs &a) {
+        const int q = (int)blockIdx.x % a.queues;
+        ticket = reinterpret_cast<unsigned *>(a.tickets + q * kTicketStride);
+        first = a.chains * q / a.queues;
+        chains = (int)(a.chains * (q + 1) / a.queues - first);
+    }
+    __device__ __forceinline__ unsigned take() const { return atomicAdd(ticket, 1u); }
+    // the unit of a ticket: link of the chain, chain; false: there is none
+    __device__ __forceinline__ bool unit(unsigned t, int links, int &link, long long &chain) const {
+        link = (int)(t / (unsigned)chains);
+        chain = first + (t - (unsigned)link * chains);
+        return link < links;
+    }
+};
+typedef unsigned long long Word;
+constexpr Word kMapMark = 1ull << 62, kStateMark = 1ull << 63;
+__device__ __forceinline__ Word map_word(float A, float b) {
+    return kMapMark | (Word)(__float_as_uint(A) & 0x3fffffffu) << 32 | __float_as_uint(b);
+}
+__device__ __forceinline__ Word state_word(float c) { return kStateMark | __float_as_uint(c); }
+__device__ __forceinline__ float factor_of(Word w) { return __uint_as_float((unsigned)(w >> 32) & 0x3fffffffu); }
+__device__ __forceinline__ float value_of(Word w) { return __uint_as_float((unsigned)w); }
 
-// A wave, a lane per channel: `mine` this unit's words of the lane (A, b, C: `pitch` apart), `back` words from a chunk's to those of the one in front; `first`: there is
-// none.  Returns the state in front of this chunk (`start` if it is the first) and publishes the one behind it.
-template <int kLookBack> __device__ __forceinline__ float chain_carry(unsigned long long *mine, int pitch, long long back, int ahead, bool on, float start, float A, float b) {
+// The state in front of this chunk from the words of the W chunks in front of it (`ahead` of them exist), a lane per channel; false: it can't be told yet.
+// `back`: words from a chunk's to those of the one in front of it.
+template <int W> __device__ __forceinline__ bool look_back(const Word *unit, int lane, long long back, int ahead, float &carry) {
+    Word w[W];
+#pragma unroll
+    for (int d = 0; d < W; ++d) w[d] = load_agent(unit - (min(d, ahead - 1) + 1) * back + lane);
+    int from = -1;                                         // the nearest chunk whose state is there, the maps of all nearer ones being there
+    bool maps = true;
+#pragma unroll
+    for (int d = 0; d < W; ++d) {
+        if (from < 0 && maps && d < ahead && __all((w[d] & kStateMark) != 0)) from = d;
+        maps = maps && __all((w[d] & kMapMark) != 0);
+    }
+    if (from < 0) return false;
+#pragma unroll
+    for (int d = W - 1; d >= 0; --d) {
+        if (d == from) carry = value_of(w[d]);
+        else if (d < from) carry = __builtin_fmaf(factor_of(w[d]), carry, value_of(w[d]));
+    }
+    return true;
+}
+// Publishes this chunk's map, returns the state in front of it (`start` if it is the first) and publishes the one behind it.
+template <int W> __device__ __forceinline__ float chain_carry(Word *unit, int lane, long long back, int ahead, float start, float A, float b) {
     float carry = start;
     if (ahead > 0) {
-        bool got = !on;
-        unsigned long long c = 0;
-        if (on) {
-            c = load_agent(mine - back + 2 * pitch);
-            got = is_marked(c);
-        }
-        if (__all(got)) {
-            carry = value_of(c);
-        } else {
-            if (on) {
-                store_agent(mine, marked(A));
-                store_agent(mine + pitch, marked(b));
-            }
-            const long long t0 = wall_clock64();
-            for (;;) {
-                unsigned long long w[kLookBack][3];
-#pragma unroll
-                for (int d = 0; d < kLookBack; ++d)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) w[d][k] = on && d < ahead ? load_agent(mine - (d + 1) * back + k * pitch) : 0;
-                // the nearest chunk whose C is there, the maps of all nearer ones being there
-                int from = -1;
-                bool maps = true;
-#pragma unroll
-                for (int d = 0; d < kLookBack; ++d) {
-                    if (from < 0 && maps && __all(!on || is_marked(w[d][2]))) from = d;
-                    maps = maps && __all(!on || (is_marked(w[d][0]) && is_marked(w[d][1])));
-                }
-                if (from >= 0) {
-#pragma unroll
-                    for (int d = kLookBack - 1; d >= 0; --d) {
-                        if (d == from) carry = value_of(w[d][2]);
-                        else if (d < from) carry = __builtin_fmaf(value_of(w[d][0]), carry, value_of(w[d][1]));
-                    }
-                    break;
-                }
-                if (wall_clock64() - t0 > kSpinLimitTicks) {
-                    carry = __builtin_nanf("");            // make the failure visible
-                    break;
-                }
-                __builtin_amdgcn_s_sleep(1);
+        store_agent(unit + lane, map_word(A, b));
+        const long long t0 = wall_clock64();
+        while (!look_back<W>(unit, lane, back, ahead, carry)) {
+            if (wall_clock64() - t0 > kSpinLimitTicks) {
+                carry = __builtin_nanf("");                // make the failure visible
+                break;
             }
         }
     }
-    if (on) store_agent(mine + 2 * pitch, marked(__builtin_fmaf(A, carry, b)));
+    store_agent(unit + lane, state_word(__builtin_fmaf(factor_of(map_word(A, b)), carry, b)));
     return carry;
 }
 
@@ -197,24 +220,26 @@ __global__ __launch_bounds__(256) void k_scan_clear(u32x4_any *p, long long n) {
 }
 
 template <typename T, int VEC, int GROUPS, bool CHAIN>
-__global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) {
+__global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs a) {
     typedef Place<VEC, GROUPS> P;
     __shared__ float s_a[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH], s_b[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH];
-    __shared__ long long s_unit[2];
+    __shared__ unsigned s_ticket[2];
     const int w = wave_id();
-    long long unit = (long long)blockIdx.x * P::SUBS;
+    const Queue queue(a);
+    unsigned ticket = 0;
     int buf = 0;
     if constexpr (CHAIN) {
-        if (threadIdx.x == 0) s_unit[1] = (long long)atomicAdd(a.ticket, 1ull);
+        if (threadIdx.x == 0) s_ticket[1] = queue.take();
         __syncthreads();
-        unit = s_unit[1];
+        ticket = __builtin_amdgcn_readfirstlane(s_ticket[1]);
     }
     for (;;) {
-        if (CHAIN && unit >= a.units) break;
-        const int chunk = CHAIN ? (int)(unit / a.chains) : 0;
-        const long long first_chain = CHAIN ? unit - chunk * a.chains : unit;
-        unsigned long long next = 0;
-        if (CHAIN && threadIdx.x == kScanThreads - 64) next = atomicAdd(a.ticket, 1ull);
+        int link = 0;
+        long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
+        if (CHAIN && !queue.unit(ticket, a.chunks, link, first_chain)) break;
+        unsigned next = 0;
+        if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
+        const int chunk = link;
         const P p(a, first_chain, chunk);
         const size_t row = (size_t)p.b * a.T;
         const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
@@ -268,16 +293,15 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) 
                     float state = (!CHAIN || chunk == 0) && a.first ? a.first[f.row] : 0.f;
                     if constexpr (CHAIN) {
                         float all = 1.f, sum = 0.f;
-#pragma unroll 8
+#pragma unroll 4
                         for (int k = 0; k < GROUPS; ++k) {
                             sum = __builtin_fmaf(fa[k][f.lane], sum, fb[k][f.lane]);
                             all *= fa[k][f.lane];
                         }
-                        unsigned long long *mine = a.words + (chunk * a.chains + f.chain) * (3 * P::WIDTH) + f.lane;
-                        state = chain_carry<4>(mine, P::WIDTH, a.chains * (3 * P::WIDTH), chunk, true, state, all, sum);
+                        state = chain_carry<8>(a.words + (link * a.chains + f.chain) * P::WIDTH, f.lane, a.chains * P::WIDTH, chunk, state, all, sum);
                     }
                     if (a.states && f.own) a.states[f.state] = state;
-#pragma unroll 8
+#pragma unroll 4
                     for (int k = 0; k < GROUPS; ++k) {
                         const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
                         fb[k][f.lane] = state;
@@ -286,7 +310,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) 
                     if (a.last && f.own && chunk == a.chunks - 1) a.last[f.row] = state;
                 }
             }
-            if (CHAIN && threadIdx.x == kScanThreads - 64) s_unit[buf] = (long long)next;
+            if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
             lds_barrier();
 #pragma unroll
             for (int v = 0; v < VEC; ++v) c[v] = s_b[buf][p.sub][p.group][p.slot + v];
@@ -300,7 +324,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) 
                 c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
                 y[v] = p.in(i) ? gate(y[v]) * c[v] : 0.f;
             }
-            if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h + (size_t)p.position(a, i) * a.H, y, p.skip);
+            if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h + (size_t)p.position(a, i) * a.H, y, p.skip, a.whole);
         }
         if constexpr (GROUPS == 1) {
             if (a.last && p.on) {
@@ -310,31 +334,33 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_fwd(const ScanArgs a) 
             }
         }
         if constexpr (!CHAIN) break;
-        unit = s_unit[buf];
+        ticket = __builtin_amdgcn_readfirstlane(s_ticket[buf]);
         buf ^= 1;
     }
 }
 
 template <typename T, int VEC, int GROUPS, bool CHAIN>
-__global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) {
+__global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs a) {
     typedef Place<VEC, GROUPS> P;
     constexpr int BUFS = CHAIN ? 2 : 1;
     __shared__ float s_a[BUFS][P::SUBS][GROUPS][P::WIDTH], s_b[BUFS][P::SUBS][GROUPS][P::WIDTH], s_r[BUFS][P::SUBS][GROUPS][P::WIDTH];
-    __shared__ long long s_unit[2];
+    __shared__ unsigned s_ticket[2];
     const int w = wave_id();
-    long long unit = (long long)blockIdx.x * P::SUBS;
+    const Queue queue(a);
+    unsigned ticket = 0;
     int buf = 0;
     if constexpr (CHAIN) {
-        if (threadIdx.x == 0) s_unit[1] = (long long)atomicAdd(a.ticket, 1ull);
+        if (threadIdx.x == 0) s_ticket[1] = queue.take();
         __syncthreads();
-        unit = s_unit[1];
+        ticket = __builtin_amdgcn_readfirstlane(s_ticket[1]);
     }
     for (;;) {
-        if (CHAIN && unit >= a.units) break;
-        const int link = CHAIN ? (int)(unit / a.chains) : 0, chunk = CHAIN ? a.chunks - 1 - link : 0;     // from the last chunk on
-        const long long first_chain = CHAIN ? unit - link * a.chains : unit;
-        unsigned long long next = 0;
-        if (CHAIN && threadIdx.x == kScanThreads - 64) next = atomicAdd(a.ticket, 1ull);
+        int link = 0;
+        long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
+        if (CHAIN && !queue.unit(ticket, a.chunks, link, first_chain)) break;
+        unsigned next = 0;
+        if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
+        const int chunk = a.chunks - 1 - link;             // from the last one on
         const P p(a, first_chain, chunk);
         const size_t row = (size_t)p.b * a.T;
         const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
@@ -397,7 +423,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) 
                 float(&fa)[GROUPS][P::WIDTH] = s_a[buf][sub], (&fb)[GROUPS][P::WIDTH] = s_b[buf][sub], (&fr)[GROUPS][P::WIDTH] = s_r[buf][sub];
                 if (f.on && (!CHAIN || w == 0)) {
                     float state = a.states[f.state];
-#pragma unroll 8
+#pragma unroll 4
                     for (int k = 0; k < GROUPS; ++k) {
                         const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
                         fb[k][f.lane] = state;
@@ -408,15 +434,14 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) 
                     float back = (!CHAIN || link == 0) && a.first ? a.first[f.row] : 0.f;
                     if constexpr (CHAIN) {
                         float all = 1.f, sum = 0.f;
-#pragma unroll 8
+#pragma unroll 4
                         for (int k = GROUPS - 1; k >= 0; --k) {
                             sum = __builtin_fmaf(fa[k][f.lane], sum, fr[k][f.lane]);
                             all *= fa[k][f.lane];
                         }
-                        unsigned long long *mine = a.words + (link * a.chains + f.chain) * (3 * P::WIDTH) + f.lane;
-                        back = chain_carry<2>(mine, P::WIDTH, a.chains * (3 * P::WIDTH), link, true, back, all, sum);
+                        back = chain_carry<4>(a.words + (link * a.chains + f.chain) * P::WIDTH, f.lane, a.chains * P::WIDTH, link, back, all, sum);
                     }
-#pragma unroll 8
+#pragma unroll 4
                     for (int k = GROUPS - 1; k >= 0; --k) {
                         const float x = __builtin_fmaf(fa[k][f.lane], back, fr[k][f.lane]);
                         fr[k][f.lane] = back;
@@ -425,7 +450,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) 
                     if (a.last && f.own && chunk == 0) a.last[f.row] = back;
                 }
             }
-            if (CHAIN && threadIdx.x == kScanThreads - 64) s_unit[buf] = (long long)next;
+            if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
             lds_barrier();
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
@@ -457,9 +482,9 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) 
             }
             if (p.on && p.s0 + i < a.T) {
                 T *to = dG + (size_t)p.position(a, i) * 3 * a.H;
-                put_from<T, VEC>(to, df, p.skip);
-                put_from<T, VEC>(to + a.H, dg, p.skip);
-                put_from<T, VEC>(to + 2 * (size_t)a.H, dout, p.skip);
+                put_from<T, VEC>(to, df, p.skip, a.whole);
+                put_from<T, VEC>(to + a.H, dg, p.skip, a.whole);
+                put_from<T, VEC>(to + 2 * (size_t)a.H, dout, p.skip, a.whole);
             }
         }
         if constexpr (GROUPS == 1) {
@@ -470,7 +495,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void k_scan_bwd(const ScanArgs a) 
             }
         }
         if constexpr (!CHAIN) break;
-        unit = s_unit[buf];
+        ticket = __builtin_amdgcn_readfirstlane(s_ticket[buf]);
         buf ^= 1;
     }
 }
@@ -494,6 +519,7 @@ static bool unaligned_scan(std::initializer_list<const void *> ps) {
 struct ScanPlan {
     int vec, groups_h, chunks;
     long long chains, units;
+    int queues;
     size_t bytes;
 };
 static ScanPlan scan_plan(const echo_scan_desc_t &d) {
@@ -503,17 +529,33 @@ static ScanPlan scan_plan(const echo_scan_desc_t &d) {
     p.chunks = (int)scan_chunks(d);
     p.chains = (long long)d.B * p.groups_h;
     p.units = p.chains * p.chunks;
-    if (p.chunks > 1) p.bytes = 256 + (size_t)p.units * 3 * 16 * p.vec * 8;
+    if (p.chunks > 1) {
+        p.bytes = kQueues * kTicketStride * 8 + (size_t)p.units * 16 * p.vec * 8;
+        // as many queues as there are chains, or a number up to kQueues that deals them out evenly
+        long long least = p.chains * 2;
+        for (int q = (int)std::min<long long>(p.chains, kQueues); q > (int)std::min<long long>(p.chains, kQueues) / 2; --q) {
+            const long long most = (p.chains + q - 1) / q * q;
+            if (most < least) least = most, p.queues = q;
+        }
+    }
     return p;
 }
 
 template <typename T, int VEC, int GROUPS, bool CHAIN> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
     constexpr int SUBS = Place<VEC, GROUPS>::SUBS;
-    const long long blocks = CHAIN ? std::min<long long>(a.units, 512) : (a.chains + SUBS - 1) / SUBS;
-    LaunchRecord r = launch_begin(bwd ? "scan_bwd" : "scan_fwd", st);
-    if (bwd) k_scan_bwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
-    else k_scan_fwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kScanThreads, 0, st>>>(a);
-    return launch_end(r);
+    const auto launch = [&](const ScanArgs &x, long long blocks) {
+        LaunchRecord r = launch_begin(bwd ? "scan_bwd" : "scan_fwd", st);
+        if (bwd) k_scan_bwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kThreads<GROUPS>, 0, st>>>(x);
+        else k_scan_fwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kThreads<GROUPS>, 0, st>>>(x);
+        return launch_end(r);
+    };
+    // as many blocks as the chip holds, the same number for each queue
+    if (CHAIN) return launch(a, (std::min<long long>(a.units, 256 * kBlocks) + a.queues - 1) / a.queues * a.queues);
+    ScanArgs x = a;
+    constexpr long long MOST = 1 << 22;                    // blocks of a launch: a grid has fewer than 2^32 threads
+    for (; x.chain0 < a.chains; x.chain0 += MOST * SUBS)
+        if (echo_status_t s = launch(x, std::min(MOST, (a.chains - x.chain0 + SUBS - 1) / SUBS))) return s;
+    return ECHO_OK;
 }
 template <typename T, int VEC> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
     if (a.chunks > 1) return launch_scan<T, VEC, kChunkGroups, true>(a, bwd, st);
@@ -524,10 +566,13 @@ template <typename T, int VEC> static echo_status_t launch_scan(const ScanArgs &
 }
 static echo_status_t run_scan(const echo_scan_desc_t &d, const ScanPlan &p, ScanArgs a, bool bwd, void *workspace, hipStream_t st) {
     a.B = d.B, a.T = d.T, a.H = d.H, a.reverse = d.reverse;
+    a.queues = 1;
+    a.whole = d.H % (d.dtype == ECHO_F32 ? 4 : 8) == 0;
     a.chunks = p.chunks, a.groups_h = p.groups_h, a.chains = p.chains, a.units = p.units;
     if (p.bytes) {
-        a.ticket = static_cast<unsigned long long *>(workspace);
-        a.words = a.ticket + 32;
+        a.tickets = static_cast<unsigned long long *>(workspace);
+        a.words = a.tickets + kQueues * kTicketStride;
+        a.queues = p.queues;
         const long long n = (long long)(p.bytes / 16);
         LaunchRecord r = launch_begin("scan_clear", st);
         k_scan_clear<<<(unsigned)std::min<long long>((n + 255) / 256, 2048), 256, 0, st>>>(static_cast<u32x4_any *>(workspace), n);
