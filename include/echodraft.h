@@ -16,7 +16,7 @@
  *   - A drafted word outside [0, V) is not taken.  NaN in p, q or u at a drafted word: not taken.
  *   - Weights that are no positive finite numbers (NaN, infinities) count as zero.  Where p[a] has no other ones there is no word to draw: -1.
  *   - r below 0 or NaN counts as 0; r of 1 and more draws the last word with a weight.
- *   - Neither p behind position n nor q and d from position n on are read.  n below 0 counts as 0, above K as K.
+ *   - What p holds behind position n, and q, d and u from position n on, does not matter.  n below 0 counts as 0, above K as K.
  *
  * Conventions: as in echoattn.h (caller-owned 16-byte aligned DEVICE memory, row-major and contiguous, work enqueued on `stream`, no
  * synchronisation, no allocation, results bit-identical from run to run, calls that share a workspace ordered by the caller, workspace contents in any

@@ -1,8 +1,8 @@
 // Verification of drafted words (include/echodraft.h has the rules): a block per sequence.
 //
 // Which words are taken takes K pairs of probabilities; the word that is drawn behind them takes one row of the model's and, if a word was not taken,
-// one of the student's.  The block sums the weights of that row by segments, finds the segment in which the sum passes r of the whole, and goes over
-// that segment again.  All sums are in 64 bits and in an order that depends on V alone.
+// one of the student's.  The block sums the weights of that row by segments, which its waves take in turn, finds the segment in which the sum passes r of
+// the whole, and a wave goes over that segment again.  All sums are in 64 bits and in an order that depends on V alone.
 #include "../../include/echodraft.h"
 
 #include <hip/hip_runtime.h>
@@ -14,7 +14,8 @@
 
 namespace echo {
 
-constexpr int kDraftWaves = 16;
+constexpr int kDraftWaves = 16, kDraftSegments = 256;
+constexpr int kDraftAtOnce = 4;      // segments whose words a wave requests at once
 
 struct DraftArgs {
     const int *drafted, *n_drafted;
@@ -24,11 +25,6 @@ struct DraftArgs {
     int *tokens, *taken;
 };
 
-__device__ __forceinline__ double wave_sum_f64(double x) {
-#pragma unroll
-    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
-    return x;
-}
 // inclusive sums over the lanes
 __device__ __forceinline__ double wave_scan_f64(double x, int lane) {
 #pragma unroll
@@ -38,104 +34,186 @@ __device__ __forceinline__ double wave_scan_f64(double x, int lane) {
     }
     return x;
 }
-
-// the weight of a word: positive and finite, or zero
-template <typename T> __device__ __forceinline__ double weight(const T *p, const T *q, int v) {
-    const float x = ld(p, v);
-    const double w = q ? (double)x - (double)ld(q, v) : (double)x;
-    return w > 0.0 && w < __builtin_inf() ? w : 0.0;
+// Sums of four values per lane over the lanes: of value l / 16 for lane l.  At the first two steps a lane keeps half of its values and hands the other half on.
+__device__ __forceinline__ double wave_sums_f64(const double (&a)[4], int lane) {
+    const bool high = lane & 32, odd = lane & 16;
+    const double b0 = (high ? a[2] : a[0]) + __shfl_xor(high ? a[0] : a[2], 32), b1 = (high ? a[3] : a[1]) + __shfl_xor(high ? a[1] : a[3], 32);
+    double c = (odd ? b1 : b0) + __shfl_xor(odd ? b0 : b1, 16);
+#pragma unroll
+    for (int off = 8; off; off >>= 1) c += __shfl_xor(c, off);
+    return c;
 }
 
-template <typename T> __global__ __launch_bounds__(64 * kDraftWaves) void k_draft_verify(const DraftArgs a) {
-    __shared__ double s_sum[kDraftWaves][4];
-    __shared__ double s_before;
-    __shared__ int s_segment;
+// Four consecutive words' probabilities as they stand in memory: the four from v on, or the row's last four, of which word() says which is which.
+// FEW: there are fewer than four words.
+template <typename T, bool FEW> struct Four {
+    RawKey<T> raw;
+    static __device__ __forceinline__ int first(int v, int V) { return max(0, min(v, V - 4)); }
+    __device__ __forceinline__ void load(const T *row, int v, int V) {
+        // (a byte offset of 32 bits on a scalar address: 2^24 words at most)
+        if constexpr (!FEW) raw.load(reinterpret_cast<const T *>(reinterpret_cast<const char *>(row) + (unsigned)first(v, V) * (unsigned)sizeof(T)), 0);
+        else raw.load_some(row, V);
+    }
+    __device__ __forceinline__ void get(float (&x)[4]) const {
+        const float4 y = raw.get();
+        x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
+    }
+};
+// the weight of a word: p - q, where that is positive and finite, or zero
+__device__ __forceinline__ double weight(float p, float q, bool word) {
+    const bool on = (int)word & (int)(p > q) & (int)(p < __builtin_inff()) & (int)(q > -__builtin_inff());      // (no branches)
+    return (double)(on ? p : 0.f) - (double)(on ? q : 0.f);
+}
+// the weights of the words from v on, zero for those that are not v .. v + 3 or not in the vocabulary
+template <typename T, bool FEW> __device__ __forceinline__ void weights(const Four<T, FEW> &p, const Four<T, FEW> &q, bool both, int v, int V, double (&w)[4]) {
+    float x[4], y[4];
+    p.get(x);
+    q.get(y);
+    const int first = Four<T, FEW>::first(v, V);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = weight(x[e], both ? y[e] : 0.f, (int)(first + e >= v) & (int)(first + e < V));
+}
+
+template <typename T, bool FEW> __global__ __launch_bounds__(64 * kDraftWaves) void k_draft_verify(const DraftArgs a) {
+    __shared__ double s_sum[kDraftSegments];
     const int b = blockIdx.x, lane = lane_id(), w = wave_id(), V = a.V;
     const int n = a.n_drafted ? clamp_len(a.n_drafted[b], a.K) : a.K;
     const T *p = static_cast<const T *>(a.target) + (size_t)b * (a.K + 1) * V, *q = static_cast<const T *>(a.draft) + (size_t)b * a.K * V;
-    // the first word that is not taken: every wave for itself
+    const int *drafted = a.drafted + (size_t)b * a.K;
+    // the first word that is not taken: every wave for itself.  (What is read does not wait for n, nor does r)
+    const float r = a.r[b];
     int take = n;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = min(i0 + lane, n - 1), d = a.drafted[(size_t)b * a.K + i];
+    for (int i0 = 0; i0 < a.K; i0 += 64) {
+        const int i = min(i0 + lane, a.K - 1), d = drafted[i];
+        const float u = a.u[(size_t)b * a.K + i];
         const bool word = (unsigned)d < (unsigned)V;
         const size_t at = (size_t)i * V + (word ? d : 0);
-        const bool good = word && (double)a.u[(size_t)b * a.K + i] * (double)ld(q, at) < (double)ld(p, at);
-        const unsigned long long bad = __ballot(!good);
+        const float pd = ld(p, at), qd = ld(q, at);
+        const unsigned long long bad = __ballot(!word || i0 + lane >= n || !((double)u * (double)qd < (double)pd));
         if (bad) {
             take = min(n, i0 + __builtin_ctzll(bad));
             break;
         }
     }
+    const bool both = take < n;
     p += (size_t)take * V;
-    q = take < n ? q + (size_t)take * V : nullptr;
+    q = both ? q + (size_t)take * V : p;
     int *tokens = a.tokens + (size_t)b * (a.K + 1);
     for (int i = threadIdx.x; i <= a.K; i += 64 * kDraftWaves)
-        if (i != take) tokens[i] = i < take ? a.drafted[(size_t)b * a.K + i] : -1;
+        if (i != take) tokens[i] = i < take ? drafted[i] : -1;
     if (threadIdx.x == 0) a.taken[b] = take;
 
-    // segments of whole groups of 64 words, four a wave
-    constexpr int SEGMENTS = 4 * kDraftWaves;
-    const int size = ((V + SEGMENTS - 1) / SEGMENTS + 63) / 64 * 64;
-    double total = 0.0;
-    for (int attempt = 0; attempt < 2; ++attempt) {
-        double sum[4];
+    // segments of 256 m words: m groups of four words for each lane
+    const int m = (V + 256 * kDraftSegments - 1) / (256 * kDraftSegments), size = 256 * m;
+    bool less = both;                                      // the weights are p - q; if nothing is left of p behind q, p itself
+    double upto = 0.0, total = 0.0, before = 0.0;
+    for (;;) {
+        // step t: group t / m of this wave's segments, its j-th 256 words of each; the next step's words are on their way
+        constexpr int U = kDraftAtOnce;
+        const int steps = kDraftSegments / (kDraftWaves * U) * m;
+        Four<T, FEW> fp[2][U], fq[2][U];
+        const auto word_of = [&](int t, int k) { return (w + (t / m * U + k) * kDraftWaves) * size + t % m * 256 + lane * 4; };
+        const auto fetch = [&](int buf, int t) __attribute__((always_inline)) {
+            // (behind the last step, and behind the last word: the row's last words once more)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int begin = (w * 4 + k) * size, end = min(V, begin + size);
-            sum[k] = 0.0;
-            for (int v = begin + lane; v < end; v += 64) sum[k] += weight(p, q, v);
-        }
+            for (int k = 0; k < U; ++k) {
+                fp[buf][k].load(p, word_of(t, k), V);
+                fq[buf][k].load(q, word_of(t, k), V);
+            }
+        };
+        double sum[U] = {};
+        const auto add = [&](int buf, int t) __attribute__((always_inline)) {
+            if (word_of(t, 0) - lane * 4 < V) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            sum[k] = wave_sum_f64(sum[k]);
-            if (lane == 0) s_sum[w][k] = sum[k];
+                for (int k = 0; k < U; ++k) {
+                    double x[4];
+                    weights(fp[buf][k], fq[buf][k], less, word_of(t, k), V, x);
+                    sum[k] += (x[0] + x[1]) + (x[2] + x[3]);
+                    __builtin_amdgcn_sched_barrier(0);     // one segment after the other: the registers are the next step's
+                }
+            }
+            if ((t + 1) % m != 0) return;
+            const double mine = wave_sums_f64(sum, lane);
+            if ((lane & 15) == 0) s_sum[w + (t / m * U + (lane >> 4)) * kDraftWaves] = mine;
+#pragma unroll
+            for (int k = 0; k < U; ++k) sum[k] = 0.0;
+        };
+        fetch(0, 0);
+        for (int t = 0; t < steps; t += 2) {
+            fetch(1, t + 1);
+            add(0, t);
+            fetch(0, t + 2);
+            if (t + 1 < steps) add(1, t + 1);
         }
         __syncthreads();
-        total = 0.0;
-        for (int k = 0; k < SEGMENTS; ++k) total += s_sum[k >> 2][k & 3];
-        if (total > 0.0 || !q) break;
-        q = nullptr;                                       // nothing is left of p behind q: p itself
-        __syncthreads();
-    }
-    if (!(total > 0.0)) {
-        if (threadIdx.x == 0) tokens[take] = -1;
-        return;
-    }
-    if (threadIdx.x == 0) {
-        const float r = a.r[b];
-        const double at = r > 0.f ? (double)r * total : 0.0;
-        double before = 0.0, found_before = 0.0;
-        int found = -1, last = 0;
-        double last_before = 0.0;
-        for (int k = 0; k < SEGMENTS; ++k) {
-            const double x = s_sum[k >> 2][k & 3];
-            if (x > 0.0) last = k, last_before = before;
-            if (found < 0 && before + x > at) found = k, found_before = before;
-            before += x;
+        // every wave: four segments a lane, their sums up to each
+        double x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = s_sum[lane * 4 + k];
+        upto = wave_scan_f64((x[0] + x[1]) + (x[2] + x[3]), lane);
+        total = __shfl(upto, 63);
+        if (total > 0.0 || !less) {
+            const double at = r > 0.f ? (double)r * total : 0.0;
+            if (w != 0) return;
+            if (!(total > 0.0)) {
+                if (lane == 0) tokens[take] = -1;
+                return;
+            }
+            // the first segment whose sum passes, or the last one that has a weight
+            before = __shfl_up(upto, 1);
+            if (lane == 0) before = 0.0;
+            int segment = -1, last = -1;
+            double start = 0.0, last_start = 0.0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (x[k] > 0.0) {
+                    last = lane * 4 + k, last_start = before;
+                    if (segment < 0 && before + x[k] > at) segment = last, start = before;
+                }
+                before += x[k];
+            }
+            const unsigned long long pass = __ballot(segment >= 0), any = __ballot(last >= 0);
+            const int from = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(any);
+            segment = __shfl(pass ? segment : last, from);
+            before = __shfl(pass ? start : last_start, from);
+            // the words of that segment, 4 m a lane
+            const int v0 = segment * size + lane * 4 * m;
+            double own = 0.0;
+            for (int j = 0; j < m; ++j) {
+                Four<T, FEW> fp, fq;
+                fp.load(p, v0 + 4 * j, V);
+                fq.load(q, v0 + 4 * j, V);
+                weights(fp, fq, less, v0 + 4 * j, V, x);
+                own += (x[0] + x[1]) + (x[2] + x[3]);
+            }
+            upto = wave_scan_f64(own, lane);
+            double sum_to = before + __shfl_up(upto, 1);
+            if (lane == 0) sum_to = before;
+            int word = -1, heavy = -1;
+            for (int j = 0; j < m; ++j) {
+                Four<T, FEW> fp, fq;
+                fp.load(p, v0 + 4 * j, V);
+                fq.load(q, v0 + 4 * j, V);
+                weights(fp, fq, less, v0 + 4 * j, V, x);
+                const int first = Four<T, FEW>::first(v0 + 4 * j, V);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sum_to += x[e];
+                    if (x[e] > 0.0) {
+                        heavy = first + e;
+                        if (word < 0 && sum_to > at) word = heavy;
+                    }
+                }
+            }
+            const unsigned long long passed = __ballot(word >= 0), heavies = __ballot(heavy >= 0);
+            if (passed) word = __shfl(word, __builtin_ctzll(passed));
+            else word = __shfl(heavy, 63 - __builtin_clzll(heavies));
+            if (lane == 0) tokens[take] = word;
+            return;
         }
-        s_segment = found < 0 ? last : found;
-        s_before = found < 0 ? last_before : found_before;
+        less = false;
+        __syncthreads();                                   // before the sums are written again
     }
-    __syncthreads();
-    if (w != 0) return;
-    const float r = a.r[b];
-    const double at = r > 0.f ? (double)r * total : 0.0;
-    const int begin = s_segment * size, end = min(V, begin + size);
-    double before = s_before;
-    int word = -1;                                         // the last word with a weight, until one passes
-    for (int v0 = begin; v0 < end; v0 += 64) {
-        const int v = v0 + lane;
-        const double x = v < end ? weight(p, q, v) : 0.0;
-        const double upto = before + wave_scan_f64(x, lane);
-        const unsigned long long pass = __ballot(x > 0.0 && upto > at), any = __ballot(x > 0.0);
-        if (pass) {
-            word = v0 + __builtin_ctzll(pass);
-            break;
-        }
-        if (any) word = v0 + 63 - __builtin_clzll(any);
-        before = __shfl(upto, 63);
-    }
-    if (lane == 0) tokens[take] = word;
 }
 
 static echo_status_t check_draft(const echo_draft_desc_t *d) {
@@ -165,8 +243,9 @@ echo_status_t echo_draft_verify(const echo_draft_desc_t *desc, const int32_t *dr
     const DraftArgs a{drafted, n_drafted, draft, target, u, r, desc->B, desc->K, desc->V, tokens, taken};
     hipStream_t st = static_cast<hipStream_t>(stream);
     LaunchRecord rec = launch_begin("draft_verify", st);
-    if (desc->dtype == ECHO_F32) k_draft_verify<float><<<desc->B, 64 * kDraftWaves, 0, st>>>(a);
-    else k_draft_verify<bf16_t><<<desc->B, 64 * kDraftWaves, 0, st>>>(a);
+    const bool few = desc->V < 4;
+    if (desc->dtype == ECHO_F32) (few ? k_draft_verify<float, true> : k_draft_verify<float, false>)<<<desc->B, 64 * kDraftWaves, 0, st>>>(a);
+    else (few ? k_draft_verify<bf16_t, true> : k_draft_verify<bf16_t, false>)<<<desc->B, 64 * kDraftWaves, 0, st>>>(a);
     return launch_end(rec);
 }
 
