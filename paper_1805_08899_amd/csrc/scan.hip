@@ -1,9 +1,9 @@
 // A gated linear recurrence over whole sequences, forward and backward (include/echoscan.h has the formulas).
 //
 // A thread owns kSteps consecutive steps of VEC channels; 16 such threads stand side by side, GROUPS of them one behind the other, and together take
-// GROUPS kSteps steps of 16 VEC channels (a unit).  A thread's steps are a linear map of the state, c -> A c + b (backward: q -> A q + R): a wave folds
-// the GROUPS maps of each channel through LDS, and every thread goes over its steps once more from the state in front of them.  A sequence longer
-// than a unit is taken unit by unit.
+// GROUPS kSteps steps of 16 VEC channels.  A thread's steps are a linear map of the state, c -> A c + b (backward: q -> A q + R).  A wave folds the maps of
+// its four groups in LDS, a lane per channel, and every wave those of the waves in front of it; from the state in front of its own, every thread goes on
+// by itself.  A sequence longer than a chunk is a chain of them (below).
 //
 // With u = 1 - f = sigmoid(-x):  c += u (g - c),  r = dh o + q,  q = r - u r  keep the digits of a u next to zero.
 #include "../../include/echoscan.h"
@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 #include "common.hpp"
 #include "launch.hpp"
@@ -87,377 +88,276 @@ struct ScanArgs {
     const float *first;              // c0; dc_last
     const int *len;
     int B, T, H, reverse, chunks, groups_h;   // groups_h: units along the channels
-    long long chains, units, chain0; // B groups_h; chains by chunks; the launch's first
+    long long chains, chain0;        // B groups_h; the launch's first
     void *out;                       // h; dG
     float *last;                     // c_last; dc0
     float *states;
-    unsigned long long *words, *tickets;      // [units][WIDTH]; [queues], kTicketStride apart: the next to be taken
+    unsigned long long *words, *tickets;      // [chunks][chains][WIDTH]; [queues], kTicketStride apart: the next to be taken
     int queues;
     bool whole;                      // rows are whole groups of 16 bytes
 };
 
-// What a thread is in a unit
+// What a thread is in a unit: its channels of a sequence, kSteps steps of a chunk
 template <int VEC, int GROUPS> struct Place {
     static constexpr int SUBS = kThreads<GROUPS> / 16 / GROUPS, WIDTH = 16 * VEC;
-    int group, sub, slot, b, base, ch, skip, chunk, s0;    // skip: of its VEC channels, those in front that are the neighbour's
+    int group, sub, slot, b, ch, skip, s0;                 // skip: of its VEC channels, those in front that are the neighbour's
     bool on;                         // it has channels of its own
     int n;                           // steps of the sequence
-    long long chain;
-    __device__ __forceinline__ Place(const ScanArgs &a, long long unit, int chunk_) : chunk(chunk_) {
-        const int lane16 = threadIdx.x & 15;
+    __device__ __forceinline__ Place(const ScanArgs &a, long long first_chain, int chunk) {
         group = (threadIdx.x >> 4) % GROUPS;
-        sub = (threadIdx.x >> 4) / GROUPS;
-        chain = min(unit + sub, a.chains - 1);
+        sub = SUBS == 1 ? 0 : (threadIdx.x >> 4) / GROUPS;
+        const long long chain = min(first_chain + sub, a.chains - 1);
         b = (int)(chain / a.groups_h);
-        base = (int)(chain - (long long)b * a.groups_h) * WIDTH;
-        slot = lane16 * VEC;
-        on = unit + sub < a.chains && base + slot < a.H;
-        ch = min(base + slot, a.H - VEC);                  // the last lane steps back to a whole group of channels
-        skip = base + slot - ch;
+        channels(a, (int)(chain - (long long)b * a.groups_h), first_chain + sub < a.chains);
         n = a.len ? clamp_len(a.len[b], a.T) : a.T;
         s0 = (chunk * GROUPS + group) * kSteps;
+    }
+    __device__ __forceinline__ Place(const ScanArgs &a, int b_, int g, int n_, int chunk) : sub(0), b(b_), n(n_) {
+        static_assert(SUBS == 1, "a chunk of one chain");
+        group = (threadIdx.x >> 4) % GROUPS;
+        channels(a, g, true);
+        s0 = (chunk * GROUPS + group) * kSteps;
+    }
+    __device__ __forceinline__ void channels(const ScanArgs &a, int g, bool there) {
+        slot = (threadIdx.x & 15) * VEC;
+        on = there && g * WIDTH + slot < a.H;
+        ch = min(g * WIDTH + slot, a.H - VEC);             // the last lane steps back to a whole group of channels
+        skip = g * WIDTH + slot - ch;
     }
     __device__ __forceinline__ bool in(int i) const { return s0 + i < n; }
     // position of the thread's step i; steps from n on stand at their own number
     __device__ __forceinline__ int position(const ScanArgs &a, int i) const { return a.reverse && in(i) ? n - 1 - s0 - i : s0 + i; }
 };
 
-// What a lane is where a wave folds the maps of unit w: a channel each
-template <int VEC, int GROUPS> struct Folder {
-    typedef Place<VEC, GROUPS> P;
+// What a lane is where a wave folds maps: a channel
+template <int VEC> struct Folder {
+    static constexpr int WIDTH = 16 * VEC;
     int lane, ch;
-    bool on, own;
-    size_t row, state;               // of c0 and c_last; of the kept states
-    long long chain;
-    __device__ __forceinline__ Folder(const ScanArgs &a, long long unit, int w, int chunk) {
-        lane = lane_id();
-        chain = min(unit + w, a.chains - 1);
-        const int b = (int)(chain / a.groups_h), c = (int)(chain - (long long)b * a.groups_h) * P::WIDTH + lane / VEC * VEC;
-        on = w < P::SUBS && lane < P::WIDTH;
+    bool on, own;                    // it is one; the unit's own
+    size_t row;                      // of c0 and c_last
+    __device__ __forceinline__ Folder(const ScanArgs &a, int b, int g, bool there) {
+        lane = lane_id() % WIDTH;
+        const int c = g * WIDTH + lane / VEC * VEC;
         ch = max(0, min(c, a.H - VEC)) + lane % VEC;
-        own = on && unit + w < a.chains && c < a.H && ch >= c;
+        on = lane_id() < WIDTH;
+        own = on && there && c < a.H && ch >= c;
         row = (size_t)b * a.H + ch;
-        state = ((size_t)b * a.chunks + chunk) * a.H + ch;
+    }
+};
+// a wave's own exchange through LDS
+__device__ __forceinline__ void settle() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// The maps of a wave's four groups, a lane per channel, and of all four; BACK: in their order backwards
+template <int WIDTH, bool BACK> struct FourMaps {
+    float A[4], b[4];
+    static __device__ __forceinline__ int order(int k) { return BACK ? 3 - k : k; }
+    __device__ __forceinline__ void read(const float (*sa)[WIDTH], const float (*sb)[WIDTH], int lane) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) A[k] = sa[order(k)][lane], b[k] = sb[order(k)][lane];
+    }
+    __device__ __forceinline__ void total(float &all, float &sum) const {
+        all = A[0], sum = b[0];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) sum = __builtin_fmaf(A[k], sum, b[k]), all *= A[k];
+    }
+    // the state in front of each group takes the place of its b; the one behind all is returned
+    __device__ __forceinline__ float write(float (*sb)[WIDTH], int lane, float state) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sb[order(k)][lane] = state;
+            state = __builtin_fmaf(A[k], state, b[k]);
+        }
+        return state;
+    }
+};
+// The maps of W waves
+template <int WIDTH, int W, bool BACK> struct WaveMaps {
+    float A[W], b[W];
+    static __device__ __forceinline__ int order(int k) { return BACK ? W - 1 - k : k; }
+    __device__ __forceinline__ void read(const float (&sa)[W][WIDTH], const float (&sb)[W][WIDTH], int lane) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) A[k] = sa[order(k)][lane], b[k] = sb[order(k)][lane];
+    }
+    __device__ __forceinline__ void total(float &all, float &sum) const {
+        all = A[0], sum = b[0];
+#pragma unroll
+        for (int k = 1; k < W; ++k) sum = __builtin_fmaf(A[k], sum, b[k]), all *= A[k];
+    }
+    // the state in front of wave w
+    __device__ __forceinline__ float state(float start, int w) const {
+#pragma unroll
+        for (int k = 0; k < W - 1; ++k)
+            if (k < order(w)) start = __builtin_fmaf(A[k], start, b[k]);
+        return start;
     }
 };
 
-// ---- chains ---------------------------------------------------------------------------------------------------------------
-// The chunks of a sequence's channels are a chain: each hands the state behind it to the next.  A chunk publishes its map (A, b) as soon as it has it, and the
-// state behind it (C) as soon as it knows the one in front of it; the next one takes C from the chunk in front, or from one up to kLookBack in front and applies
-// the maps of those between, in order, with the same operation that each of them applies to its own: results do not depend on how far it looked.
-// Map and state go out in one 64-bit word, b or C below and above it A, which is 0 to 1 and leaves the upper two bits for what it is (A that is NaN comes with
-// a b that is), so that nothing has to be waited for in between; the words are cleared in front of the launch.
-// Units are taken by ticket, chunk after chunk: whoever waits, waits for a unit that has been taken already and waits for lower tickets only.  The chains are
-// dealt to up to kQueues queues with a ticket counter and blocks each: one counter for all gives out a ticket every 15 to 20 ns, no matter who asks
-// (4 x 16384 x 1280 bf16, forward: 181 us of 10240 tickets).
-struct Queue {
-    unsigned *ticket;
-    long long first;                 // chain; neighbours are one queue's, and with it one XCD's: they share cache lines where rows are not whole ones
-    int chains;
-    __device__ __forceinline__ Queue(const ScanArgs &a) {
-        const int q = (int)blockIdx.x % a.queues;
-        ticket = reinterpret_cast<unsigned *>(a.tickets + q * kTicketStride);
-        first = a.chains * q / a.queues;
-        chains = (int)(a.chains * (q + 1) / a.queues - first);
-    }
-    __device__ __forceinline__ unsigned take() const { return atomicAdd(ticket, 1u); }
-    // the unit of a ticket: link of the chain, chain; false: there is none
-    __device__ __forceinline__ bool unit(unsigned t, int links, int &link, long long &chain) const {
-        link = (int)(t / (unsigned)chains);
-        chain = first + (t - (unsigned)link * chains);
-        return link < links;
-    }
-};
-typedef unsigned long long Word;
-constexpr Word kMapMark = 1ull << 62, kStateMark = 1ull << 63;
-__device__ __forceinline__ Word map_word(float A, float b) {
-    return kMapMark | (Word)(__float_as_uint(A) & 0x3fffffffu) << 32 | __float_as_uint(b);
-}
-__device__ __forceinline__ Word state_word(float c) { return kStateMark | __float_as_uint(c); }
-__device__ __forceinline__ float factor_of(Word w) { return __uint_as_float((unsigned)(w >> 32) & 0x3fffffffu); }
-__device__ __forceinline__ float value_of(Word w) { return __uint_as_float((unsigned)w); }
-
-// The state in front of this chunk from the words of the W chunks in front of it (`ahead` of them exist), a lane per channel; false: it can't be told yet.
-// `back`: words from a chunk's to those of the one in front of it.
-template <int W> __device__ __forceinline__ bool look_back(const Word *unit, int lane, long long back, int ahead, float &carry) {
-    Word w[W];
-#pragma unroll
-    for (int d = 0; d < W; ++d) w[d] = load_agent(unit - (min(d, ahead - 1) + 1) * back + lane);
-    int from = -1;                                         // the nearest chunk whose state is there, the maps of all nearer ones being there
-    bool maps = true;
-#pragma unroll
-    for (int d = 0; d < W; ++d) {
-        if (from < 0 && maps && d < ahead && __all((w[d] & kStateMark) != 0)) from = d;
-        maps = maps && __all((w[d] & kMapMark) != 0);
-    }
-    if (from < 0) return false;
-#pragma unroll
-    for (int d = W - 1; d >= 0; --d) {
-        if (d == from) carry = value_of(w[d]);
-        else if (d < from) carry = __builtin_fmaf(factor_of(w[d]), carry, value_of(w[d]));
-    }
-    return true;
-}
-// Publishes this chunk's map, returns the state in front of it (`start` if it is the first) and publishes the one behind it.
-template <int W> __device__ __forceinline__ float chain_carry(Word *unit, int lane, long long back, int ahead, float start, float A, float b) {
-    float carry = start;
-    if (ahead > 0) {
-        store_agent(unit + lane, map_word(A, b));
-        const long long t0 = wall_clock64();
-        while (!look_back<W>(unit, lane, back, ahead, carry)) {
-            if (wall_clock64() - t0 > kSpinLimitTicks) {
-                carry = __builtin_nanf("");                // make the failure visible
-                break;
-            }
+// A thread's rows.  FULL: all steps of the unit are the sequence's, and all of its addresses are one 32-bit offset behind scalar ones.
+template <typename T, bool FULL> struct Row {
+    T *base;
+    unsigned off;                    // bytes
+    int step;                        // elements from step to step
+    // rows of `width` elements, of which the thread's channels of array k stand `between` elements behind those of array k - 1
+    template <typename P> __device__ __forceinline__ Row(const ScanArgs &a, const void *array, int width, const P &p, int chunk) {
+        base = (T *)array + (size_t)p.b * a.T * width;
+        if constexpr (FULL) {
+            const int low = a.reverse ? p.n - (chunk + 1) * ECHO_SCAN_CHUNK : chunk * ECHO_SCAN_CHUNK;
+            base += (size_t)low * width;
+            step = a.reverse ? -width : width;
+            // (at most 127 rows of 3 2^20 elements: 2^31 bytes)
+            off = ((unsigned)(a.reverse ? ECHO_SCAN_CHUNK - 1 - p.group * kSteps : p.group * kSteps) * (unsigned)width + (unsigned)p.ch) * (unsigned)sizeof(T);
+        } else {
+            base += p.ch;
         }
     }
-    store_agent(unit + lane, state_word(__builtin_fmaf(factor_of(map_word(A, b)), carry, b)));
-    return carry;
+    template <typename P> __device__ __forceinline__ T *at(const ScanArgs &a, const P &p, int i, int width, int behind, bool load) const {
+        if constexpr (FULL) return (T *)((const char *)(base + ((long long)i * step + behind)) + off);
+        else return base + (size_t)(load && !p.in(i) ? 0 : p.position(a, i)) * width + behind;
+    }
+};
+
+// A wave's channels where there are no chains: of its unit, which GROUPS / 4 waves share
+template <int VEC, int GROUPS> __device__ __forceinline__ Folder<VEC> wave_folder(const ScanArgs &a, long long first_chain) {
+    const long long mine = first_chain + wave_id() / (GROUPS / 4), chain = min(mine, a.chains - 1);
+    const int b = (int)(chain / a.groups_h);
+    return Folder<VEC>(a, b, (int)(chain - (long long)b * a.groups_h), mine < a.chains);
 }
 
-__global__ __launch_bounds__(256) void k_scan_clear(u32x4_any *p, long long n) {
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = u32x4_any{0u, 0u, 0u, 0u};
-}
-
-template <typename T, int VEC, int GROUPS, bool CHAIN>
+// ---- one chunk ---------------------------------------------------------------------------------------------------------------
+template <typename T, int VEC, int GROUPS>
 __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs a) {
     typedef Place<VEC, GROUPS> P;
-    __shared__ float s_a[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH], s_b[CHAIN ? 2 : 1][P::SUBS][GROUPS][P::WIDTH];
-    __shared__ unsigned s_ticket[2];
-    const int w = wave_id();
-    const Queue queue(a);
-    unsigned ticket = 0;
-    int buf = 0;
-    if constexpr (CHAIN) {
-        if (threadIdx.x == 0) s_ticket[1] = queue.take();
-        __syncthreads();
-        ticket = __builtin_amdgcn_readfirstlane(s_ticket[1]);
+    constexpr int ALL = P::SUBS * GROUPS, W = GROUPS / 4;
+    __shared__ float s_a[ALL][P::WIDTH], s_b[ALL][P::WIDTH], s_wa[W > 1 ? W : 1][P::WIDTH], s_wb[W > 1 ? W : 1][P::WIDTH];
+    const int w = wave_id(), own = threadIdx.x >> 4;       // the thread's group in the block
+    const long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
+    const P p(a, first_chain, 0);
+    const Row<const T, false> G(a, a.G, 3 * a.H, p, 0);
+    const Row<T, false> h(a, a.out, a.H, p, 0);
+    Lanes<T, VEC> x[kSteps][3];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) x[i][k].load(G.at(a, p, i, 3 * a.H, k * a.H, true));
+    float c[VEC];
+    if constexpr (GROUPS == 1) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) c[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
+        if (a.states && p.on) {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v)
+                if (v >= p.skip) a.states[(size_t)p.b * a.H + p.ch + v] = c[v];
+        }
     }
-    for (;;) {
-        int link = 0;
-        long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
-        if (CHAIN && !queue.unit(ticket, a.chunks, link, first_chain)) break;
-        unsigned next = 0;
-        if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
-        const int chunk = link;
-        const P p(a, first_chain, chunk);
-        const size_t row = (size_t)p.b * a.T;
-        const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
-        T *h = static_cast<T *>(a.out) + row * a.H + p.ch;
-        Lanes<T, VEC> x[kSteps][3];
+    float u[kSteps][VEC], g[kSteps][VEC];
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const size_t at = (size_t)(p.in(i) ? p.position(a, i) : 0) * 3 * a.H;
+    for (int i = 0; i < kSteps; ++i) {
+        float y[VEC];
+        x[i][0].get(y);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) x[i][k].load(G + at + (size_t)k * a.H);
-        }
-        float c[VEC];
-        if constexpr (GROUPS == 1) {
+        for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
+        x[i][1].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) c[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
-            if (a.states && p.on) {
+        for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
+    }
+    if constexpr (GROUPS > 1) {
 #pragma unroll
-                for (int v = 0; v < VEC; ++v)
-                    if (v >= p.skip) a.states[(size_t)p.b * a.H + p.ch + v] = c[v];
+        for (int v = 0; v < VEC; ++v) {
+            float A = 1.f, b = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
+                A = __builtin_fmaf(-u[i][v], A, A);
             }
+            s_a[own][p.slot + v] = A;
+            s_b[own][p.slot + v] = b;
         }
-        float u[kSteps][VEC], g[kSteps][VEC];
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            float y[VEC];
-            x[i][0].get(y);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
-            x[i][1].get(y);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
-        }
-        if constexpr (GROUPS > 1) {
-            float A[VEC], b[VEC];
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                A[v] = 1.f, b[v] = 0.f;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    b[v] = __builtin_fmaf(u[i][v], g[i][v] - b[v], b[v]);
-                    A[v] = __builtin_fmaf(-u[i][v], A[v], A[v]);
-                }
-                s_a[buf][p.sub][p.group][p.slot + v] = A[v];
-                s_b[buf][p.sub][p.group][p.slot + v] = b[v];
-            }
+        const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
+        float state = a.first ? a.first[f.row] : 0.f;
+        if (a.states && f.own && w % W == 0) a.states[f.row] = state;
+        settle();
+        FourMaps<P::WIDTH, false> m;
+        m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+        if constexpr (W > 1) {
+            float all, sum;
+            m.total(all, sum);
+            if (f.on) s_wa[w][f.lane] = all, s_wb[w][f.lane] = sum;
             lds_barrier();
-            if (w < P::SUBS) {
-                const Folder<VEC, GROUPS> f(a, first_chain, w, chunk);
-                if (f.on) {
-                    float(&fa)[GROUPS][P::WIDTH] = s_a[buf][w], (&fb)[GROUPS][P::WIDTH] = s_b[buf][w];
-                    float state = (!CHAIN || chunk == 0) && a.first ? a.first[f.row] : 0.f;
-                    if constexpr (CHAIN) {
-                        float all = 1.f, sum = 0.f;
-#pragma unroll 4
-                        for (int k = 0; k < GROUPS; ++k) {
-                            sum = __builtin_fmaf(fa[k][f.lane], sum, fb[k][f.lane]);
-                            all *= fa[k][f.lane];
-                        }
-                        state = chain_carry<8>(a.words + (link * a.chains + f.chain) * P::WIDTH, f.lane, a.chains * P::WIDTH, chunk, state, all, sum);
-                    }
-                    if (a.states && f.own) a.states[f.state] = state;
-#pragma unroll 4
-                    for (int k = 0; k < GROUPS; ++k) {
-                        const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
-                        fb[k][f.lane] = state;
-                        state = x;
-                    }
-                    if (a.last && f.own && chunk == a.chunks - 1) a.last[f.row] = state;
-                }
-            }
-            if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
-            lds_barrier();
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) c[v] = s_b[buf][p.sub][p.group][p.slot + v];
+            WaveMaps<P::WIDTH, W, false> wm;
+            wm.read(s_wa, s_wb, f.lane);
+            state = wm.state(state, w);
         }
+        if (f.on) state = m.write(s_b + 4 * w, f.lane, state);
+        if (a.last && f.own && w % W == W - 1) a.last[f.row] = state;
+        settle();
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            float y[VEC];
-            x[i][2].get(y);
+        for (int v = 0; v < VEC; ++v) c[v] = s_b[own][p.slot + v];
+    }
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
-                y[v] = p.in(i) ? gate(y[v]) * c[v] : 0.f;
-            }
-            if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h + (size_t)p.position(a, i) * a.H, y, p.skip, a.whole);
+    for (int i = 0; i < kSteps; ++i) {
+        float y[VEC];
+        x[i][2].get(y);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
+            y[v] = p.in(i) ? gate(y[v]) * c[v] : 0.f;
         }
-        if constexpr (GROUPS == 1) {
-            if (a.last && p.on) {
+        if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h.at(a, p, i, a.H, 0, false), y, p.skip, a.whole);
+    }
+    if constexpr (GROUPS == 1) {
+        if (a.last && p.on) {
 #pragma unroll
-                for (int v = 0; v < VEC; ++v)
-                    if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = c[v];
-            }
+            for (int v = 0; v < VEC; ++v)
+                if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = c[v];
         }
-        if constexpr (!CHAIN) break;
-        ticket = __builtin_amdgcn_readfirstlane(s_ticket[buf]);
-        buf ^= 1;
     }
 }
 
-template <typename T, int VEC, int GROUPS, bool CHAIN>
-__global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs a) {
-    typedef Place<VEC, GROUPS> P;
-    constexpr int BUFS = CHAIN ? 2 : 1;
-    __shared__ float s_a[BUFS][P::SUBS][GROUPS][P::WIDTH], s_b[BUFS][P::SUBS][GROUPS][P::WIDTH], s_r[BUFS][P::SUBS][GROUPS][P::WIDTH];
-    __shared__ unsigned s_ticket[2];
-    const int w = wave_id();
-    const Queue queue(a);
-    unsigned ticket = 0;
-    int buf = 0;
-    if constexpr (CHAIN) {
-        if (threadIdx.x == 0) s_ticket[1] = queue.take();
-        __syncthreads();
-        ticket = __builtin_amdgcn_readfirstlane(s_ticket[1]);
-    }
-    for (;;) {
-        int link = 0;
-        long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
-        if (CHAIN && !queue.unit(ticket, a.chunks, link, first_chain)) break;
-        unsigned next = 0;
-        if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
-        const int chunk = a.chunks - 1 - link;             // from the last one on
-        const P p(a, first_chain, chunk);
-        const size_t row = (size_t)p.b * a.T;
-        const T *G = static_cast<const T *>(a.G) + row * 3 * a.H + p.ch;
-        const T *dh = static_cast<const T *>(a.dh) + row * a.H + p.ch;
-        T *dG = static_cast<T *>(a.out) + row * 3 * a.H + p.ch;
+// A thread's kSteps steps backwards: its gates and dh (u = g = o = d = 0 at steps that are none of the sequence's)
+template <int VEC> struct Back {
+    float u[kSteps][VEC], g[kSteps][VEC], o[kSteps][VEC], d[kSteps][VEC];
+    template <bool FULL, typename T, typename P>
+    __device__ __forceinline__ void load(const ScanArgs &a, const P &p, const Row<const T, FULL> &G, const Row<const T, FULL> &dh) {
         Lanes<T, VEC> x[kSteps][3], up[kSteps];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            const size_t at = p.in(i) ? p.position(a, i) : 0;
 #pragma unroll
-            for (int k = 0; k < 3; ++k) x[i][k].load(G + (at * 3 + k) * a.H);
-            up[i].load(dh + at * a.H);
+            for (int k = 0; k < 3; ++k) x[i][k].load(G.at(a, p, i, 3 * a.H, k * a.H, true));
+            up[i].load(dh.at(a, p, i, a.H, 0, true));
         }
-        float c[VEC], q[VEC];
-        if constexpr (GROUPS == 1) {
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                c[v] = a.states[(size_t)p.b * a.H + p.ch + v];
-                q[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
-            }
-        }
-        float u[kSteps][VEC], g[kSteps][VEC], o[kSteps][VEC], d[kSteps][VEC];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
+            const bool in = FULL || p.in(i);
             float y[VEC];
             x[i][0].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) u[i][v] = in ? forget_rest(y[v]) : 0.f;
             x[i][1].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) g[i][v] = in ? candidate(y[v]) : 0.f;
             x[i][2].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) o[i][v] = p.in(i) ? gate(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) o[i][v] = in ? gate(y[v]) : 0.f;
             up[i].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) d[i][v] = p.in(i) ? y[v] : 0.f;
+            for (int v = 0; v < VEC; ++v) d[i][v] = in ? y[v] : 0.f;
         }
-        if constexpr (GROUPS > 1) {
+    }
+    // the maps of the state, forwards, and of q, backwards, which share the factor
+    __device__ __forceinline__ void maps(int v, float &A, float &b, float &R) const {
+        A = 1.f, b = 0.f, R = 0.f;
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                float A = 1.f, b = 0.f, R = 0.f;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
-                    A = __builtin_fmaf(-u[i][v], A, A);
-                    const int k = kSteps - 1 - i;
-                    const float r = __builtin_fmaf(d[k][v], o[k][v], R);
-                    R = __builtin_fmaf(-u[k][v], r, r);
-                }
-                s_a[buf][p.sub][p.group][p.slot + v] = A;
-                s_b[buf][p.sub][p.group][p.slot + v] = b;
-                s_r[buf][p.sub][p.group][p.slot + v] = R;
-            }
-            lds_barrier();
-            // the states in front of the groups, and behind them f r of the next step: two waves' work in a chain, otherwise one's
-            if (w < (CHAIN ? 2 : P::SUBS)) {
-                const int sub = CHAIN ? 0 : w;
-                const Folder<VEC, GROUPS> f(a, first_chain, sub, chunk);
-                float(&fa)[GROUPS][P::WIDTH] = s_a[buf][sub], (&fb)[GROUPS][P::WIDTH] = s_b[buf][sub], (&fr)[GROUPS][P::WIDTH] = s_r[buf][sub];
-                if (f.on && (!CHAIN || w == 0)) {
-                    float state = a.states[f.state];
-#pragma unroll 4
-                    for (int k = 0; k < GROUPS; ++k) {
-                        const float x = __builtin_fmaf(fa[k][f.lane], state, fb[k][f.lane]);
-                        fb[k][f.lane] = state;
-                        state = x;
-                    }
-                }
-                if (f.on && (!CHAIN || w == 1)) {
-                    float back = (!CHAIN || link == 0) && a.first ? a.first[f.row] : 0.f;
-                    if constexpr (CHAIN) {
-                        float all = 1.f, sum = 0.f;
-#pragma unroll 4
-                        for (int k = GROUPS - 1; k >= 0; --k) {
-                            sum = __builtin_fmaf(fa[k][f.lane], sum, fr[k][f.lane]);
-                            all *= fa[k][f.lane];
-                        }
-                        back = chain_carry<4>(a.words + (link * a.chains + f.chain) * P::WIDTH, f.lane, a.chains * P::WIDTH, link, back, all, sum);
-                    }
-#pragma unroll 4
-                    for (int k = GROUPS - 1; k >= 0; --k) {
-                        const float x = __builtin_fmaf(fa[k][f.lane], back, fr[k][f.lane]);
-                        fr[k][f.lane] = back;
-                        back = x;
-                    }
-                    if (a.last && f.own && chunk == 0) a.last[f.row] = back;
-                }
-            }
-            if (CHAIN && threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
-            lds_barrier();
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                c[v] = s_b[buf][p.sub][p.group][p.slot + v];
-                q[v] = s_r[buf][p.sub][p.group][p.slot + v];
-            }
+        for (int i = 0; i < kSteps; ++i) {
+            b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
+            A = __builtin_fmaf(-u[i][v], A, A);
+            const int k = kSteps - 1 - i;
+            const float r = __builtin_fmaf(d[k][v], o[k][v], R);
+            R = __builtin_fmaf(-u[k][v], r, r);
         }
+    }
+    // dG from the state in front of the thread's steps and the q behind them; q: that in front of them
+    template <bool FULL, typename T, typename P>
+    __device__ __forceinline__ void store(const ScanArgs &a, const P &p, const Row<T, FULL> &dG, float (&c)[VEC], float (&q)[VEC]) const {
         float before[kSteps][VEC];
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
@@ -474,29 +374,452 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
             for (int v = 0; v < VEC; ++v) {
                 const float r = __builtin_fmaf(d[i][v], o[i][v], q[v]);
                 const float ru = r * u[i][v];
-                df[v] = ru * (1.f - u[i][v]) * (before[i][v] - g[i][v]);
+                df[v] = __builtin_fmaf(-ru, u[i][v], ru) * (before[i][v] - g[i][v]);
                 dg[v] = ru * __builtin_fmaf(-g[i][v], g[i][v], 1.f);
-                dout[v] = d[i][v] * c[v] * o[i][v] * (1.f - o[i][v]);
+                dout[v] = d[i][v] * c[v] * __builtin_fmaf(-o[i][v], o[i][v], o[i][v]);
                 c[v] = before[i][v];
                 q[v] = r - ru;
             }
-            if (p.on && p.s0 + i < a.T) {
-                T *to = dG + (size_t)p.position(a, i) * 3 * a.H;
-                put_from<T, VEC>(to, df, p.skip, a.whole);
-                put_from<T, VEC>(to + a.H, dg, p.skip, a.whole);
-                put_from<T, VEC>(to + 2 * (size_t)a.H, dout, p.skip, a.whole);
+            if (p.on && (FULL || p.s0 + i < a.T)) {
+                put_from<T, VEC>(dG.at(a, p, i, 3 * a.H, 0, false), df, p.skip, a.whole);
+                put_from<T, VEC>(dG.at(a, p, i, 3 * a.H, a.H, false), dg, p.skip, a.whole);
+                put_from<T, VEC>(dG.at(a, p, i, 3 * a.H, 2 * a.H, false), dout, p.skip, a.whole);
             }
         }
-        if constexpr (GROUPS == 1) {
-            if (a.last && p.on) {
+    }
+};
+
+template <typename T, int VEC, int GROUPS>
+__global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs a) {
+    typedef Place<VEC, GROUPS> P;
+    constexpr int ALL = P::SUBS * GROUPS, W = GROUPS / 4, WS = W > 1 ? W : 1;
+    __shared__ float s_a[ALL][P::WIDTH], s_b[ALL][P::WIDTH], s_r[ALL][P::WIDTH], s_wa[WS][P::WIDTH], s_wb[WS][P::WIDTH], s_wr[WS][P::WIDTH];
+    const int w = wave_id(), own = threadIdx.x >> 4;       // the thread's group in the block
+    const long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
+    const P p(a, first_chain, 0);
+    Back<VEC> x;
+    x.template load<false, T>(a, p, Row<const T, false>(a, a.G, 3 * a.H, p, 0), Row<const T, false>(a, a.dh, a.H, p, 0));
+    float c[VEC], q[VEC];
+    if constexpr (GROUPS == 1) {
 #pragma unroll
-                for (int v = 0; v < VEC; ++v)
-                    if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = q[v];
+        for (int v = 0; v < VEC; ++v) {
+            c[v] = a.states[(size_t)p.b * a.H + p.ch + v];
+            q[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) x.maps(v, s_a[own][p.slot + v], s_b[own][p.slot + v], s_r[own][p.slot + v]);
+        const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
+        float state = a.states[f.row], back = a.first ? a.first[f.row] : 0.f;
+        settle();
+        FourMaps<P::WIDTH, false> m;
+        FourMaps<P::WIDTH, true> r;
+        m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+        r.read(s_a + 4 * w, s_r + 4 * w, f.lane);
+        if constexpr (W > 1) {
+            float all, sum, rest;
+            m.total(all, sum);
+            r.total(all, rest);
+            if (f.on) s_wa[w][f.lane] = all, s_wb[w][f.lane] = sum, s_wr[w][f.lane] = rest;
+            lds_barrier();
+            WaveMaps<P::WIDTH, W, false> wm;
+            wm.read(s_wa, s_wb, f.lane);
+            state = wm.state(state, w);
+            WaveMaps<P::WIDTH, W, true> wr;
+            wr.read(s_wa, s_wr, f.lane);
+            back = wr.state(back, w);
+        }
+        if (f.on) {
+            m.write(s_b + 4 * w, f.lane, state);
+            back = r.write(s_r + 4 * w, f.lane, back);
+        }
+        if (a.last && f.own && w % W == 0) a.last[f.row] = back;
+        settle();
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            c[v] = s_b[own][p.slot + v];
+            q[v] = s_r[own][p.slot + v];
+        }
+    }
+    x.template store<false, T>(a, p, Row<T, false>(a, a.out, 3 * a.H, p, 0), c, q);
+    if constexpr (GROUPS == 1) {
+        if (a.last && p.on) {
+#pragma unroll
+            for (int v = 0; v < VEC; ++v)
+                if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = q[v];
+        }
+    }
+}
+
+// ---- chains of chunks -----------------------------------------------------------------------------------------------------------
+// The chunks of a sequence's channels are a chain, up to the one that holds its last step: each hands the state behind it to the next.  A chunk publishes its map
+// (A, b) as soon as it has it, and the state behind it (C) as soon as it knows the one in front of it; the next one takes C from the chunk in front, or from one up
+// to kLookBack in front and applies the maps of those between, in order, with the same operation that each of them applies to its own: results do not
+// depend on how far it looked.  Map and state go out in one 64-bit word, b or C below and above it A, which is 0 to 1 and leaves the upper two bits for
+// what it is (A that is NaN comes with a b that is), so that nothing has to be waited for in between; the words are cleared in front of the launch.
+// Units are taken by ticket, chunk after chunk: whoever waits, waits for a unit that has been taken already and waits for lower tickets only.  The chains are
+// dealt to up to kQueues queues with a ticket counter and blocks each: one counter for all gives out a ticket every 15 to 20 ns, no matter who asks
+// (4 x 16384 x 1280 bf16, forward: 181 us of 10240 tickets).
+struct Queue {
+    unsigned *ticket;
+    unsigned first, chains;          // chain; neighbours are one queue's, and with it one XCD's: they share cache lines where rows are not whole ones
+    __device__ __forceinline__ Queue(const ScanArgs &a) {
+        const int q = (int)(blockIdx.x % (unsigned)a.queues);
+        ticket = reinterpret_cast<unsigned *>(a.tickets + q * kTicketStride);
+        first = (unsigned)(a.chains * q / a.queues);
+        chains = (unsigned)(a.chains * (q + 1) / a.queues) - first;
+    }
+    __device__ __forceinline__ unsigned take() const { return atomicAdd(ticket, 1u); }          // one lane's
+};
+typedef unsigned long long Word;
+constexpr Word kMapMark = 1ull << 62, kStateMark = 1ull << 63;
+__device__ __forceinline__ Word map_word(float A, float b) {
+    return kMapMark | (Word)(__float_as_uint(A) & 0x3fffffffu) << 32 | __float_as_uint(b);
+}
+__device__ __forceinline__ Word state_word(float c) { return kStateMark | __float_as_uint(c); }
+__device__ __forceinline__ float factor_of(Word w) { return __uint_as_float((unsigned)(w >> 32) & 0x3fffffffu); }
+__device__ __forceinline__ float value_of(Word w) { return __uint_as_float((unsigned)w); }
+
+// From the marks of the chunks in front (bit d: the one d + 1 in front): the nearest whose state is there while the maps of all nearer ones are, or -1
+__device__ __forceinline__ int nearest_state(unsigned states, unsigned maps) {
+    if (states == 0) return -1;
+    const int d = __builtin_ctz(states);
+    return (~maps & ((1u << d) - 1)) == 0 ? d : -1;
+}
+
+// How a block gets the state in front of its chunk.  One wave, a lane per channel, publishes the map and looks at the nearest four chunks; if they do not
+// tell, all eight waves look at four each, as often as it takes.
+constexpr int kLookBack = 32, kLookWaves = kThreads<kChunkGroups> / 64;
+template <int WIDTH> struct Chain {
+    float s_factor[kLookBack][WIDTH], s_value[kLookBack][WIDTH];
+    unsigned s_marks[kLookWaves];
+    int s_from;                      // -1: not known yet
+
+    // words d0 + 1 .. d0 + 4 in front; bit d of the marks: states, bit 4 + d: maps.  back: words from a chunk's to those of the one in front
+    static __device__ __forceinline__ unsigned look(const Word *unit, int lane, long long back, int d0, int ahead, Word (&w)[4]) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) w[d] = load_agent(unit - (min(d0 + d, ahead - 1) + 1) * back + lane);
+        unsigned marks = 0;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            if (d0 + d >= ahead) break;
+            if (__all((w[d] & kStateMark) != 0)) marks |= 1u << d;
+            if (__all((w[d] & kMapMark) != 0)) marks |= 16u << d;
+        }
+        return marks;
+    }
+    // The word of the chunk in front, requested early: in the middle of a long chain it has the state by the time it is wanted
+    static __device__ __forceinline__ Word early(const Word *unit, int lane, long long back, int ahead) {
+        return ahead > 0 ? load_agent(unit - back + lane) : 0;
+    }
+    // The wave's first look; `carry` is what it gives where it returns true.
+    static __device__ __forceinline__ bool first_look(Word *unit, int lane, long long back, int ahead, Word front, float A, float b, float &carry) {
+        if (ahead == 0) return true;
+        if (__all((front & kStateMark) != 0)) {
+            carry = value_of(front);
+            return true;
+        }
+        store_agent(unit + lane, map_word(A, b));
+        Word w[4];
+        const unsigned marks = look(unit, lane, back, 0, ahead, w);
+        const int from = nearest_state(marks & 15u, marks >> 4);
+        if (from < 0) return false;
+#pragma unroll
+        for (int d = 3; d >= 0; --d) {
+            if (d == from) carry = value_of(w[d]);
+            else if (d < from) carry = __builtin_fmaf(factor_of(w[d]), carry, value_of(w[d]));
+        }
+        return true;
+    }
+    // All waves: until it is known.  The values are in LDS then.
+    __device__ __forceinline__ int look_on(const Word *unit, long long back, int ahead) {
+        const int lane = lane_id(), w = wave_id();
+        const long long t0 = wall_clock64();
+        for (;;) {
+            unsigned marks = 0;
+            if (lane < WIDTH && 4 * w < ahead) {
+                Word x[4];
+                marks = look(unit, lane, back, 4 * w, ahead, x);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) s_factor[4 * w + d][lane] = factor_of(x[d]), s_value[4 * w + d][lane] = value_of(x[d]);
+            }
+            // (a chunk that never hands on is given up after kSpinLimitTicks: NaN makes the failure visible)
+            if (w == 0 && wall_clock64() - t0 > kSpinLimitTicks) {
+                marks |= 256u;
+            }
+            if (lane == 0) s_marks[w] = marks;
+            lds_barrier();
+            unsigned states = 0, maps = 0, end = 0;
+#pragma unroll
+            for (int k = 0; k < kLookWaves; ++k) {
+                const unsigned m = s_marks[k];
+                states |= (m & 15u) << 4 * k;
+                maps |= (m >> 4 & 15u) << 4 * k;
+                end |= m >> 8;
+            }
+            const int from = __builtin_amdgcn_readfirstlane(end ? kLookBack : nearest_state(states, maps));
+            if (from >= 0) return from;
+            lds_barrier();                                 // before they are written again
+        }
+    }
+    __device__ __forceinline__ float carry_from(int lane, int from) const {
+        if (from >= kLookBack) return __builtin_nanf("");
+        float carry = s_value[from][lane];
+        for (int d = from - 1; d >= 0; --d) carry = __builtin_fmaf(s_factor[d][lane], carry, s_value[d][lane]);
+        return carry;
+    }
+    static __device__ __forceinline__ void hand_on(Word *unit, int lane, float A, float carry, float b) {
+        store_agent(unit + lane, state_word(__builtin_fmaf(factor_of(map_word(A, b)), carry, b)));
+    }
+};
+
+__global__ __launch_bounds__(256) void k_scan_clear(u32x4_any *p, long long n) {
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) p[i] = u32x4_any{0u, 0u, 0u, 0u};
+}
+
+// A unit of a chain, the same for the whole block
+struct Unit {
+    int b, g, n, chunk, last;        // last: the chunk of the sequence's last step
+    unsigned chain;
+    bool there;
+    __device__ __forceinline__ Unit(const ScanArgs &a, const Queue &queue, unsigned ticket, bool backwards) {
+        const unsigned turn = ticket / queue.chains;
+        chain = queue.first + (ticket - turn * queue.chains);
+        there = turn < (unsigned)a.chunks;
+        chunk = backwards ? a.chunks - 1 - (int)turn : (int)turn;          // backwards from the last one on
+        b = (int)(chain / (unsigned)a.groups_h);
+        g = (int)(chain - (unsigned)b * (unsigned)a.groups_h);
+        n = there ? a.len ? clamp_len(a.len[b], a.T) : a.T : 0;
+        last = n > 0 ? (n - 1) / ECHO_SCAN_CHUNK : 0;
+    }
+    __device__ __forceinline__ bool full() const { return (chunk + 1) * ECHO_SCAN_CHUNK <= n; }
+};
+
+template <typename T, int VEC> struct FwdChain {
+    static constexpr int GROUPS = kChunkGroups, WIDTH = 16 * VEC;
+    typedef Place<VEC, GROUPS> P;
+    static constexpr int W = GROUPS / 4;
+    float s_a[GROUPS][WIDTH], s_b[GROUPS][WIDTH], s_wa[2][W][WIDTH], s_wb[2][W][WIDTH], s_carry[2][WIDTH];
+    Chain<WIDTH> chain;
+    int s_known[2];
+
+    template <bool FULL> __device__ __forceinline__ void run(const ScanArgs &a, const Queue &queue, Unit &unit, int buf, unsigned *s_ticket) {
+        unsigned next = 0;
+        if (threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
+        const P p(a, unit.b, unit.g, unit.n, unit.chunk);
+        Word *words = a.words + ((long long)unit.chunk * a.chains + unit.chain) * WIDTH;
+        const long long back = a.chains * WIDTH;
+        const Folder<VEC> f(a, unit.b, unit.g, true);
+        const int w = wave_id();
+        const Word front = w == 0 ? Chain<WIDTH>::early(words, f.lane, back, unit.chunk) : 0;
+        const Row<const T, FULL> G(a, a.G, 3 * a.H, p, unit.chunk);
+        Lanes<T, VEC> x[kSteps][3];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) x[i][k].load(G.at(a, p, i, 3 * a.H, k * a.H, true));
+        float A[kSteps][VEC], b[kSteps][VEC];              // the maps of the thread's first steps
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float y[VEC], z[VEC];
+            x[i][0].get(y);
+            x[i][1].get(z);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                const bool in = FULL || p.in(i);
+                const float u = in ? forget_rest(y[v]) : 0.f, g = in ? candidate(z[v]) : 0.f;
+                const float b0 = i ? b[i ? i - 1 : 0][v] : 0.f, A0 = i ? A[i ? i - 1 : 0][v] : 1.f;
+                b[i][v] = __builtin_fmaf(u, g - b0, b0);
+                A[i][v] = __builtin_fmaf(-u, A0, A0);
             }
         }
-        if constexpr (!CHAIN) break;
-        ticket = __builtin_amdgcn_readfirstlane(s_ticket[buf]);
-        buf ^= 1;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            s_a[p.group][p.slot + v] = A[kSteps - 1][v];
+            s_b[p.group][p.slot + v] = b[kSteps - 1][v];
+        }
+        float carry = w == 0 && unit.chunk == 0 && a.first ? a.first[f.row] : 0.f;
+        settle();
+        // (what is read from LDS here is read again behind the barriers: there are no registers to keep it)
+        float all, sum;
+        {
+            FourMaps<WIDTH, false> m;
+            m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+            m.total(all, sum);
+        }
+        if (f.on) s_wa[buf][w][f.lane] = all, s_wb[buf][w][f.lane] = sum;
+        lds_barrier();
+        if (w == 0) {
+            WaveMaps<WIDTH, W, false> wm;
+            wm.read(s_wa[buf], s_wb[buf], f.lane);
+            wm.total(all, sum);
+        }
+        const auto finish = [&]() __attribute__((always_inline)) {
+            if (unit.chunk < unit.last) Chain<WIDTH>::hand_on(words, f.lane, all, carry, sum);
+            s_carry[buf][f.lane] = carry;
+            if (a.states && f.own) a.states[((size_t)unit.b * a.chunks + unit.chunk) * a.H + f.ch] = carry;
+        };
+        if (w == 0 && f.on) {
+            const bool known = Chain<WIDTH>::first_look(words, f.lane, back, unit.chunk, front, all, sum, carry);
+            if (known) finish();
+            if (f.lane == 0) s_known[buf] = known;
+        }
+        if (threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
+        lds_barrier();
+        if (!__builtin_amdgcn_readfirstlane(s_known[buf])) {
+            const int from = chain.look_on(words, back, unit.chunk);
+            if (w == 0 && f.on) {
+                carry = chain.carry_from(f.lane, from);
+                finish();
+            }
+            lds_barrier();
+        }
+        if (f.on) {
+            WaveMaps<WIDTH, W, false> wm;
+            wm.read(s_wa[buf], s_wb[buf], f.lane);
+            FourMaps<WIDTH, false> m;
+            m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+            const float end = m.write(s_b + 4 * w, f.lane, wm.state(s_carry[buf][f.lane], w));
+            if (a.last && f.own && unit.chunk == unit.last && w == W - 1) a.last[f.row] = end;
+        }
+        settle();
+        const Row<T, FULL> h(a, a.out, a.H, p, unit.chunk);
+        unit = Unit(a, queue, __builtin_amdgcn_readfirstlane(s_ticket[buf]), false);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float y[VEC];
+            x[i][2].get(y);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                const float c = __builtin_fmaf(A[i][v], s_b[p.group][p.slot + v], b[i][v]);
+                y[v] = FULL || p.in(i) ? gate(y[v]) * c : 0.f;
+            }
+            if (p.on && (FULL || p.s0 + i < a.T)) put_from<T, VEC>(h.at(a, p, i, a.H, 0, false), y, p.skip, a.whole);
+        }
+    }
+};
+
+template <typename T, int VEC> struct BwdChain {
+    static constexpr int GROUPS = kChunkGroups, WIDTH = 16 * VEC;
+    typedef Place<VEC, GROUPS> P;
+    static constexpr int W = GROUPS / 4;
+    float s_a[GROUPS][WIDTH], s_b[GROUPS][WIDTH], s_r[GROUPS][WIDTH], s_wa[2][W][WIDTH], s_wb[2][W][WIDTH], s_wr[2][W][WIDTH], s_carry[2][WIDTH];
+    Chain<WIDTH> chain;
+    int s_known[2];
+
+    template <bool FULL> __device__ __forceinline__ void run(const ScanArgs &a, const Queue &queue, Unit &unit, int buf, unsigned *s_ticket) {
+        unsigned next = 0;
+        if (threadIdx.x == kThreads<GROUPS> - 64) next = queue.take();
+        const P p(a, unit.b, unit.g, unit.n, unit.chunk);
+        const int w = wave_id(), link = unit.last - unit.chunk;                // links from the last chunk on
+        Word *words = a.words + ((long long)unit.chunk * a.chains + unit.chain) * WIDTH;
+        const long long back = -a.chains * WIDTH;
+        const Folder<VEC> f(a, unit.b, unit.g, true);
+        Back<VEC> x;
+        x.template load<FULL, T>(a, p, Row<const T, FULL>(a, a.G, 3 * a.H, p, unit.chunk), Row<const T, FULL>(a, a.dh, a.H, p, unit.chunk));
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) x.maps(v, s_a[p.group][p.slot + v], s_b[p.group][p.slot + v], s_r[p.group][p.slot + v]);
+        settle();
+        float all, sum;
+        {
+            FourMaps<WIDTH, false> m;
+            m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+            m.total(all, sum);
+        }
+        if (f.on) s_wa[buf][w][f.lane] = all, s_wb[buf][w][f.lane] = sum;
+        {
+            FourMaps<WIDTH, true> r;
+            r.read(s_a + 4 * w, s_r + 4 * w, f.lane);
+            r.total(all, sum);
+        }
+        if (f.on) s_wr[buf][w][f.lane] = sum;
+        const float state = a.states[((size_t)unit.b * a.chunks + unit.chunk) * a.H + f.ch];      // (wanted behind the barrier)
+        float carry = 0.f;
+        lds_barrier();
+        const auto finish = [&]() __attribute__((always_inline)) {
+            if (unit.chunk > 0) Chain<WIDTH>::hand_on(words, f.lane, all, carry, sum);
+            s_carry[buf][f.lane] = carry;
+        };
+        if (w == 0 && f.on) {
+            if (link == 0 && a.first) carry = a.first[f.row];
+            WaveMaps<WIDTH, W, true> wr;
+            wr.read(s_wa[buf], s_wr[buf], f.lane);
+            wr.total(all, sum);
+            const bool known = Chain<WIDTH>::first_look(words, f.lane, back, link, 0, all, sum, carry);
+            if (known) finish();
+            if (f.lane == 0) s_known[buf] = known;
+        }
+        // the states in front of the groups meanwhile
+        if (f.on) {
+            WaveMaps<WIDTH, W, false> wm;
+            wm.read(s_wa[buf], s_wb[buf], f.lane);
+            FourMaps<WIDTH, false> m;
+            m.read(s_a + 4 * w, s_b + 4 * w, f.lane);
+            m.write(s_b + 4 * w, f.lane, wm.state(state, w));
+        }
+        if (threadIdx.x == kThreads<GROUPS> - 64) s_ticket[buf] = next;
+        lds_barrier();
+        if (!__builtin_amdgcn_readfirstlane(s_known[buf])) {
+            const int from = chain.look_on(words, back, link);
+            if (w == 0 && f.on) {
+                carry = chain.carry_from(f.lane, from);
+                finish();
+            }
+            lds_barrier();
+        }
+        if (f.on) {
+            WaveMaps<WIDTH, W, true> wr;
+            wr.read(s_wa[buf], s_wr[buf], f.lane);
+            FourMaps<WIDTH, true> r;
+            r.read(s_a + 4 * w, s_r + 4 * w, f.lane);
+            const float end = r.write(s_r + 4 * w, f.lane, wr.state(s_carry[buf][f.lane], w));
+            if (a.last && f.own && unit.chunk == 0 && w == 0) a.last[f.row] = end;
+        }
+        settle();
+        float c[VEC], q[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            c[v] = s_b[p.group][p.slot + v];
+            q[v] = s_r[p.group][p.slot + v];
+        }
+        const Row<T, FULL> dG(a, a.out, 3 * a.H, p, unit.chunk);
+        x.template store<FULL, T>(a, p, dG, c, q);
+        unit = Unit(a, queue, __builtin_amdgcn_readfirstlane(s_ticket[buf]), true);
+    }
+};
+
+// Positions behind a sequence's end, a whole chunk of them
+template <typename T, int VEC> __device__ __forceinline__ void put_zeros(const ScanArgs &a, const Unit &unit, int arrays) {
+    const Place<VEC, kChunkGroups> p(a, unit.b, unit.g, unit.n, unit.chunk);
+    const Row<T, false> out(a, a.out, arrays * a.H, p, unit.chunk);
+    float zero[VEC] = {};
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) asm volatile("" : "+v"(zero[v]));           // (made here: in front of the loop over the units they would hold registers)
+    for (int i = 0; i < kSteps; ++i)
+        for (int k = 0; k < arrays; ++k)
+            if (p.on && p.s0 + i < a.T) put_from<T, VEC>(out.at(a, p, i, arrays * a.H, k * a.H, false), zero, p.skip, a.whole);
+}
+
+template <typename T, int VEC, bool BWD>
+__global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_chain(const ScanArgs a) {
+    __shared__ std::conditional_t<BWD, BwdChain<T, VEC>, FwdChain<T, VEC>> s;
+    __shared__ unsigned s_ticket[2];
+    constexpr int THREADS = kThreads<kChunkGroups>;
+    const Queue queue(a);
+    if (threadIdx.x == 0) s_ticket[1] = queue.take();
+    __syncthreads();
+    Unit unit(a, queue, __builtin_amdgcn_readfirstlane(s_ticket[1]), BWD);
+    for (int buf = 0; unit.there; buf ^= 1) {
+        if (unit.chunk > unit.last) {
+            if (threadIdx.x == THREADS - 64) s_ticket[buf] = queue.take();
+            put_zeros<T, VEC>(a, unit, BWD ? 3 : 1);
+            lds_barrier();
+            unit = Unit(a, queue, __builtin_amdgcn_readfirstlane(s_ticket[buf]), BWD);
+        } else if (unit.full()) {
+            s.template run<true>(a, queue, unit, buf, s_ticket);
+        } else {
+            s.template run<false>(a, queue, unit, buf, s_ticket);
+        }
     }
 }
 
@@ -518,7 +841,7 @@ static bool unaligned_scan(std::initializer_list<const void *> ps) {
 // Words and ticket of the chains.  Nothing where all steps are one chunk's.
 struct ScanPlan {
     int vec, groups_h, chunks;
-    long long chains, units;
+    long long chains;
     int queues;
     size_t bytes;
 };
@@ -528,9 +851,8 @@ static ScanPlan scan_plan(const echo_scan_desc_t &d) {
     p.groups_h = (d.H + 16 * p.vec - 1) / (16 * p.vec);
     p.chunks = (int)scan_chunks(d);
     p.chains = (long long)d.B * p.groups_h;
-    p.units = p.chains * p.chunks;
     if (p.chunks > 1) {
-        p.bytes = kQueues * kTicketStride * 8 + (size_t)p.units * 16 * p.vec * 8;
+        p.bytes = kQueues * kTicketStride * 8 + (size_t)p.chains * p.chunks * 16 * p.vec * 8;
         // as many queues as there are chains, or a number up to kQueues that deals them out evenly
         long long least = p.chains * 2;
         for (int q = (int)std::min<long long>(p.chains, kQueues); q > (int)std::min<long long>(p.chains, kQueues) / 2; --q) {
@@ -541,34 +863,37 @@ static ScanPlan scan_plan(const echo_scan_desc_t &d) {
     return p;
 }
 
-template <typename T, int VEC, int GROUPS, bool CHAIN> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
+template <typename T, int VEC, int GROUPS> static echo_status_t launch_scan(ScanArgs a, bool bwd, hipStream_t st) {
     constexpr int SUBS = Place<VEC, GROUPS>::SUBS;
-    const auto launch = [&](const ScanArgs &x, long long blocks) {
-        LaunchRecord r = launch_begin(bwd ? "scan_bwd" : "scan_fwd", st);
-        if (bwd) k_scan_bwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kThreads<GROUPS>, 0, st>>>(x);
-        else k_scan_fwd<T, VEC, GROUPS, CHAIN><<<(unsigned)blocks, kThreads<GROUPS>, 0, st>>>(x);
-        return launch_end(r);
-    };
-    // as many blocks as the chip holds, the same number for each queue
-    if (CHAIN) return launch(a, (std::min<long long>(a.units, 256 * kBlocks) + a.queues - 1) / a.queues * a.queues);
-    ScanArgs x = a;
     constexpr long long MOST = 1 << 22;                    // blocks of a launch: a grid has fewer than 2^32 threads
-    for (; x.chain0 < a.chains; x.chain0 += MOST * SUBS)
-        if (echo_status_t s = launch(x, std::min(MOST, (a.chains - x.chain0 + SUBS - 1) / SUBS))) return s;
+    for (; a.chain0 < a.chains; a.chain0 += MOST * SUBS) {
+        const unsigned blocks = (unsigned)std::min(MOST, (a.chains - a.chain0 + SUBS - 1) / SUBS);
+        LaunchRecord r = launch_begin(bwd ? "scan_bwd" : "scan_fwd", st);
+        if (bwd) k_scan_bwd<T, VEC, GROUPS><<<blocks, kThreads<GROUPS>, 0, st>>>(a);
+        else k_scan_fwd<T, VEC, GROUPS><<<blocks, kThreads<GROUPS>, 0, st>>>(a);
+        if (echo_status_t s = launch_end(r)) return s;
+    }
     return ECHO_OK;
 }
 template <typename T, int VEC> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
-    if (a.chunks > 1) return launch_scan<T, VEC, kChunkGroups, true>(a, bwd, st);
-    if (a.T <= kSteps) return launch_scan<T, VEC, 1, false>(a, bwd, st);
-    if (a.T <= 4 * kSteps) return launch_scan<T, VEC, 4, false>(a, bwd, st);
-    if (a.T <= 16 * kSteps) return launch_scan<T, VEC, 16, false>(a, bwd, st);
-    return launch_scan<T, VEC, kChunkGroups, false>(a, bwd, st);
+    if (a.chunks > 1) {
+        // as many blocks as the chip holds, the same number for each queue
+        const unsigned blocks = (unsigned)((std::min<long long>(a.chains * a.chunks, 256 * kBlocks) + a.queues - 1) / a.queues * a.queues);
+        LaunchRecord r = launch_begin(bwd ? "scan_bwd_chain" : "scan_fwd_chain", st);
+        if (bwd) k_scan_chain<T, VEC, true><<<blocks, kThreads<kChunkGroups>, 0, st>>>(a);
+        else k_scan_chain<T, VEC, false><<<blocks, kThreads<kChunkGroups>, 0, st>>>(a);
+        return launch_end(r);
+    }
+    if (a.T <= kSteps) return launch_scan<T, VEC, 1>(a, bwd, st);
+    if (a.T <= 4 * kSteps) return launch_scan<T, VEC, 4>(a, bwd, st);
+    if (a.T <= 16 * kSteps) return launch_scan<T, VEC, 16>(a, bwd, st);
+    return launch_scan<T, VEC, kChunkGroups>(a, bwd, st);
 }
 static echo_status_t run_scan(const echo_scan_desc_t &d, const ScanPlan &p, ScanArgs a, bool bwd, void *workspace, hipStream_t st) {
     a.B = d.B, a.T = d.T, a.H = d.H, a.reverse = d.reverse;
     a.queues = 1;
     a.whole = d.H % (d.dtype == ECHO_F32 ? 4 : 8) == 0;
-    a.chunks = p.chunks, a.groups_h = p.groups_h, a.chains = p.chains, a.units = p.units;
+    a.chunks = p.chunks, a.groups_h = p.groups_h, a.chains = p.chains;
     if (p.bytes) {
         a.tickets = static_cast<unsigned long long *>(workspace);
         a.words = a.tickets + kQueues * kTicketStride;
