@@ -37,61 +37,78 @@ struct TeacherLists {
 };
 echo_status_t launch_teacher_lists(const TeacherLists &l, hipStream_t st);
 
-// The shares of words v .. v + 3 in row n (below 0: none), v a multiple of 4.  For few rows: the lane looks through the row's words of v's range.
-__device__ __forceinline__ f32x4 teacher_shares(const Teacher &t, int n, int v) {
-    f32x4 q = {0.f, 0.f, 0.f, 0.f};
-    const int mark = v / kMarkWords;
-    if (n < 0 || mark + 1 >= t.marks) return q;
-    const unsigned char *start = t.start + (size_t)n * t.marks + mark;
-    for (int e = start[0]; e < start[1]; ++e) {
-        const int r = t.words[(size_t)n * t.K + e] - v;
-        const float x = t.shares[(size_t)n * t.K + e];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (r == k) q[k] = x;
-    }
-    return q;
-}
-
-// The shares of 16 rows and WORDS words for a wave that holds their logits as the matrix cores leave them (lane l: row l % 16): put into LDS where they are,
-// read by everybody, and taken out again.  Nothing of it but the few words that a row has among these costs more than one read.
-template <int WORDS> struct TeacherTile {
+// The shares of TN times 16 rows and of WORDS words for a wave that holds their logits as the matrix cores leave them (lane l: row l % 16 of each): put into LDS
+// where they are, read by everybody, and taken out again.  Four lanes look after a row.  What a row has among these words is hardly ever more than an entry or
+// two; the first four of all TN rows are requested together, in three trips to the caches (one row after the other, each with its own three, took 18 % of a
+// tile of 256 x 256 x 1024).
+template <int WORDS, int TN> struct TeacherTile {
     static constexpr int PITCH = WORDS + 4, BYTES = 16 * PITCH * 4;            // 4 more floats a row: a fragment's 16 rows take all banks
     const Teacher &t;
     float *mine;
-    int v0, row, begin, end;
-    bool any;
-    // `on`: it is used; lds: BYTES of every wave, nobody else's from here to the last clear()
-    __device__ __forceinline__ TeacherTile(const Teacher &teacher, float *lds, int first_word, bool on) : t(teacher), v0(first_word) {
+    int v0;
+    int row[TN], range[TN], word[TN];                                          // range: first and last entry + 1, in 8 bits each
+    float share[TN];
+    // `on`: it is used; lds: BYTES of every wave, nobody else's from here to the last clear(); row_of(j): the lane's row among rows j, below 0: none
+    template <typename RowOf> __device__ __forceinline__ TeacherTile(const Teacher &teacher, float *lds, int first_word, bool on, RowOf row_of) : t(teacher), v0(first_word) {
         mine = lds + wave_id() * 16 * PITCH;
         if (!on) return;
+        zero();
+        const int mark = min(v0 / kMarkWords, t.marks - 2);
+        const bool there = v0 / kMarkWords == mark;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) row[j] = row_of(j);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const unsigned char *start = t.start + (size_t)max(row[j], 0) * t.marks + mark;
+            range[j] = start[0] | start[1] << 8;
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            if (row[j] < 0 || !there) range[j] = 0;
+            const int e = begin(j) + (lane_id() >> 4);
+            const size_t at = (size_t)max(row[j], 0) * t.K + min(e, t.K - 1);
+            word[j] = t.words[at];
+            share[j] = t.shares[at];
+        }
+    }
+    __device__ __forceinline__ int begin(int j) const { return range[j] & 255; }
+    __device__ __forceinline__ int end(int j) const { return range[j] >> 8; }
+    __device__ __forceinline__ void zero() {
         for (int k = lane_id(); k < 16 * PITCH / 4; k += 64) reinterpret_cast<f32x4 *>(mine)[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    __device__ __forceinline__ void put(int n) {                               // the lane's row, below 0: none
-        row = n;
-        begin = end = 0;
-        const int mark = v0 / kMarkWords;
-        if (n >= 0 && mark + 1 < t.marks) {
-            const unsigned char *start = t.start + (size_t)n * t.marks + mark;
-            begin = start[0], end = start[1];
-        }
-        any = __ballot(begin < end) != 0;
-        if (any) write(false);
-    }
-    __device__ __forceinline__ void clear() {
-        if (any) write(true);
-    }
-    __device__ __forceinline__ f32x4 get(int v) const {                        // of the lane's row, words v0 + v .. + 3
-        return any ? *reinterpret_cast<const f32x4 *>(mine + (lane_id() & 15) * PITCH + v) : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    // four lanes share a row
-    __device__ __forceinline__ void write(bool zero) {
+    __device__ __forceinline__ float *place(int v) const { return mine + (lane_id() & 15) * PITCH + v; }
+    __device__ __forceinline__ bool any(int j) const { return __ballot(begin(j) < end(j)) != 0; }
+    __device__ __forceinline__ bool many(int j) const { return __ballot(begin(j) + 4 < end(j)) != 0; }
+    __device__ __forceinline__ bool first(int j) const { return begin(j) + (lane_id() >> 4) < end(j) && (unsigned)(word[j] - v0) < (unsigned)WORDS; }
+    __device__ __forceinline__ void put(int j) {
+        if (!any(j)) return;
         wait();
-        for (int e = begin + (lane_id() >> 4); e < end; e += 4) {
-            const int v = t.words[(size_t)row * t.K + e] - v0;
-            if ((unsigned)v < (unsigned)WORDS) mine[(lane_id() & 15) * PITCH + v] = zero ? 0.f : t.shares[(size_t)row * t.K + e];
+        if (first(j)) *place(word[j] - v0) = share[j];
+        if (many(j)) {
+            constexpr int U = 4;
+            for (int e0 = begin(j) + 4 + (lane_id() >> 4); __ballot(e0 < end(j)); e0 += 4 * U) {
+                int w[U];
+                float x[U];
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    const size_t at = (size_t)max(row[j], 0) * t.K + min(e0 + 4 * k, t.K - 1);
+                    w[k] = t.words[at], x[k] = t.shares[at];
+                }
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+                    if (e0 + 4 * k < end(j) && (unsigned)(w[k] - v0) < (unsigned)WORDS) *place(w[k] - v0) = x[k];
+            }
         }
         wait();
+    }
+    __device__ __forceinline__ f32x4 get(int j, int v) const {                 // of the lane's row, words v0 + v .. + 3
+        return any(j) ? *reinterpret_cast<const f32x4 *>(place(v)) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void clear(int j) {
+        if (!any(j)) return;
+        wait();
+        if (many(j)) zero();
+        else if (first(j)) *place(word[j] - v0) = 0.f;
     }
     // what this wave has written or read in LDS is done: the lanes' exchange needs no more
     static __device__ __forceinline__ void wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }

@@ -387,7 +387,11 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
     const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
-    typedef TeacherTile<C::TM * 16> Shares;
+    typedef TeacherTile<C::TM * 16, C::TN> Shares;
+    const auto row_of = [&](int j) {
+        const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+        return n < count ? a.rows[n] : -1;
+    };
     if constexpr (TEACHER) {
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
@@ -397,21 +401,21 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     if constexpr (MODE == Mode::kForward) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
         static_assert(3 * C::WM * C::BN * 4 + C::WAVES * Shares::BYTES <= C::LDS_BYTES, "room for the shares");
-        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER);
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER, row_of);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int nt = (wn * C::TN + j) * 16 + (lane & 15), n = n0 + nt;
             const int y = !TEACHER && n < count ? a.labels[a.rows[n]] - vw : -1;
             float z = 0.f;
             if constexpr (TEACHER) {
-                shares.put(n < count ? a.rows[n] : -1);
+                shares.put(j);
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i) {
-                    const f32x4 q = shares.get(i * 16 + lr);
+                    const f32x4 q = shares.get(j, i * 16 + lr);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) z += q[r] != 0.f ? q[r] * acc[i][j][r] : 0.f;      // a logit of a word past the end may be anything
                 }
-                shares.clear();
+                shares.clear(j);
                 z += __shfl_xor(z, 16);
                 z += __shfl_xor(z, 32);
             } else if (a.eps > 0.f) {
@@ -485,19 +489,19 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 for (int i = 0; i < C::TM; ++i)
                     if (n0 + (wn * C::TN + j) * 16 + (lane & 15) >= count) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        Shares shares(a.teacher, reinterpret_cast<float *>(lds), vw - lr, TEACHER);
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds), vw - lr, TEACHER, row_of);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
             const bool row = n < count;
             const int at = row ? a.rows[n] : 0;
             const int y = !TEACHER && row ? a.labels[at] - vw : -1;
-            if constexpr (TEACHER) shares.put(row ? at : -1);
+            if constexpr (TEACHER) shares.put(j);
             const float lse = row ? a.lse[at] : 0.f, g = !row ? 0.f : half_of(MODE) ? 0x1p15f : a.dloss[at] * kDzScale;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
                 f32x4 q;
-                if constexpr (TEACHER) q = shares.get(i * 16 + lr);
+                if constexpr (TEACHER) q = shares.get(j, i * 16 + lr);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int v = i * 16 + r;
@@ -510,7 +514,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                     acc[i][j][r] = x;
                 }
             }
-            if constexpr (TEACHER) shares.clear();
+            if constexpr (TEACHER) shares.clear(j);
         }
         if constexpr (TEACHER) lds_barrier();                                  // the shares' place is the other waves' for dz
         // dz passes through LDS a plane at a time, [row][word]: each lane writes four words of a row; whole rows leave for dz, and read
@@ -810,16 +814,19 @@ template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 
 
 // The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
 template <int NT, int WAVES, bool TEACHER>
-__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z) {
+__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z, float *s_shares) {
     constexpr int ROWS = 16 * NT;
     const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
+    TeacherTile<16, NT> shares(a.teacher, s_shares, v0, TEACHER, [&](int j) { return 16 * j + (lane & 15) < a.N ? 16 * j + (lane & 15) : -1; });
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int n = 16 * j + (lane & 15), y = !TEACHER && n < a.N ? a.labels[n] - vw : -1;
         f32x4 q = {0.f, 0.f, 0.f, 0.f};
         if constexpr (TEACHER) {
             acc[j] *= a.teacher.inv_t;
-            q = teacher_shares(a.teacher, n < a.N ? n : -1, vw);
+            shares.put(j);
+            q = shares.get(j, vw - v0);
+            shares.clear(j);
         }
         float z = 0.f, top = -__builtin_inff(), sum = 0.f;
 #pragma unroll
@@ -864,20 +871,23 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
 }
 
 // dz of the same: few enough to be stored as the lanes hold it.  Rows n0 .. n0 + a.N, and zeros up to a multiple of 8 and for words past the end
-template <int NT, bool TEACHER> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0) {
+template <int NT, bool TEACHER> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0, float *s_shares) {
     const int lane = lane_id(), vw = v0 + 4 * (lane >> 4);
+    TeacherTile<16, NT> shares(a.teacher, s_shares, a.v0 + v0, TEACHER, [&](int j) { return 16 * j + (lane & 15) < a.N ? a.rows[16 * j + (lane & 15)] : -1; });
     const float low = a.eps / (float)a.all_words, off = 1.0f - a.eps;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int n = 16 * j + (lane & 15);
-        if (n >= (a.N + 7) / 8 * 8) continue;
-        const bool row = n < a.N;
-        const int at = a.rows[min(n, a.N - 1)], y = TEACHER ? -1 : a.labels[at] - a.v0 - vw;
         f32x4 q = {0.f, 0.f, 0.f, 0.f};
         if constexpr (TEACHER) {
             acc[j] *= a.teacher.inv_t;
-            q = teacher_shares(a.teacher, row ? at : -1, a.v0 + vw);
+            shares.put(j);
+            q = shares.get(j, vw - v0);
+            shares.clear(j);
         }
+        if (n >= (a.N + 7) / 8 * 8) continue;
+        const bool row = n < a.N;
+        const int at = a.rows[min(n, a.N - 1)], y = TEACHER ? -1 : a.labels[at] - a.v0 - vw;
         const float lse = a.lse[at], g = a.dloss[at] * kDzScale;
         f32x4 x;
 #pragma unroll
@@ -934,7 +944,8 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
             if (t0 + d + AHEAD < steps) fetch(d, t0 + d + AHEAD);
             acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
         }
-    few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z);
+    __shared__ __align__(16) float s_shares[TEACHER ? 4 * TeacherTile<16, 1>::BYTES / 4 : 1];
+    few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z, s_shares);
 }
 
 // 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
@@ -1039,8 +1050,10 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
         step(t, fw[0]);
         if (t + 1 < steps) step(t + 1, fw[1]);
     }
-    if constexpr (BWD) few_dz<NT, TEACHER>(a, acc, n0, v0);
-    else few_join<NT, WAVES, TEACHER>(a, acc, tile, v0, s_max, s_sum, s_z);
+    static_assert(WAVES * TeacherTile<16, NT>::BYTES <= sizeof(s_h), "room for the shares");      // (behind the last barrier nobody reads the rows)
+    float *s_shares = reinterpret_cast<float *>(s_h);
+    if constexpr (BWD) few_dz<NT, TEACHER>(a, acc, n0, v0, s_shares);
+    else few_join<NT, WAVES, TEACHER>(a, acc, tile, v0, s_max, s_sum, s_z, s_shares);
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
