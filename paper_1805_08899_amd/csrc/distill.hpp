@@ -41,30 +41,37 @@ echo_status_t launch_teacher_lists(const TeacherLists &l, hipStream_t st);
 // where they are, read by everybody, and taken out again.  Four lanes look after a row.  What a row has among these words is hardly ever more than an entry or
 // two; the first four of all TN rows are requested together, in three trips to the caches (one row after the other, each with its own three, took 18 % of a
 // tile of 256 x 256 x 1024).
-template <int WORDS, int TN> struct TeacherTile {
-    static constexpr int PITCH = WORDS + 4, BYTES = 16 * PITCH * 4;            // 4 more floats a row: a fragment's 16 rows take all banks
-    const Teacher &t;
-    float *mine;
-    int v0;
-    int row[TN], range[TN], word[TN];                                          // range: first and last entry + 1, in 8 bits each
-    float share[TN];
-    // `on`: it is used; lds: BYTES of every wave, nobody else's from here to the last clear(); row_of(j): the lane's row among rows j, below 0: none
-    template <typename RowOf> __device__ __forceinline__ TeacherTile(const Teacher &teacher, float *lds, int first_word, bool on, RowOf row_of) : t(teacher), v0(first_word) {
-        mine = lds + wave_id() * 16 * PITCH;
-        if (!on) return;
-        zero();
-        const int mark = min(v0 / kMarkWords, t.marks - 2);
-        const bool there = v0 / kMarkWords == mark;
+// Where they stand: the row, and first and last entry + 1 in 8 bits each.  What does not depend on the logits may be requested in front of their product.
+template <int TN> struct TeacherRanges {
+    int row[TN], range[TN];
+    // row_of(j): the lane's row among rows j, below 0: none; first_word: the wave's
+    template <typename RowOf> __device__ __forceinline__ void look_up(const Teacher &t, int first_word, RowOf row_of) {
+        const int mark = min(first_word / kMarkWords, t.marks - 2);
+        const bool there = first_word / kMarkWords == mark;
 #pragma unroll
         for (int j = 0; j < TN; ++j) row[j] = row_of(j);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const unsigned char *start = t.start + (size_t)max(row[j], 0) * t.marks + mark;
-            range[j] = start[0] | start[1] << 8;
+            range[j] = row[j] >= 0 && there ? start[0] | start[1] << 8 : 0;
         }
+    }
+};
+template <int WORDS, int TN> struct TeacherTile {
+    static constexpr int PITCH = WORDS + 4, BYTES = 16 * PITCH * 4;            // 4 more floats a row: a fragment's 16 rows take all banks
+    const Teacher &t;
+    float *mine;
+    int v0;
+    int row[TN], range[TN], word[TN];
+    float share[TN];
+    // `on`: it is used; lds: BYTES of every wave, nobody else's from here to the last clear()
+    __device__ __forceinline__ TeacherTile(const Teacher &teacher, float *lds, int first_word, bool on, const TeacherRanges<TN> &r) : t(teacher), v0(first_word) {
+        mine = lds + wave_id() * 16 * PITCH;
+        if (!on) return;
+        zero();
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
-            if (row[j] < 0 || !there) range[j] = 0;
+            row[j] = r.row[j], range[j] = r.range[j];
             const int e = begin(j) + (lane_id() >> 4);
             const size_t at = (size_t)max(row[j], 0) * t.K + min(e, t.K - 1);
             word[j] = t.words[at];

@@ -380,42 +380,47 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     int im, in;
     if (!tile_of_block(blockIdx.x, (a.W.rows + C::BM - 1) / C::BM, (count + C::BN - 1) / C::BN, im, in)) return;
     const int m0 = im * C::BM, n0 = in * C::BN;
+    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
+    // The large tile of dz has no registers for the ranges besides its product's.
+    constexpr bool EARLY = MODE == Mode::kForward || C::BM < 256;
+    TeacherRanges<C::TN> ranges;
+    const auto look_up = [&] {
+        ranges.look_up(a.teacher, a.v0 + m0 + wm * C::TM * 16, [&](int j) {
+            const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
+            return n < count ? a.rows[n] : -1;
+        });
+    };
+    if constexpr (TEACHER && EARLY) look_up();
     f32x4 acc[C::TM][C::TN];
     Operand h = a.h;
     h.rows = count;
     tile_product<C>(acc, a.W, h, m0, n0, 0, a.D, a.pairs, lds);
-    const int lane = lane_id(), w = wave_id(), wm = w / C::WN, wn = w % C::WN, lr = 4 * (lane >> 4);
+    if constexpr (TEACHER && !EARLY) look_up();
     const int vw = a.v0 + m0 + wm * C::TM * 16 + lr;                           // this lane's first word: it holds words vw + 16 i + r
     const bool tail = a.v0 + m0 + C::BM > a.V;
     typedef TeacherTile<C::TM * 16, C::TN> Shares;
-    const auto row_of = [&](int j) {
-        const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
-        return n < count ? a.rows[n] : -1;
-    };
-    if constexpr (TEACHER) {
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j) acc[i][j] *= a.teacher.inv_t;
-    }
     if constexpr (MODE == Mode::kForward) {
         float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
         static_assert(3 * C::WM * C::BN * 4 + C::WAVES * Shares::BYTES <= C::LDS_BYTES, "room for the shares");
-        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER, row_of);
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER, ranges);
+        // the teacher's temperature is taken into the exponent, and off maxima and means
+        const float log2e = TEACHER ? kLog2e * a.teacher.inv_t : kLog2e;
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int nt = (wn * C::TN + j) * 16 + (lane & 15), n = n0 + nt;
             const int y = !TEACHER && n < count ? a.labels[a.rows[n]] - vw : -1;
             float z = 0.f;
-            if constexpr (TEACHER) {
+            if constexpr (TEACHER) {                                           // the mean of the logits by their shares
                 shares.put(j);
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i) {
                     const f32x4 q = shares.get(j, i * 16 + lr);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) z += q[r] != 0.f ? q[r] * acc[i][j][r] : 0.f;      // a logit of a word past the end may be anything
+                    for (int r = 0; r < 4; ++r) y[r] += q[r] != 0.f ? q[r] * acc[i][j][r] : 0.f;       // a logit of a word past the end may be anything
                 }
                 shares.clear(j);
+                z = a.teacher.inv_t * ((y[0] + y[1]) + (y[2] + y[3]));
                 z += __shfl_xor(z, 16);
                 z += __shfl_xor(z, 32);
             } else if (a.eps > 0.f) {
@@ -455,11 +460,11 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[i][j][r] - at) * kLog2e);
+                for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[i][j][r] - at) * log2e);
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (lane < 16) {
-                s_max[wm * C::BN + nt] = top;
+                s_max[wm * C::BN + nt] = TEACHER ? top * a.teacher.inv_t : top;
                 s_sum[wm * C::BN + nt] = sum;
                 s_z[wm * C::BN + nt] = z;
             }
@@ -489,7 +494,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
                 for (int i = 0; i < C::TM; ++i)
                     if (n0 + (wn * C::TN + j) * 16 + (lane & 15) >= count) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        Shares shares(a.teacher, reinterpret_cast<float *>(lds), vw - lr, TEACHER, row_of);
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds), vw - lr, TEACHER, ranges);
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
             const int n = n0 + (wn * C::TN + j) * 16 + (lane & 15);
@@ -501,7 +506,10 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
 #pragma unroll
             for (int i = 0; i < C::TM; ++i) {
                 f32x4 q;
-                if constexpr (TEACHER) q = shares.get(j, i * 16 + lr);
+                if constexpr (TEACHER) {
+                    q = shares.get(j, i * 16 + lr);
+                    acc[i][j] *= a.teacher.inv_t;
+                }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int v = i * 16 + r;
@@ -817,7 +825,9 @@ template <int NT, int WAVES, bool TEACHER>
 __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z, float *s_shares) {
     constexpr int ROWS = 16 * NT;
     const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
-    TeacherTile<16, NT> shares(a.teacher, s_shares, v0, TEACHER, [&](int j) { return 16 * j + (lane & 15) < a.N ? 16 * j + (lane & 15) : -1; });
+    TeacherRanges<NT> ranges;
+    if constexpr (TEACHER) ranges.look_up(a.teacher, v0, [&](int j) { return 16 * j + (lane & 15) < a.N ? 16 * j + (lane & 15) : -1; });
+    TeacherTile<16, NT> shares(a.teacher, s_shares, v0, TEACHER, ranges);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         const int n = 16 * j + (lane & 15), y = !TEACHER && n < a.N ? a.labels[n] - vw : -1;
@@ -873,7 +883,9 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
 // dz of the same: few enough to be stored as the lanes hold it.  Rows n0 .. n0 + a.N, and zeros up to a multiple of 8 and for words past the end
 template <int NT, bool TEACHER> __device__ __forceinline__ void few_dz(const FewArgs &a, f32x4 (&acc)[NT], int n0, int v0, float *s_shares) {
     const int lane = lane_id(), vw = v0 + 4 * (lane >> 4);
-    TeacherTile<16, NT> shares(a.teacher, s_shares, a.v0 + v0, TEACHER, [&](int j) { return 16 * j + (lane & 15) < a.N ? a.rows[16 * j + (lane & 15)] : -1; });
+    TeacherRanges<NT> ranges;
+    if constexpr (TEACHER) ranges.look_up(a.teacher, a.v0 + v0, [&](int j) { return 16 * j + (lane & 15) < a.N ? a.rows[16 * j + (lane & 15)] : -1; });
+    TeacherTile<16, NT> shares(a.teacher, s_shares, a.v0 + v0, TEACHER, ranges);
     const float low = a.eps / (float)a.all_words, off = 1.0f - a.eps;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
