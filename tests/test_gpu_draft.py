@@ -56,6 +56,17 @@ def test_against_the_oracle(B, K, V, store, lengths):
         Problem(B, K, V, store, seed + V, lengths, spread=(0.7, 0.0, 3.0)[seed]).check()
 
 
+@pytest.mark.parametrize("B,V,store", [(70, 65537, "f32"), (64, 65537, "bf16"), (3, 65536, "f32"), (65, 40001, "bf16"), (2, 39999, "f32"), (1, 131073, "f32")])
+def test_where_segments_and_blocks_change(B, V, store):
+    p = Problem(B, 1, V, store, seed=B, lengths=True)
+    p.check()
+    p.target[:, :] = 0                                       # nothing is left of p, nor of p behind q
+    p.target[::2, :, V - 1] = 0.5                            # but for the last word of every other sequence
+    p.draft[:, :, V - 1] = 0.75
+    p.u[:] = 0.9
+    p.check()
+
+
 def test_all_kinds_of_endings_occur():
     p = Problem(300, 4, 200, seed=5)
     tokens, taken = p.check()

@@ -164,6 +164,23 @@ def test_against_the_oracle(B, T, H, store, reverse, lengths):
     assert all(np.array_equal(got[k], again[k]) for k in got), "not the same from run to run"
 
 
+@pytest.mark.parametrize("store,reverse", [("f32", False), ("bf16", True)])
+def test_lengths_at_the_ends_of_chunks(store, reverse):
+    """Sequences that end with a chunk, one step behind it and in front of it, chunks without a step, and a sequence without any."""
+    p = Problem(9, 520, 70, store, reverse, lengths=[128, 129, 127, 0, 256, 257, 520, 512, 1], seed=20)
+    p.check(p.run())
+
+
+def test_more_units_than_blocks():
+    """222 chains of 3 chunks, which the blocks take in turns from queues of unequal length, a third of them empty; most sequences are short."""
+    r = np.random.default_rng(21)
+    p = Problem(37, 300, 330, "bf16", True, lengths=(300 * r.random(37) ** 2).astype(int).tolist(), seed=21)
+    got = p.run()
+    p.check(got)
+    again = p.run()
+    assert all(np.array_equal(got[k], again[k]) for k in got)
+
+
 @pytest.mark.parametrize("T", [1, 7, 200])
 def test_what_may_be_left_out(T):
     p = Problem(3, T, 37, lengths=None, c0=False, dc_last=False, seed=1)
