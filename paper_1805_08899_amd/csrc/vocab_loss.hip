@@ -1082,8 +1082,9 @@ __device__ __forceinline__ void loss_of_row(float top, float sum, float z, float
 
 // The same against a teacher: z is the sum of the logits by their shares, `own` the sum of share log share.
 __device__ __forceinline__ void loss_of_row(float top, float sum, float z, const Teacher &t, int n, float &loss, float &lse) {
-    lse = top + logf(sum);
-    loss = t.temperature * t.temperature * (t.own[n] + (lse - z));
+    const float rest = logf(sum);
+    lse = top + rest;
+    loss = t.temperature * t.temperature * (t.own[n] + ((top - z) + rest));    // without the digits that lse loses to its size
 }
 
 // A block per row.
