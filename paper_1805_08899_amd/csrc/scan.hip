@@ -146,6 +146,8 @@ template <int VEC> struct Folder {
 };
 // a wave's own exchange through LDS
 __device__ __forceinline__ void settle() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// A number that was requested is here
+__device__ __forceinline__ void here(float &x) { asm volatile("" : "+v"(x)); }
 
 // The maps of a wave's four groups, a lane per channel, and of all four; BACK: in their order backwards
 template <int WIDTH, bool BACK> struct FourMaps {
@@ -216,9 +218,9 @@ template <typename T, bool FULL> struct Row {
     }
 };
 
-// A wave's channels where there are no chains: of its unit, which GROUPS / 4 waves share
+// A wave's channels where there are no chains: of its unit, which GROUPS / 4 waves share (GROUPS of 1: nothing is folded)
 template <int VEC, int GROUPS> __device__ __forceinline__ Folder<VEC> wave_folder(const ScanArgs &a, long long first_chain) {
-    const long long mine = first_chain + wave_id() / (GROUPS / 4), chain = min(mine, a.chains - 1);
+    const long long mine = first_chain + wave_id() / (GROUPS > 4 ? GROUPS / 4 : 1), chain = min(mine, a.chains - 1);
     const int b = (int)(chain / a.groups_h);
     return Folder<VEC>(a, b, (int)(chain - (long long)b * a.groups_h), mine < a.chains);
 }
@@ -239,6 +241,8 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
         for (int k = 0; k < 3; ++k) x[i][k].load(G.at(a, p, i, 3 * a.H, k * a.H, true));
+    const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
+    float state = GROUPS > 1 && a.first ? a.first[f.row] : 0.f;
     float c[VEC];
     if constexpr (GROUPS == 1) {
 #pragma unroll
@@ -272,8 +276,6 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
             s_a[own][p.slot + v] = A;
             s_b[own][p.slot + v] = b;
         }
-        const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
-        float state = a.first ? a.first[f.row] : 0.f;
         if (a.states && f.own && w % W == 0) a.states[f.row] = state;
         settle();
         FourMaps<P::WIDTH, false> m;
@@ -282,6 +284,7 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
             float all, sum;
             m.total(all, sum);
             if (f.on) s_wa[w][f.lane] = all, s_wb[w][f.lane] = sum;
+            here(state);                                   // in front of the barrier: behind it the unit's last wave writes c_last, which may be c0
             lds_barrier();
             WaveMaps<P::WIDTH, W, false> wm;
             wm.read(s_wa, s_wb, f.lane);
@@ -397,6 +400,8 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
     const int w = wave_id(), own = threadIdx.x >> 4;       // the thread's group in the block
     const long long first_chain = a.chain0 + (long long)blockIdx.x * P::SUBS;
     const P p(a, first_chain, 0);
+    const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
+    float state = GROUPS > 1 ? a.states[f.row] : 0.f, back = GROUPS > 1 && a.first ? a.first[f.row] : 0.f;
     Back<VEC> x;
     x.template load<false, T>(a, p, Row<const T, false>(a, a.G, 3 * a.H, p, 0), Row<const T, false>(a, a.dh, a.H, p, 0));
     float c[VEC], q[VEC];
@@ -409,8 +414,6 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
     } else {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) x.maps(v, s_a[own][p.slot + v], s_b[own][p.slot + v], s_r[own][p.slot + v]);
-        const Folder<VEC> f = wave_folder<VEC, GROUPS>(a, first_chain);
-        float state = a.states[f.row], back = a.first ? a.first[f.row] : 0.f;
         settle();
         FourMaps<P::WIDTH, false> m;
         FourMaps<P::WIDTH, true> r;
@@ -421,6 +424,7 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
             m.total(all, sum);
             r.total(all, rest);
             if (f.on) s_wa[w][f.lane] = all, s_wb[w][f.lane] = sum, s_wr[w][f.lane] = rest;
+            here(back);                                    // (as in the forward pass: dc0 may be dc_last)
             lds_barrier();
             WaveMaps<P::WIDTH, W, false> wm;
             wm.read(s_wa, s_wb, f.lane);

@@ -199,6 +199,14 @@ def test_states_in_place(B, T, H, reverse):
     p.check(p.run(in_place=True))
 
 
+@pytest.mark.parametrize("B,T,H", [(40, 33, 130), (9, 64, 70), (300, 65, 66), (64, 128, 257)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_states_in_place_that_several_waves_read(B, T, H, reverse):
+    """A chunk's states are read by each of its waves and written by one of them, which has to wait for the others' reads."""
+    p = Problem(B, T, H, reverse=reverse, lengths="random", seed=B)
+    p.check(p.run(in_place=True))
+
+
 def test_steps_one_by_one_are_the_sequence():
     torch, eb, _ = _torch()
     p = Problem(4, 9, 70, seed=3)
