@@ -1084,7 +1084,8 @@ __device__ __forceinline__ void loss_of_row(float top, float sum, float z, float
 __device__ __forceinline__ void loss_of_row(float top, float sum, float z, const Teacher &t, int n, float &loss, float &lse) {
     const float rest = logf(sum);
     lse = top + rest;
-    loss = t.temperature * t.temperature * (t.own[n] + ((top - z) + rest));    // without the digits that lse loses to its size
+    // without the digits that lse loses to its size; the temperature's square by itself may leave fp32's range
+    loss = t.temperature * (t.temperature * (t.own[n] + ((top - z) + rest)));
 }
 
 // A block per row.

@@ -145,6 +145,20 @@ def test_against_the_oracle(N, V, D, K, store, out, T):
     assert all(np.array_equal(got[k], again[k]) for k in got), "not the same from run to run"
 
 
+@pytest.mark.parametrize("exponent", [-64, 64])
+@pytest.mark.parametrize("N,V,D,K,store,out", [(3, 4, 16, 4, "f32", "f32"), (40, 130, 32, 9, "f32", "f32"), (40, 130, 32, 9, "bf16", "f32"),
+                                               (200, 300, 32, 9, "f32", "f32"), (200, 300, 32, 9, "bf16", "bf16")])
+def test_the_limits_of_the_temperature(N, V, D, K, store, out, exponent):
+    """Its square is no fp32 number there.  At the upper limit a loss whose value is one is within the bound, other values are infinite."""
+    p = Problem(N, V, D, K, store, out, 2.0 ** exponent, seed=N, pad=0.0)
+    got = p.run()
+    loss, _ = sr.distill_forward(p.h.double().numpy(), p.W.double().numpy(), p.words, p.logits.numpy(), p.T)
+    huge = loss >= 2.0 ** 127
+    assert (got["loss"][huge] >= 2.0 ** 126.9).all()
+    got["loss"][huge] = loss[huge]
+    p.check(got)
+
+
 def test_larger_tiles():
     """Sizes that fill rounds of tiles of 256 x 256, in all three ways of keeping dz, against the smaller calls' results for the same rows."""
     for store, out in (("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")):
