@@ -3,7 +3,7 @@
 // A thread owns kSteps consecutive steps of VEC channels; 16 such threads stand side by side, GROUPS of them one behind the other, and together take
 // GROUPS kSteps steps of 16 VEC channels.  A thread's steps are a linear map of the state, c -> A c + b (backward: q -> A q + R).  A wave folds the maps of
 // its four groups in LDS, a lane per channel, and every wave those of the waves in front of it; from the state in front of its own, every thread goes on
-// by itself.  A sequence longer than a chunk is a chain of them (below).
+// by itself.  A sequence longer than a chunk is a chain of them, whose chunks are one block's or many blocks' (below).
 //
 // With u = 1 - f = sigmoid(-x):  c += u (g - c),  r = dh o + q,  q = r - u r  keep the digits of a u next to zero.
 #include "../../include/echoscan.h"
@@ -22,6 +22,7 @@ namespace echo {
 constexpr int kSteps = 4;
 template <int GROUPS> constexpr int kThreads = GROUPS > 16 ? 512 : 256;
 constexpr int kBlocks = 2;            // to a compute unit
+constexpr int kXcds = 8;
 constexpr int kQueues = 32, kTicketStride = 16;            // (words of 8 bytes: a cache line)
 constexpr int kChunkGroups = ECHO_SCAN_CHUNK / kSteps;
 constexpr float kLog2eS = 1.4426950408889634f;
@@ -793,9 +794,9 @@ template <typename T, int VEC> struct BwdChain {
 };
 
 // Positions behind a sequence's end, a whole chunk of them
-template <typename T, int VEC> __device__ __forceinline__ void put_zeros(const ScanArgs &a, const Unit &unit, int arrays) {
-    const Place<VEC, kChunkGroups> p(a, unit.b, unit.g, unit.n, unit.chunk);
-    const Row<T, false> out(a, a.out, arrays * a.H, p, unit.chunk);
+template <typename T, int VEC> __device__ __forceinline__ void put_zeros(const ScanArgs &a, int b, int g, int n, int chunk, int arrays) {
+    const Place<VEC, kChunkGroups> p(a, b, g, n, chunk);
+    const Row<T, false> out(a, a.out, arrays * a.H, p, chunk);
     float zero[VEC] = {};
 #pragma unroll
     for (int v = 0; v < VEC; ++v) asm volatile("" : "+v"(zero[v]));           // (made here: in front of the loop over the units they would hold registers)
@@ -816,7 +817,7 @@ __global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_chain(const 
     for (int buf = 0; unit.there; buf ^= 1) {
         if (unit.chunk > unit.last) {
             if (threadIdx.x == THREADS - 64) s_ticket[buf] = queue.take();
-            put_zeros<T, VEC>(a, unit, BWD ? 3 : 1);
+            put_zeros<T, VEC>(a, unit.b, unit.g, unit.n, unit.chunk, BWD ? 3 : 1);
             lds_barrier();
             unit = Unit(a, queue, __builtin_amdgcn_readfirstlane(s_ticket[buf]), BWD);
         } else if (unit.full()) {
@@ -825,6 +826,190 @@ __global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_chain(const 
             s.template run<false>(a, queue, unit, buf, s_ticket);
         }
     }
+}
+
+// ---- chains that are a block's ---------------------------------------------------------------------------------------------
+// A short chain, or one of so many that they keep all compute units busy to the end, is better off with one block for all of its chunks: the state stays in LDS,
+// nothing is cleared and nobody looks at others' words.  Chain of blocks / blocks' chains, us, forward and backward:
+//   two chunks: 1 x 200 x 1024 bf16 8.7 / 7.8 and 10.3 / 10.2, 16 x 200 x 1024 bf16 11.8 / 9.8 and 13.7 / 12.9 (f32 16.0 / 13.4 and 21.8 / 23.3), 128 x 200 x 1024 bf16
+//     52 / 39 and 79 / 69
+//   three and four, 256 chains and a multiple: 32 x 300 x 1022 bf16 28.5 / 22 and 42.6 / 36.2, 64 x 300 x 512 f32 35.2 / 31.1 and 58.8 / 53.5; 128 x 500 x 1024 f32 183 / 170 and
+//     319 / 317; 16 x 500 x 1024 bf16 19.8 / 18.1 and 28.8 / 28.8; a few more than that: 33 x 500 x 1024 bf16 34 / 37 and 52 / 60; few: 8 x 500 x 1024 bf16 13.0 / 14.7 and 15.6 / 21.5
+//   more of them: 32 x 1000 x 1024 bf16 60 / 58 and 101 / 106; of unequal length 64 x 2000 x 512 f32 166 / 185 and 311 / 338
+// (The next chunk's gates requested while this one's maps are folded: 17 registers in memory with bf16 gates, 22 -> 30.5 us of 32 x 300 x 1022.)
+static bool walks(long long chains, int chunks) {
+    if (chunks < 2 || chains > 1 << 22) return false;      // (a grid has fewer than 2^32 threads)
+    if (chunks == 2) return true;
+    return chunks <= 4 && chains >= 512 && (chains + 255) / 256 * 256 <= chains + chains / 16;
+}
+template <bool BWD> struct Walk {
+    int b, g, n, last, chunk;
+    bool there;
+    __device__ __forceinline__ explicit Walk(const ScanArgs &a) {
+        // neighbours are one XCD's
+        const int q = (int)(blockIdx.x % kXcds);
+        const unsigned first = (unsigned)(a.chains * q / kXcds), chain = first + blockIdx.x / kXcds;
+        there = chain < (unsigned)(a.chains * (q + 1) / kXcds);
+        b = (int)(chain / (unsigned)a.groups_h);
+        g = (int)(chain - (unsigned)b * (unsigned)a.groups_h);
+        n = there && a.len ? clamp_len(a.len[b], a.T) : a.T;
+        last = n > 0 ? (n - 1) / ECHO_SCAN_CHUNK : 0;
+        chunk = BWD ? last : 0;
+    }
+    __device__ __forceinline__ bool full(int c) const { return (c + 1) * ECHO_SCAN_CHUNK <= n; }
+};
+
+template <typename T, int VEC> struct FwdWalk {
+    static constexpr int GROUPS = kChunkGroups, WIDTH = 16 * VEC, W = GROUPS / 4;
+    typedef Place<VEC, GROUPS> P;
+    struct Shared { float a[GROUPS][WIDTH], b[GROUPS][WIDTH], wa[2][W][WIDTH], wb[2][W][WIDTH], carry[2][WIDTH]; };
+    template <bool FULL> static __device__ __forceinline__ void run(const ScanArgs &a, const Walk<false> &k, int buf, Shared &s) {
+        const P p(a, k.b, k.g, k.n, k.chunk);
+        const Folder<VEC> f(a, k.b, k.g, true);
+        const int w = wave_id();
+        const Row<const T, FULL> G(a, a.G, 3 * a.H, p, k.chunk);
+        Lanes<T, VEC> x[kSteps][3];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) x[i][j].load(G.at(a, p, i, 3 * a.H, j * a.H, true));
+        float A[kSteps][VEC], b[kSteps][VEC];
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float y[VEC], z[VEC];
+            x[i][0].get(y);
+            x[i][1].get(z);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                const bool in = FULL || p.in(i);
+                const float u = in ? forget_rest(y[v]) : 0.f, g = in ? candidate(z[v]) : 0.f;
+                const float b0 = i ? b[i ? i - 1 : 0][v] : 0.f, A0 = i ? A[i ? i - 1 : 0][v] : 1.f;
+                b[i][v] = __builtin_fmaf(u, g - b0, b0);
+                A[i][v] = __builtin_fmaf(-u, A0, A0);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            s.a[p.group][p.slot + v] = A[kSteps - 1][v];
+            s.b[p.group][p.slot + v] = b[kSteps - 1][v];
+        }
+        settle();
+        {
+            float all, sum;
+            FourMaps<WIDTH, false> m;
+            m.read(s.a + 4 * w, s.b + 4 * w, f.lane);
+            m.total(all, sum);
+            if (f.on) s.wa[buf][w][f.lane] = all, s.wb[buf][w][f.lane] = sum;
+        }
+        lds_barrier();
+        if (f.on) {
+            WaveMaps<WIDTH, W, false> wm;
+            wm.read(s.wa[buf], s.wb[buf], f.lane);
+            FourMaps<WIDTH, false> m;
+            m.read(s.a + 4 * w, s.b + 4 * w, f.lane);
+            const float state = wm.state(s.carry[buf][f.lane], w), end = m.write(s.b + 4 * w, f.lane, state);
+            if (w == 0 && a.states && f.own) a.states[((size_t)k.b * a.chunks + k.chunk) * a.H + f.ch] = state;
+            if (w == W - 1) {
+                s.carry[buf ^ 1][f.lane] = end;
+                if (a.last && f.own && k.chunk == k.last) a.last[f.row] = end;
+            }
+        }
+        settle();
+        const Row<T, FULL> h(a, a.out, a.H, p, k.chunk);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            float y[VEC];
+            x[i][2].get(y);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                const float c = __builtin_fmaf(A[i][v], s.b[p.group][p.slot + v], b[i][v]);
+                y[v] = FULL || p.in(i) ? gate(y[v]) * c : 0.f;
+            }
+            if (p.on && (FULL || p.s0 + i < a.T)) put_from<T, VEC>(h.at(a, p, i, a.H, 0, false), y, p.skip, a.whole);
+        }
+    }
+};
+
+template <typename T, int VEC> __global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_fwd_walk(const ScanArgs a) {
+    typedef FwdWalk<T, VEC> F;
+    __shared__ typename F::Shared s;
+    Walk<false> k(a);
+    if (!k.there) return;
+    const Folder<VEC> f(a, k.b, k.g, true);
+    if (wave_id() == 0 && f.on) s.carry[0][f.lane] = a.first ? a.first[f.row] : 0.f;
+    for (int buf = 0; k.chunk <= k.last; ++k.chunk, buf ^= 1) {
+        if (k.full(k.chunk)) F::template run<true>(a, k, buf, s);
+        else F::template run<false>(a, k, buf, s);
+    }
+    for (; k.chunk < a.chunks; ++k.chunk) put_zeros<T, VEC>(a, k.b, k.g, k.n, k.chunk, 1);
+}
+
+template <typename T, int VEC> struct BwdWalk {
+    static constexpr int GROUPS = kChunkGroups, WIDTH = 16 * VEC, W = GROUPS / 4;
+    typedef Place<VEC, GROUPS> P;
+    struct Shared { float a[GROUPS][WIDTH], b[GROUPS][WIDTH], r[GROUPS][WIDTH], wa[2][W][WIDTH], wb[2][W][WIDTH], wr[2][W][WIDTH], carry[2][WIDTH]; };
+    template <bool FULL> static __device__ __forceinline__ void run(const ScanArgs &a, const Walk<true> &k, int buf, Shared &s) {
+        const P p(a, k.b, k.g, k.n, k.chunk);
+        const Folder<VEC> f(a, k.b, k.g, true);
+        const int w = wave_id();
+        Back<VEC> x;
+        const float first = a.states[((size_t)k.b * a.chunks + k.chunk) * a.H + f.ch];
+        x.template load<FULL, T>(a, p, Row<const T, FULL>(a, a.G, 3 * a.H, p, k.chunk), Row<const T, FULL>(a, a.dh, a.H, p, k.chunk));
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) x.maps(v, s.a[p.group][p.slot + v], s.b[p.group][p.slot + v], s.r[p.group][p.slot + v]);
+        settle();
+        {
+            float all, sum, rest;
+            FourMaps<WIDTH, false> m;
+            m.read(s.a + 4 * w, s.b + 4 * w, f.lane);
+            m.total(all, sum);
+            FourMaps<WIDTH, true> r;
+            r.read(s.a + 4 * w, s.r + 4 * w, f.lane);
+            r.total(all, rest);
+            if (f.on) s.wa[buf][w][f.lane] = all, s.wb[buf][w][f.lane] = sum, s.wr[buf][w][f.lane] = rest;
+        }
+        lds_barrier();
+        if (f.on) {
+            {
+                WaveMaps<WIDTH, W, false> wm;
+                wm.read(s.wa[buf], s.wb[buf], f.lane);
+                FourMaps<WIDTH, false> m;
+                m.read(s.a + 4 * w, s.b + 4 * w, f.lane);
+                m.write(s.b + 4 * w, f.lane, wm.state(first, w));
+            }
+            WaveMaps<WIDTH, W, true> wr;
+            wr.read(s.wa[buf], s.wr[buf], f.lane);
+            FourMaps<WIDTH, true> r;
+            r.read(s.a + 4 * w, s.r + 4 * w, f.lane);
+            const float end = r.write(s.r + 4 * w, f.lane, wr.state(s.carry[buf][f.lane], w));
+            if (w == 0) {
+                s.carry[buf ^ 1][f.lane] = end;
+                if (a.last && f.own && k.chunk == 0) a.last[f.row] = end;
+            }
+        }
+        settle();
+        float c[VEC], q[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+            c[v] = s.b[p.group][p.slot + v];
+            q[v] = s.r[p.group][p.slot + v];
+        }
+        x.template store<FULL, T>(a, p, Row<T, FULL>(a, a.out, 3 * a.H, p, k.chunk), c, q);
+    }
+};
+
+template <typename T, int VEC> __global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_bwd_walk(const ScanArgs a) {
+    typedef BwdWalk<T, VEC> B;
+    __shared__ typename B::Shared s;
+    Walk<true> k(a);
+    if (!k.there) return;
+    const Folder<VEC> f(a, k.b, k.g, true);
+    if (wave_id() == 0 && f.on) s.carry[0][f.lane] = a.first ? a.first[f.row] : 0.f;
+    for (int buf = 0; k.chunk >= 0; --k.chunk, buf ^= 1) {
+        if (k.full(k.chunk)) B::template run<true>(a, k, buf, s);
+        else B::template run<false>(a, k, buf, s);
+    }
+    for (int chunk = k.last + 1; chunk < a.chunks; ++chunk) put_zeros<T, VEC>(a, k.b, k.g, k.n, chunk, 3);
 }
 
 static echo_status_t check_scan(const echo_scan_desc_t *d) {
@@ -842,7 +1027,7 @@ static bool unaligned_scan(std::initializer_list<const void *> ps) {
     return (m & 15u) != 0;
 }
 
-// Words and ticket of the chains.  Nothing where all steps are one chunk's.
+// Words and tickets of the chains.  Nothing where all steps are one chunk's, or a chain is one block's.
 struct ScanPlan {
     int vec, groups_h, chunks;
     long long chains;
@@ -855,7 +1040,7 @@ static ScanPlan scan_plan(const echo_scan_desc_t &d) {
     p.groups_h = (d.H + 16 * p.vec - 1) / (16 * p.vec);
     p.chunks = (int)scan_chunks(d);
     p.chains = (long long)d.B * p.groups_h;
-    if (p.chunks > 1) {
+    if (p.chunks > 1 && !walks(p.chains, p.chunks)) {
         p.bytes = kQueues * kTicketStride * 8 + (size_t)p.chains * p.chunks * 16 * p.vec * 8;
         // as many queues as there are chains, or a number up to kQueues that deals them out evenly
         long long least = p.chains * 2;
@@ -880,6 +1065,13 @@ template <typename T, int VEC, int GROUPS> static echo_status_t launch_scan(Scan
     return ECHO_OK;
 }
 template <typename T, int VEC> static echo_status_t launch_scan(const ScanArgs &a, bool bwd, hipStream_t st) {
+    if (walks(a.chains, a.chunks)) {
+        const unsigned blocks = (unsigned)((a.chains + kXcds - 1) / kXcds * kXcds);
+        LaunchRecord r = launch_begin(bwd ? "scan_bwd_walk" : "scan_fwd_walk", st);
+        if (bwd) k_scan_bwd_walk<T, VEC><<<blocks, kThreads<kChunkGroups>, 0, st>>>(a);
+        else k_scan_fwd_walk<T, VEC><<<blocks, kThreads<kChunkGroups>, 0, st>>>(a);
+        return launch_end(r);
+    }
     if (a.chunks > 1) {
         // as many blocks as the chip holds, the same number for each queue
         const unsigned blocks = (unsigned)((std::min<long long>(a.chains * a.chunks, 256 * kBlocks) + a.queues - 1) / a.queues * a.queues);

@@ -171,6 +171,21 @@ def test_lengths_at_the_ends_of_chunks(store, reverse):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("B,T,H,store", [(5, 129, 66, "f32"), (3, 255, 130, "bf16"), (9, 256, 3, "f32"), (40, 200, 64, "bf16"),      # two chunks
+                                         (8, 260, 4094, "bf16"), (16, 385, 2047, "f32"), (2, 512, 16384, "f32"),                    # many chains of three or four
+                                         (7, 260, 4094, "bf16")])                                                                  # a few less
+@pytest.mark.parametrize("reverse", [False, True])
+def test_chains_of_one_block_and_of_many(B, T, H, store, reverse):
+    r = np.random.default_rng(B)
+    lengths = r.integers(0, T + 1, B)
+    lengths[:5] = [T, 128, 0, 129, 1][:B]
+    p = Problem(B, T, H, store, reverse, lengths.tolist(), seed=21)
+    got = p.run(in_place=True)
+    p.check(got)
+    again = p.run(in_place=True)
+    assert all(np.array_equal(got[k], again[k]) for k in got)
+
+
 def test_more_units_than_blocks():
     """222 chains of 3 chunks, which the blocks take in turns from queues of unequal length, a third of them empty; most sequences are short."""
     r = np.random.default_rng(21)
