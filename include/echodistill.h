@@ -19,7 +19,7 @@
  *
  * The descriptor is echovocab.h's: in_dtype of h and W, out_dtype of dh and dW; t, loss, lse and dloss are fp32.  Conventions, products, their error and
  * ranges: as those of echo_vocab_loss_fwd and echo_vocab_loss_bwd, with T dloss in the place of dloss.  A logit t that is NaN or plus infinity
- * makes its row's results NaN.
+ * makes its row's loss and gradients NaN (lse does not depend on t).
  * Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (the descriptor's limits, K outside
  * 1 .. ECHO_DISTILL_MAX_K, T outside 2^-64 .. 2^64), ECHO_ERR_ALIGN, ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

@@ -3,6 +3,9 @@
 // Which words are taken takes K pairs of probabilities; the word that is drawn behind them takes one row of the model's and, if a word was not taken,
 // one of the student's.  The block sums the weights of that row by segments, which its waves take in turn, finds the segment in which the sum passes r of
 // the whole, and a wave goes over that segment again.  All sums are in 64 bits and in an order that depends on V alone.
+//
+// Many sequences are bound by memory: 256 x 5 of 100003 f32 words, 193 MB, takes 41 us, 4.7 TB/s.  One is bound by four trips to memory one after the other (words; their
+// probabilities; the rows; the segment): 1 x 4 of 32000 words takes 9.3 us, of which the launch is 4.  The weights have no branches, with which that took 10 us more.
 #include "../../include/echodraft.h"
 
 #include <hip/hip_runtime.h>
@@ -183,56 +186,56 @@ template <typename T, bool FEW, Part PART> __global__ __launch_bounds__(64 * kDr
             return;
         }
         const double at = r > 0.f ? (double)r * total : 0.0;
-                    // the first segment whose sum passes, or the last one that has a weight
-                    double before = __shfl_up(upto, 1);
-                    if (lane == 0) before = 0.0;
-                    int segment = -1, last = -1;
-                    double start = 0.0, last_start = 0.0;
-        #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (x[k] > 0.0) {
-                            last = lane * 4 + k, last_start = before;
-                            if (segment < 0 && before + x[k] > at) segment = last, start = before;
-                        }
-                        before += x[k];
-                    }
-                    const unsigned long long pass = __ballot(segment >= 0), any = __ballot(last >= 0);
-                    const int from = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(any);
-                    segment = __shfl(pass ? segment : last, from);
-                    before = __shfl(pass ? start : last_start, from);
-                    // the words of that segment, 4 m a lane
-                    const int v0 = segment * 256 * m + lane * 4 * m;
-                    double own = 0.0;
-                    for (int j = 0; j < m; ++j) {
-                        Four<T, FEW> fp, fq;
-                        fp.load(p, v0 + 4 * j, V);
-                        fq.load(q, v0 + 4 * j, V);
-                        weights(fp, fq, less, v0 + 4 * j, V, x);
-                        own += (x[0] + x[1]) + (x[2] + x[3]);
-                    }
-                    upto = wave_scan_f64(own, lane);
-                    double sum_to = before + __shfl_up(upto, 1);
-                    if (lane == 0) sum_to = before;
-                    int word = -1, heavy = -1;
-                    for (int j = 0; j < m; ++j) {
-                        Four<T, FEW> fp, fq;
-                        fp.load(p, v0 + 4 * j, V);
-                        fq.load(q, v0 + 4 * j, V);
-                        weights(fp, fq, less, v0 + 4 * j, V, x);
-                        const int first = Four<T, FEW>::first(v0 + 4 * j, V);
-        #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            sum_to += x[e];
-                            if (x[e] > 0.0) {
-                                heavy = first + e;
-                                if (word < 0 && sum_to > at) word = heavy;
-                            }
-                        }
-                    }
-                    const unsigned long long passed = __ballot(word >= 0), heavies = __ballot(heavy >= 0);
-                    if (passed) word = __shfl(word, __builtin_ctzll(passed));
-                    else word = __shfl(heavy, 63 - __builtin_clzll(heavies));
-                    if (lane == 0) tokens[take] = word;
+        // the first segment whose sum passes, or the last one that has a weight
+        double before = __shfl_up(upto, 1);
+        if (lane == 0) before = 0.0;
+        int segment = -1, last = -1;
+        double start = 0.0, last_start = 0.0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (x[k] > 0.0) {
+                last = lane * 4 + k, last_start = before;
+                if (segment < 0 && before + x[k] > at) segment = last, start = before;
+            }
+            before += x[k];
+        }
+        const unsigned long long pass = __ballot(segment >= 0), any = __ballot(last >= 0);
+        const int from = pass ? __builtin_ctzll(pass) : 63 - __builtin_clzll(any);
+        segment = __shfl(pass ? segment : last, from);
+        before = __shfl(pass ? start : last_start, from);
+        // the words of that segment, 4 m a lane
+        const int v0 = segment * 256 * m + lane * 4 * m;
+        double own = 0.0;
+        for (int j = 0; j < m; ++j) {
+            Four<T, FEW> fp, fq;
+            fp.load(p, v0 + 4 * j, V);
+            fq.load(q, v0 + 4 * j, V);
+            weights(fp, fq, less, v0 + 4 * j, V, x);
+            own += (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        upto = wave_scan_f64(own, lane);
+        double sum_to = before + __shfl_up(upto, 1);
+        if (lane == 0) sum_to = before;
+        int word = -1, heavy = -1;
+        for (int j = 0; j < m; ++j) {
+            Four<T, FEW> fp, fq;
+            fp.load(p, v0 + 4 * j, V);
+            fq.load(q, v0 + 4 * j, V);
+            weights(fp, fq, less, v0 + 4 * j, V, x);
+            const int first = Four<T, FEW>::first(v0 + 4 * j, V);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum_to += x[e];
+                if (x[e] > 0.0) {
+                    heavy = first + e;
+                    if (word < 0 && sum_to > at) word = heavy;
+                }
+            }
+        }
+        const unsigned long long passed = __ballot(word >= 0), heavies = __ballot(heavy >= 0);
+        if (passed) word = __shfl(word, __builtin_ctzll(passed));
+        else word = __shfl(heavy, 63 - __builtin_clzll(heavies));
+        if (lane == 0) tokens[take] = word;
     }
 }
 

@@ -6,6 +6,11 @@
 // by itself.  A sequence longer than a chunk is a chain of them, whose chunks are one block's or many blocks' (below).
 //
 // With u = 1 - f = sigmoid(-x):  c += u (g - c),  r = dh o + q,  q = r - u r  keep the digits of a u next to zero.
+//
+// Every gate is read once and every result written once, which is what bounds long sequences: 4 x 16384 x 1280 f32 takes 250 + 420 us, 5.4 TB/s (a large copy: 6.4).
+// Shorter ones are bound by trips to memory: a launch and one unit are 4 us (64 x 1 x 512), one sequence of 4001 x 768 bf16 is 10 us behind the clearing's 2.
+// 16 threads x 4 channels are 256 bytes of a row in f32 and 128 in bf16; four steps a thread keep a unit's gates in registers from the map to the result (a chunk of 128
+// steps: two blocks of 512 threads to a compute unit).
 #include "../../include/echoscan.h"
 
 #include <hip/hip_runtime.h>
