@@ -268,6 +268,31 @@ def test_a_NaN_stays_with_its_sequence_and_channel():
     assert not np.isnan(got["dG"][[0, 2]]).any() and not np.isnan(got["h"][1, :150]).any()
 
 
+@pytest.mark.parametrize("store", ["f32", "bf16"])
+def test_longer_chains(store):
+    """What the tests above show for chunks of one block, for those that are handed on: states left out, saturated gates, a NaN."""
+    p = Problem(3, 600, 37, store, lengths=None, c0=False, dc_last=False, seed=11)
+    p.check(p.run())
+    p.check(p.run(want_last=False))
+    for scale in (30.0, 1e4):
+        p = Problem(2, 600, 8, store, scale=scale, seed=12)
+        with np.errstate(over="ignore"):
+            p.check(p.run())
+    p = Problem(3, 700, 9, store, seed=13)
+    clean = p.run()
+    p.G[1, 150, 4] = float("nan")                           # a gate that forgets
+    p.G[1, 450, 9 + 6] = float("nan")                       # a candidate
+    got = p.run()
+    for ch, t in ((4, 150), (6, 450)):
+        assert np.isnan(got["h"][1, t:, ch]).all() and np.isnan(got["c_last"][1, ch]) and np.isnan(got["dc0"][1, ch]) == (ch == 4)
+        assert np.array_equal(got["h"][1, :t, ch], clean["h"][1, :t, ch])
+    rest = np.setdiff1d(np.arange(9), [4, 6])
+    for k in ("h", "c_last", "dc0"):
+        assert np.array_equal(got[k][..., rest], clean[k][..., rest]) and np.array_equal(got[k][[0, 2]], clean[k][[0, 2]])
+    three = np.concatenate([rest, 9 + rest, 18 + rest])
+    assert np.array_equal(got["dG"][..., three], clean["dG"][..., three])
+
+
 def test_lengths_outside_their_range():
     p = Problem(3, 6, 5, lengths=[-3, 6, 4], seed=7)
     want = p.run()
@@ -288,7 +313,7 @@ def test_on_another_stream_and_two_at_once():
         assert all(np.array_equal(got[k], w[k]) for k in w)
 
 
-@pytest.mark.parametrize("T", [3, 60, 1000])
+@pytest.mark.parametrize("T", [3, 60, 200, 1000])
 def test_captured_and_replayed(T):
     torch, eb, types = _torch()
     p = Problem(2, T, 72, lengths="random", seed=10)
@@ -326,10 +351,10 @@ def test_captured_and_replayed(T):
         assert all(torch.equal(out[key], want[key]) for key in out), k
 
 
-def test_offsets_past_32_bits():
+@pytest.mark.parametrize("B,T,H", [(3, 4096, 65536), (3, 256, 1 << 20), (6, 120, 1 << 20)])      # many blocks' chains, a block's, one chunk
+def test_offsets_past_32_bits(B, T, H):
     """G of 2^31.2 numbers: the last sequence against the same one by itself."""
     torch, eb, _ = _torch()
-    B, T, H = 3, 4096, 65536
     st = torch.cuda.current_stream()
     G = torch.empty(B, T, 3 * H, dtype=torch.bfloat16, device="cuda")
     g = torch.Generator(device="cuda").manual_seed(11)
