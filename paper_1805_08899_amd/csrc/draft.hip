@@ -185,7 +185,8 @@ template <typename T, bool FEW, Part PART> __global__ __launch_bounds__(64 * kDr
             if (lane == 0) tokens[take] = -1;
             return;
         }
-        const double at = r > 0.f ? (double)r * total : 0.0;
+        // (from 1 on no sum passes: sums in other orders than the total's may lie a rounding above it)
+        const double at = r >= 1.f ? __builtin_inf() : r > 0.f ? (double)r * total : 0.0;
         // the first segment whose sum passes, or the last one that has a weight
         double before = __shfl_up(upto, 1);
         if (lane == 0) before = 0.0;
