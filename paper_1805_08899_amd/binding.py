@@ -498,8 +498,8 @@ def echo_draft_verify_workspace_bytes(desc) -> int:
 def echo_draft_verify(desc, drafted, n_drafted, draft, target, u, r, tokens, taken, workspace, workspace_bytes=None,
                       stream=None) -> int:
     return lib().echo_draft_verify(ctypes.byref(desc), _words(drafted, desc.B, desc.K), _index(n_drafted, desc.B), _ptr(draft),
-                                   _ptr(target), _ptr(u), _ptr(r), _ptr(tokens), _ptr(taken), _ptr(workspace),
-                                   _ws_bytes(workspace, workspace_bytes), _stream(stream))
+                                   _ptr(target), _ptr(u), _ptr(r), _words(tokens, desc.B, desc.K + 1), _index(taken, desc.B),
+                                   _ptr(workspace), _ws_bytes(workspace, workspace_bytes), _stream(stream))
 
 
 def echo_status_string(status: int) -> str:

@@ -161,6 +161,11 @@ struct Index : Ptr<const int32_t> {                        // tokens, labels, ke
     }
 };
 struct Words : Index {};                                   // so many per row: the number behind the next argument, or the descriptor's K
+struct IndexOut : Index {                                  // the same where the call writes them
+    using C = int32_t *;
+    C value() const { return static_cast<C>(p); }
+};
+struct WordsOut : IndexOut {};                             // the descriptor's K and one more per row
 struct Stream {
     using C = void *;
     void *p = nullptr;
@@ -301,6 +306,8 @@ bool resolve(Words &x, PyObject *const *slot, const VocabDesc &d) {
     return int_value(slot[2], k) && x.resolve(slot[0], both(d.value()->N, static_cast<int32_t>(k)));
 }
 bool resolve(Words &x, PyObject *const *slot, const DraftDesc &d) { return x.resolve(slot[0], both(d.value()->B, d.value()->K)); }
+bool resolve(IndexOut &x, PyObject *const *slot, const DraftDesc &d) { return x.resolve(slot[0], d.value()->B); }
+bool resolve(WordsOut &x, PyObject *const *slot, const DraftDesc &d) { return x.resolve(slot[0], both(d.value()->B, (int64_t)d.value()->K + 1)); }
 
 template <typename... K, size_t... I>
 PyObject *call_with(Names &n, PyObject **slot, std::index_sequence<I...>) {
@@ -362,7 +369,7 @@ using ScanFwd = Call<24, ScanDesc, In, InF, Index, Work, OutF, OutF, Work, Bytes
 using ScanBwd = Call<25, ScanDesc, In, InF, In, Index, InF, Work, OutF, Work, Bytes, Stream>;
 using DistillFwd = Call<26, VocabDesc, In, In, Words, InF, I32, Float, OutF, OutF, Work, Bytes, Stream>;
 using DistillBwd = Call<27, VocabDesc, InF, InF, In, In, Words, InF, I32, Float, Work, Work, Work, Bytes, Stream>;
-using DraftVerify = Call<28, DraftDesc, Words, Index, In, In, InF, InF, Ptr<int32_t>, Ptr<int32_t>, Work, Bytes, Stream>;
+using DraftVerify = Call<28, DraftDesc, Words, Index, In, In, InF, InF, WordsOut, IndexOut, Work, Bytes, Stream>;
 
 #define NAMES(CALL, FN, REQUIRED, ...) template <> Names CALL::names = {FN, {__VA_ARGS__, nullptr}, REQUIRED, {}, 0, nullptr}
 NAMES(Fwd, "echo_attn_fwd", 9, "desc", "Qp", "Kp", "V", "v", "key_len", "context", "P", "workspace", "workspace_bytes", "stream");
