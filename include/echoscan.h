@@ -29,7 +29,8 @@
  * dc_last, which may be one buffer.
  *   - dtype: storage of G, h, dh and dG, each rounded once, to nearest even, from fp32.  c0, c_last, dc_last, dc0 and the kept states are
  *     fp32, and so are all gates, states and sums.
- *   - 1 - f is taken as sigmoid(-x), which keeps its digits where a gate forgets next to nothing; f itself is 1 minus that, off by up to 2^-24.
+ *   - f and 1 - f = sigmoid(-x) are each good to a few units of their own last place: what a gate that is nearly closed lets through, and its gradient, keep their
+ *     digits as those of a gate that forgets next to nothing do.  o (1 - o) and 1 - g^2 are formed from o and g as fp32 has them, off by up to 2^-23.
  *   - Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (a limit below), ECHO_ERR_ALIGN,
  *     ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

@@ -5,7 +5,10 @@
 // its four groups in LDS, a lane per channel, and every wave those of the waves in front of it; from the state in front of its own, every thread goes on
 // by itself.  A sequence longer than a chunk is a chain of them, whose chunks are one block's or many blocks' (below).
 //
-// With u = 1 - f = sigmoid(-x):  c += u (g - c),  r = dh o + q,  q = r - u r  keep the digits of a u next to zero.
+// f and u = 1 - f = sigmoid(-x) are each good to a few units of their own last place, the smaller one as e / (1 + e) with e = 2^(-|x| log2 e): with f as 1 - u, what
+// a gate at -12 lets through would be off by 1 % and nothing be left from -17 on.  A thread that keeps a gate keeps the smaller of both, f with its sign
+// set (Forget below).  It costs a selection per gate where either is wanted: both passes of 64 x 50 x 512 f32 11.7 -> 12.4 us, of 4 x 16384 x 1280 bf16 414 -> 433,
+// of f32 none.
 //
 // Every gate is read once and every result written once, which is what bounds long sequences: 4 x 16384 x 1280 f32 takes 250 + 420 us, 5.4 TB/s (a large copy: 6.4).
 // Shorter ones are bound by trips to memory: a launch and one unit are 4 us (64 x 1 x 512), one sequence of 4001 x 768 bf16 is 10 us behind the clearing's 2.
@@ -34,9 +37,33 @@ constexpr float kLog2eS = 1.4426950408889634f;
 
 // sigmoid(x) = 1 / (1 + 2^(-x log2 e)); tanh(x) = 1 - 2 / (2^(2 x log2 e) + 1).  exp2 overflows to infinity, whose reciprocal is 0.
 __device__ __forceinline__ float gate(float x) { return fast_rcp(1.0f + fast_exp2(-kLog2eS * x)); }
-__device__ __forceinline__ float forget_rest(float x) { return fast_rcp(1.0f + fast_exp2(kLog2eS * x)); }   // 1 - sigmoid(x)
+// f = sigmoid(x) and u = 1 - f from the smaller one, `least`, as a thread keeps it: f with its sign set, or u; 0, an open gate, for a step that is none of the sequence's
+struct Forget {
+    float least;
+    bool f_least;
+    static __device__ __forceinline__ float pack(float x) {
+        const float e = fast_exp2(-kLog2eS * fabsf(x));
+        return copysignf(e * fast_rcp(1.0f + e), x);
+    }
+    __device__ __forceinline__ explicit Forget(float packed) : least(fabsf(packed)), f_least(__float_as_int(packed) < 0) {}
+    __device__ __forceinline__ float f() const { return f_least ? least : 1.0f - least; }
+    __device__ __forceinline__ float u() const { return f_least ? 1.0f - least : least; }
+    // f c + u g: from the one of c and g that counts more, `least` of the way to the other
+    __device__ __forceinline__ float step(float c, float g) const {
+        const float more = f_least ? g : c, less = f_least ? c : g;
+        return __builtin_fmaf(least, less - more, more);
+    }
+};
 __device__ __forceinline__ float candidate(float x) {
     return __builtin_fmaf(-2.0f, fast_rcp(fast_exp2(kTwoLog2e * x) + 1.0f), 1.0f);
+}
+// A thread's map of its steps up to step i, from that of those in front: c -> A c + b.  x: the forget gate's; in: the step is the sequence's
+template <int VEC> __device__ __forceinline__ void add_step(float (&A)[kSteps][VEC], float (&b)[kSteps][VEC], int i, int v, float x, float g, bool in) {
+    const float e = fast_exp2(-kLog2eS * fabsf(x)), most = fast_rcp(1.0f + e), least = e * most;
+    const float f = x < 0.f ? least : most, u = x < 0.f ? most : least;
+    const float b0 = i ? b[i ? i - 1 : 0][v] : 0.f, A0 = i ? A[i ? i - 1 : 0][v] : 1.f;
+    b[i][v] = in ? __builtin_fmaf(f, b0, u * g) : b0;
+    A[i][v] = in ? f * A0 : A0;
 }
 
 // VEC consecutive channels of a row as they stand in memory; rows begin at any element
@@ -259,28 +286,29 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
                 if (v >= p.skip) a.states[(size_t)p.b * a.H + p.ch + v] = c[v];
         }
     }
-    float u[kSteps][VEC], g[kSteps][VEC];
+    // GROUPS of 1: the forget gate as kept, and the candidate, step by step; else the maps of the thread's first steps
+    float A[kSteps][VEC], b[kSteps][VEC];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        float y[VEC];
+        float y[VEC], z[VEC];
         x[i][0].get(y);
+        x[i][1].get(z);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) u[i][v] = p.in(i) ? forget_rest(y[v]) : 0.f;
-        x[i][1].get(y);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) g[i][v] = p.in(i) ? candidate(y[v]) : 0.f;
+        for (int v = 0; v < VEC; ++v) {
+            const float g = candidate(z[v]);
+            if constexpr (GROUPS == 1) {
+                A[i][v] = p.in(i) ? Forget::pack(y[v]) : 0.f;
+                b[i][v] = p.in(i) ? g : 0.f;
+            } else {
+                add_step(A, b, i, v, y[v], g, p.in(i));
+            }
+        }
     }
     if constexpr (GROUPS > 1) {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-            float A = 1.f, b = 0.f;
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
-                A = __builtin_fmaf(-u[i][v], A, A);
-            }
-            s_a[own][p.slot + v] = A;
-            s_b[own][p.slot + v] = b;
+            s_a[own][p.slot + v] = A[kSteps - 1][v];
+            s_b[own][p.slot + v] = b[kSteps - 1][v];
         }
         if (a.states && f.own && w % W == 0) a.states[f.row] = state;
         settle();
@@ -308,8 +336,14 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
         x[i][2].get(y);
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-            c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
-            y[v] = p.in(i) ? gate(y[v]) * c[v] : 0.f;
+            float at;
+            if constexpr (GROUPS == 1) {
+                // step by step from call to call: f as a factor would lose a third of a percent of a gate that forgets 1e-5 to its rounding, the same in every step
+                at = c[v] = Forget(A[i][v]).step(c[v], b[i][v]);
+            } else {
+                at = __builtin_fmaf(A[i][v], c[v], b[i][v]);
+            }
+            y[v] = p.in(i) ? gate(y[v]) * at : 0.f;
         }
         if (p.on && p.s0 + i < a.T) put_from<T, VEC>(h.at(a, p, i, a.H, 0, false), y, p.skip, a.whole);
     }
@@ -322,7 +356,7 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
     }
 }
 
-// A thread's kSteps steps backwards: its gates and dh (u = g = o = d = 0 at steps that are none of the sequence's)
+// A thread's kSteps steps backwards: its gates, u as kept, and dh (u = g = o = d = 0 at steps that are none of the sequence's)
 template <int VEC> struct Back {
     float u[kSteps][VEC], g[kSteps][VEC], o[kSteps][VEC], d[kSteps][VEC];
     template <bool FULL, typename T, typename P>
@@ -340,7 +374,7 @@ template <int VEC> struct Back {
             float y[VEC];
             x[i][0].get(y);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) u[i][v] = in ? forget_rest(y[v]) : 0.f;
+            for (int v = 0; v < VEC; ++v) u[i][v] = in ? Forget::pack(y[v]) : 0.f;
             x[i][1].get(y);
 #pragma unroll
             for (int v = 0; v < VEC; ++v) g[i][v] = in ? candidate(y[v]) : 0.f;
@@ -357,11 +391,11 @@ template <int VEC> struct Back {
         A = 1.f, b = 0.f, R = 0.f;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
-            b = __builtin_fmaf(u[i][v], g[i][v] - b, b);
-            A = __builtin_fmaf(-u[i][v], A, A);
+            const Forget at(u[i][v]);
+            b = __builtin_fmaf(at.f(), b, at.u() * g[i][v]);
+            A *= at.f();
             const int k = kSteps - 1 - i;
-            const float r = __builtin_fmaf(d[k][v], o[k][v], R);
-            R = __builtin_fmaf(-u[k][v], r, r);
+            R = Forget(u[k][v]).f() * __builtin_fmaf(d[k][v], o[k][v], R);
         }
     }
     // dG from the state in front of the thread's steps and the q behind them; q: that in front of them
@@ -373,7 +407,7 @@ template <int VEC> struct Back {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 before[i][v] = c[v];
-                c[v] = __builtin_fmaf(u[i][v], g[i][v] - c[v], c[v]);
+                c[v] = Forget(u[i][v]).step(c[v], g[i][v]);
             }
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
@@ -382,12 +416,13 @@ template <int VEC> struct Back {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 const float r = __builtin_fmaf(d[i][v], o[i][v], q[v]);
-                const float ru = r * u[i][v];
-                df[v] = __builtin_fmaf(-ru, u[i][v], ru) * (before[i][v] - g[i][v]);
+                const Forget k(u[i][v]);
+                const float part = r * k.least, rest = r - part, ru = k.f_least ? rest : part;
+                df[v] = __builtin_fmaf(-part, k.least, part) * (before[i][v] - g[i][v]);
                 dg[v] = ru * __builtin_fmaf(-g[i][v], g[i][v], 1.f);
                 dout[v] = d[i][v] * c[v] * __builtin_fmaf(-o[i][v], o[i][v], o[i][v]);
                 c[v] = before[i][v];
-                q[v] = r - ru;
+                q[v] = k.f_least ? part : rest;
             }
             if (p.on && (FULL || p.s0 + i < a.T)) {
                 put_from<T, VEC>(dG.at(a, p, i, 3 * a.H, 0, false), df, p.skip, a.whole);
@@ -635,13 +670,7 @@ template <typename T, int VEC> struct FwdChain {
             x[i][0].get(y);
             x[i][1].get(z);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const bool in = FULL || p.in(i);
-                const float u = in ? forget_rest(y[v]) : 0.f, g = in ? candidate(z[v]) : 0.f;
-                const float b0 = i ? b[i ? i - 1 : 0][v] : 0.f, A0 = i ? A[i ? i - 1 : 0][v] : 1.f;
-                b[i][v] = __builtin_fmaf(u, g - b0, b0);
-                A[i][v] = __builtin_fmaf(-u, A0, A0);
-            }
+            for (int v = 0; v < VEC; ++v) add_step(A, b, i, v, y[v], candidate(z[v]), FULL || p.in(i));
         }
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
@@ -885,13 +914,7 @@ template <typename T, int VEC> struct FwdWalk {
             x[i][0].get(y);
             x[i][1].get(z);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                const bool in = FULL || p.in(i);
-                const float u = in ? forget_rest(y[v]) : 0.f, g = in ? candidate(z[v]) : 0.f;
-                const float b0 = i ? b[i ? i - 1 : 0][v] : 0.f, A0 = i ? A[i ? i - 1 : 0][v] : 1.f;
-                b[i][v] = __builtin_fmaf(u, g - b0, b0);
-                A[i][v] = __builtin_fmaf(-u, A0, A0);
-            }
+            for (int v = 0; v < VEC; ++v) add_step(A, b, i, v, y[v], candidate(z[v]), FULL || p.in(i));
         }
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
