@@ -31,6 +31,8 @@
  *     fp32, and so are all gates, states and sums.
  *   - f and 1 - f = sigmoid(-x) are each good to a few units of their own last place: what a gate that is nearly closed lets through, and its gradient, keep their
  *     digits as those of a gate that forgets next to nothing do.  o (1 - o) and 1 - g^2 are formed from o and g as fp32 has them, off by up to 2^-23.
+ *   - An infinite c0 stays infinite in h and c_last, an infinite dc_last or dh in dc0, as long as the product of the gates in between is a number of fp32's; behind that
+ *     it is NaN.  In dG, which multiplies and subtracts them, what they reach is infinite or NaN.  Other channels and sequences do not notice.
  *   - Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (a limit below), ECHO_ERR_ALIGN,
  *     ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

@@ -339,7 +339,8 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_fwd(const ScanArgs
             float at;
             if constexpr (GROUPS == 1) {
                 // step by step from call to call: f as a factor would lose a third of a percent of a gate that forgets 1e-5 to its rounding, the same in every step
-                at = c[v] = Forget(A[i][v]).step(c[v], b[i][v]);
+                const Forget k(A[i][v]);
+                at = c[v] = fabsf(c[v]) == __builtin_inff() ? k.f() * c[v] : k.step(c[v], b[i][v]);
             } else {
                 at = __builtin_fmaf(A[i][v], c[v], b[i][v]);
             }
@@ -445,12 +446,16 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
     float state = GROUPS > 1 ? a.states[f.row] : 0.f, back = GROUPS > 1 && a.first ? a.first[f.row] : 0.f;
     Back<VEC> x;
     x.template load<false, T>(a, p, Row<const T, false>(a, a.G, 3 * a.H, p, 0), Row<const T, false>(a, a.dh, a.H, p, 0));
-    float c[VEC], q[VEC];
+    float c[VEC], q[VEC], dc0[VEC];
     if constexpr (GROUPS == 1) {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
             c[v] = a.states[(size_t)p.b * a.H + p.ch + v];
             q[v] = a.first ? a.first[(size_t)p.b * a.H + p.ch + v] : 0.f;
+            // dc0 by the steps' map, as it is of longer sequences
+            float A, b, R;
+            x.maps(v, A, b, R);
+            dc0[v] = __builtin_fmaf(A, q[v], R);
         }
     } else {
 #pragma unroll
@@ -491,7 +496,7 @@ __global__ __launch_bounds__(kThreads<GROUPS>, 4) void k_scan_bwd(const ScanArgs
         if (a.last && p.on) {
 #pragma unroll
             for (int v = 0; v < VEC; ++v)
-                if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = q[v];
+                if (v >= p.skip) a.last[(size_t)p.b * a.H + p.ch + v] = dc0[v];
         }
     }
 }
