@@ -20,6 +20,9 @@
  * The descriptor is echovocab.h's: in_dtype of h and W, out_dtype of dh and dW; t, loss, lse and dloss are fp32.  Conventions, products, their error and
  * ranges: as those of echo_vocab_loss_fwd and echo_vocab_loss_bwd, with T dloss in the place of dloss.  A logit t that is NaN or plus infinity
  * makes its row's loss and gradients NaN (lse does not depend on t).
+ * The loss is the difference of sum_k q log q and sum_k q log p, each of them good to some 2^-23 of its own size times the roundings of the sums behind it: where
+ * student and teacher are nearly sure of the same word both are small and the loss keeps its digits, as that of a sure label does; where they agree on
+ * several words it may be far smaller than either.
  * Errors, before anything is launched: ECHO_ERR_NULL, ECHO_ERR_DTYPE, ECHO_ERR_SHAPE (the descriptor's limits, K outside
  * 1 .. ECHO_DISTILL_MAX_K, T outside 2^-64 .. 2^64), ECHO_ERR_ALIGN, ECHO_ERR_WORKSPACE; ECHO_ERR_HIP for a failed launch.
  */

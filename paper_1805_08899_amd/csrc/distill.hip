@@ -30,15 +30,19 @@ __global__ __launch_bounds__(256) void k_distill_lists(const TeacherLists a) {
         if (in[k]) top = fmaxf(top, x[k]);
     }
     top = wave_max(top);
-    float sum = 0.f;
+    // the sum without the first of the largest, which is 1: log(1 + rest) keeps the digits of a teacher that is sure of a word
+    float rest = 0.f;
+    bool out = false;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         x[k] = (x[k] - top) / a.temperature;
         q[k] = in[k] ? expf(x[k]) : 0.f;
-        sum += q[k];
+        const unsigned long long ones = __ballot(q[k] == 1.f);
+        rest += !out && ones && lane == __builtin_ctzll(ones) ? 0.f : q[k];
+        out |= ones != 0;
     }
-    sum = wave_sum(sum);
-    const float log_sum = logf(sum);
+    rest = wave_sum(rest);
+    const float sum = 1.f + rest, log_sum = log1pf(rest);
     float own = 0.f;
     int label = -1, many = 0;
 #pragma unroll

@@ -18,7 +18,7 @@ struct Teacher {
     const int *words;                // [N][K], ascending
     const float *shares;             // [N][K]
     const unsigned char *start;      // [N][marks]: how many of the row's words are below kMarkWords times the mark's number
-    const float *own;                // [N]: sum of share log share
+    const float *own;                // [N]: sum of share log share, small for a teacher that is sure of a word
     int K, marks;
     float inv_t, temperature;
     __device__ __forceinline__ void from_row(int n) {

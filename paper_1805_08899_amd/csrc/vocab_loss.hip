@@ -373,6 +373,39 @@ __device__ __forceinline__ float scaled_sum(float sum, float from, float to) {
     return from == to ? sum : sum * fast_exp2((from - to) * kLog2e);
 }
 
+// Against a teacher, whose row may be as sure of a word as the student's, a sum of exponentials is kept without the largest one, which is 1 next to the
+// maximum: `rest` and `top` stand for (1 + rest) exp(top), -1 and minus infinity for no exponentials at all.  log(1 + rest) has the digits of a small rest.
+// Where the sum is 1.25 or more, 1 off it leaves rest 5 times the sum's error at most; below that the numbers are added by their fractions: of those in (0, 1] only the 1
+// has none (a forward pass of 6400 x 32000 x 512 bf16, 64 entries a row, 311 us; all numbers by their fractions 322; one sum with the 1 in it 297).
+__device__ __forceinline__ void join_rest(float &top, float &rest, float t, float r) {
+    const bool more = t > top;
+    const float high = more ? t : top, low = more ? top : t;
+    rest = (more ? r : rest) + scaled_sum(1.f + (more ? rest : r), low, high);
+    top = high;
+}
+// The rest of a row of the matrix cores' results (lanes l, l + 16, l + 32, l + 48) from each lane's sum and, where they are wanted, its sum of fractions
+template <bool ASK, typename Fractions> __device__ __forceinline__ float row_rest(float top, float sum, Fractions fractions) {
+    float all = sum + __shfl_xor(sum, 16);
+    all += __shfl_xor(all, 32);
+    float rest = all - 1.f;
+    if (!ASK || __ballot(all < 1.25f)) {                   // (of a few numbers not worth the question)
+        float part = fractions();
+        const float ones = rintf(sum - part);              // likeliest words: the first lane that has one leaves one out
+        const int lane = lane_id();
+        const unsigned long long in_front = (lane < 16 ? 0ull : 0x0001000100010001ull >> (64 - 16 * (lane >> 4)) << (lane & 15));
+        part += ones > 0.f && (__ballot(ones > 0.f) & in_front) == 0 ? ones - 1.f : ones;
+        part += __shfl_xor(part, 16);
+        part += __shfl_xor(part, 32);
+        if (all < 1.25f) rest = top == -__builtin_inff() ? part - 1.f : part;
+    }
+    return rest;
+}
+// The cross entropy of a row is kept as far as it goes beyond the maximum's: the mean, by their shares, of how far its words' logits are below it.  `far` and
+// `share` of a part of the words go to another maximum `to` >= from.
+__device__ __forceinline__ float far_from(float far, float share, float from, float to) {
+    return share != 0.f && from != to ? far + share * (to - from) : far;
+}
+
 // TEACHER: the target is a row's shares among the teacher's words (distill.hpp) instead of its label, and logits are divided by the temperature.
 template <class C, Mode MODE, bool TEACHER = false>
 __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a) {
@@ -401,9 +434,9 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
     const bool tail = a.v0 + m0 + C::BM > a.V;
     typedef TeacherTile<C::TM * 16, C::TN> Shares;
     if constexpr (MODE == Mode::kForward) {
-        float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN;
-        static_assert(3 * C::WM * C::BN * 4 + C::WAVES * Shares::BYTES <= C::LDS_BYTES, "room for the shares");
-        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 3 * C::WM * C::BN, vw - lr, TEACHER, ranges);
+        float *s_max = reinterpret_cast<float *>(lds), *s_sum = s_max + C::WM * C::BN, *s_z = s_sum + C::WM * C::BN, *s_share = s_z + C::WM * C::BN;
+        static_assert(4 * C::WM * C::BN * 4 + C::WAVES * Shares::BYTES <= C::LDS_BYTES, "room for the shares");
+        Shares shares(a.teacher, reinterpret_cast<float *>(lds) + 4 * C::WM * C::BN, vw - lr, TEACHER, ranges);
         // the teacher's temperature is taken into the exponent, and off maxima and means
         const float log2e = TEACHER ? kLog2e * a.teacher.inv_t : kLog2e;
 #pragma unroll
@@ -411,20 +444,7 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
             const int nt = (wn * C::TN + j) * 16 + (lane & 15), n = n0 + nt;
             const int y = !TEACHER && n < count ? a.labels[a.rows[n]] - vw : -1;
             float z = 0.f;
-            if constexpr (TEACHER) {                                           // the mean of the logits by their shares
-                shares.put(j);
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < C::TM; ++i) {
-                    const f32x4 q = shares.get(j, i * 16 + lr);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) y[r] += q[r] != 0.f ? q[r] * acc[i][j][r] : 0.f;       // a logit of a word past the end may be anything
-                }
-                shares.clear(j);
-                z = a.teacher.inv_t * ((y[0] + y[1]) + (y[2] + y[3]));
-                z += __shfl_xor(z, 16);
-                z += __shfl_xor(z, 32);
-            } else if (a.eps > 0.f) {
+            if (!TEACHER && a.eps > 0.f) {
 #pragma unroll
                 for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -457,29 +477,66 @@ __global__ __launch_bounds__(C::THREADS) void k_vocab_logits(const LogitsArgs a)
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float at = top == -__builtin_inff() ? 0.f : top;             // nothing but the label and words past the end
-            float sum = 0.f;
+            float sum = 0.f, share = 0.f;
 #pragma unroll
             for (int i = 0; i < C::TM; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[i][j][r] - at) * log2e);
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
+            if constexpr (TEACHER) {
+                sum = row_rest<true>(top, sum, [&] {
+                    float x = 0.f;
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x += __builtin_amdgcn_fractf(fast_exp2((acc[i][j][r] - at) * log2e));
+                    return x;
+                });
+                if (shares.any(j)) {
+                    shares.put(j);
+                    f32x4 far = {0.f, 0.f, 0.f, 0.f}, of = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < C::TM; ++i) {
+                        const f32x4 q = shares.get(j, i * 16 + lr);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) far[r] += q[r] != 0.f ? q[r] * (at - acc[i][j][r]) : 0.f, of[r] += q[r];
+                    }
+                    shares.clear(j);
+                    z = a.teacher.inv_t * ((far[0] + far[1]) + (far[2] + far[3]));
+                    share = (of[0] + of[1]) + (of[2] + of[3]);
+                    z += __shfl_xor(z, 16);
+                    z += __shfl_xor(z, 32);
+                    share += __shfl_xor(share, 16);
+                    share += __shfl_xor(share, 32);
+                }
+            } else {
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+            }
             if (lane < 16) {
                 s_max[wm * C::BN + nt] = TEACHER ? top * a.teacher.inv_t : top;
                 s_sum[wm * C::BN + nt] = sum;
                 s_z[wm * C::BN + nt] = z;
+                if constexpr (TEACHER) s_share[wm * C::BN + nt] = share;
             }
         }
         __syncthreads();
         for (int nt = threadIdx.x; nt < C::BN; nt += C::THREADS) {
             if (n0 + nt >= count) break;
             float top = s_max[nt], z = 0.f, sum = 0.f;
+            if constexpr (TEACHER) {
+                sum = s_sum[nt];
 #pragma unroll
-            for (int k = 1; k < C::WM; ++k) top = fmaxf(top, s_max[k * C::BN + nt]);
+                for (int k = 1; k < C::WM; ++k) join_rest(top, sum, s_max[k * C::BN + nt], s_sum[k * C::BN + nt]);
 #pragma unroll
-            for (int k = 0; k < C::WM; ++k) {
-                sum += scaled_sum(s_sum[k * C::BN + nt], s_max[k * C::BN + nt], top);
-                z += s_z[k * C::BN + nt];
+                for (int k = 0; k < C::WM; ++k) z += far_from(s_z[k * C::BN + nt], s_share[k * C::BN + nt], s_max[k * C::BN + nt], top);
+            } else {
+#pragma unroll
+                for (int k = 1; k < C::WM; ++k) top = fmaxf(top, s_max[k * C::BN + nt]);
+#pragma unroll
+                for (int k = 0; k < C::WM; ++k) {
+                    sum += scaled_sum(s_sum[k * C::BN + nt], s_max[k * C::BN + nt], top);
+                    z += s_z[k * C::BN + nt];
+                }
             }
             const size_t at = (size_t)(a.first_tile + im) * a.pitch + n0 + nt;
             a.part_max[at] = top;
@@ -823,7 +880,8 @@ template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 
 
 // The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
 template <int NT, int WAVES, bool TEACHER>
-__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z, float *s_shares) {
+__device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int tile, int v0, float *s_max, float *s_sum, float *s_z, float *s_share,
+                                         float *s_shares) {
     constexpr int ROWS = 16 * NT;
     const int lane = lane_id(), w = wave_id(), vw = v0 + 4 * (lane >> 4);       // this lane holds words vw + r
     TeacherRanges<NT> ranges;
@@ -845,7 +903,7 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
             if (vw + r >= a.V) {
                 acc[j][r] = -__builtin_inff();
             } else {
-                z += !TEACHER ? acc[j][r] : q[r] != 0.f ? q[r] * acc[j][r] : 0.f;
+                z += acc[j][r];
                 if (y == r) {                                                  // the label's logit is left out of maximum and sum
                     a.z_label[n] = acc[j][r];
                     acc[j][r] = -__builtin_inff();
@@ -856,24 +914,52 @@ __device__ __forceinline__ void few_join(const FewArgs &a, f32x4 (&acc)[NT], int
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float at = top == -__builtin_inff() ? 0.f : top;
+        float share = 0.f;
+        if constexpr (TEACHER) {
+            z = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z += q[r] != 0.f ? q[r] * (at - acc[j][r]) : 0.f, share += q[r];
+            share += __shfl_xor(share, 16);
+            share += __shfl_xor(share, 32);
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) sum += fast_exp2((acc[j][r] - at) * kLog2e);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
+        if constexpr (TEACHER) {
+            sum = row_rest<false>(top, sum, [&] {
+                float x = 0.f;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x += __builtin_amdgcn_fractf(fast_exp2((acc[j][r] - at) * kLog2e));
+                return x;
+            });
+        } else {
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+        }
         z += __shfl_xor(z, 16);
         z += __shfl_xor(z, 32);
-        if (lane < 16) s_max[w * ROWS + n] = top, s_sum[w * ROWS + n] = sum, s_z[w * ROWS + n] = z;
+        if (lane < 16) {
+            s_max[w * ROWS + n] = top, s_sum[w * ROWS + n] = sum, s_z[w * ROWS + n] = z;
+            if constexpr (TEACHER) s_share[w * ROWS + n] = share;
+        }
     }
     __syncthreads();
     const int n = threadIdx.x;
     if (n >= a.N) return;
     float top = s_max[n], sum = 0.f, z = 0.f;
+    if constexpr (TEACHER) {
+        sum = s_sum[n];
 #pragma unroll
-    for (int k = 1; k < WAVES; ++k) top = fmaxf(top, s_max[k * ROWS + n]);
+        for (int k = 1; k < WAVES; ++k) join_rest(top, sum, s_max[k * ROWS + n], s_sum[k * ROWS + n]);
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) {
-        sum += scaled_sum(s_sum[k * ROWS + n], s_max[k * ROWS + n], top);
-        z += s_z[k * ROWS + n];
+        for (int k = 0; k < WAVES; ++k) z += far_from(s_z[k * ROWS + n], s_share[k * ROWS + n], s_max[k * ROWS + n], top);
+    } else {
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) top = fmaxf(top, s_max[k * ROWS + n]);
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            sum += scaled_sum(s_sum[k * ROWS + n], s_max[k * ROWS + n], top);
+            z += s_z[k * ROWS + n];
+        }
     }
     const size_t at = (size_t)n * a.tiles + tile;
     a.part_max[at] = top;
@@ -930,7 +1016,7 @@ template <int NT, bool TEACHER> __device__ __forceinline__ void few_dz(const Few
 template <typename T, int AHEAD, bool TEACHER>
 __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
     constexpr int PLANES = FewFragment<T>::PLANES;
-    __shared__ float s_max[64], s_sum[64], s_z[64];
+    __shared__ float s_max[64], s_sum[64], s_z[64], s_share[TEACHER ? 64 : 1];
     const int lane = lane_id(), v0 = (blockIdx.x * 4 + wave_id()) * 16, steps = (a.D + 31) / 32, k_lane = 8 * (lane >> 4);
     const int first = min(v0, a.V - 1);
     const __amdgpu_buffer_rsrc_t words = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(static_cast<const T *>(a.W) + (size_t)first * a.D), 0, 0x7ffffff0, 0x00020000);
@@ -958,7 +1044,7 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
             acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
         }
     __shared__ __align__(16) float s_shares[TEACHER ? 4 * TeacherTile<16, 1>::BYTES / 4 : 1];
-    few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z, s_shares);
+    few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z, s_share, s_shares);
 }
 
 // 128 k at a time: the words' next 256 and the rows' next 128 are on their way; the rows stand in LDS twice.
@@ -971,7 +1057,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     constexpr int GROUPS = ROWS * kFewK / 8, ITEMS = (GROUPS + 64 * WAVES - 1) / (64 * WAVES);      // groups of 8 numbers of the rows, per thread
     constexpr int STAGE = PLANES * ROWS * kFewPitch;
     __shared__ __align__(16) char s_h[2 * STAGE];
-    __shared__ float s_max[WAVES * ROWS], s_sum[WAVES * ROWS], s_z[WAVES * ROWS];
+    __shared__ float s_max[WAVES * ROWS], s_sum[WAVES * ROWS], s_z[WAVES * ROWS], s_share[TEACHER ? WAVES * ROWS : 1];
     // the groups' blocks of a tile side by side: its words are read from memory once
     const int tile = blockIdx.x / all.groups, n0 = (blockIdx.x - tile * all.groups) * kFewGroup;
     FewArgs a = all;
@@ -1066,7 +1152,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
     static_assert(WAVES * TeacherTile<16, NT>::BYTES <= sizeof(s_h), "room for the shares");      // (behind the last barrier nobody reads the rows)
     float *s_shares = reinterpret_cast<float *>(s_h);
     if constexpr (BWD) few_dz<NT, TEACHER>(a, acc, n0, v0, s_shares);
-    else few_join<NT, WAVES, TEACHER>(a, acc, tile, v0, s_max, s_sum, s_z, s_shares);
+    else few_join<NT, WAVES, TEACHER>(a, acc, tile, v0, s_max, s_sum, s_z, s_share, s_shares);
 }
 
 // loss and lse of a row from its maximum, sum and sum of logits without and with the label:
@@ -1081,13 +1167,24 @@ __device__ __forceinline__ void loss_of_row(float top, float sum, float z, float
     if (eps > 0.f) loss += eps * (zl - z / (float)V);
 }
 
-// The same against a teacher: z is the sum of the logits by their shares, `own` the sum of share log share.
-__device__ __forceinline__ void loss_of_row(float top, float sum, float z, const Teacher &t, int n, float &loss, float &lse) {
-    const float rest = logf(sum);
-    lse = top + rest;
-    // without the digits that lse loses to its size; the temperature's square by itself may leave fp32's range
-    loss = t.temperature * (t.temperature * (t.own[n] + ((top - z) + rest)));
+// The same against a teacher: from its maximum, the rest of its exponentials and how far its words are below the maximum; `own` is the sum of share log share.  Each
+// of the terms is small where student and teacher are sure of the same word.  The temperature's square by itself may leave fp32's range.
+__device__ __forceinline__ void loss_of_row(float top, float rest, float far, const Teacher &t, int n, float &loss, float &lse) {
+    const float log_sum = log1pf(rest);
+    lse = top + log_sum;
+    loss = t.temperature * (t.temperature * (t.own[n] + (far + log_sum)));
 }
+// How far a row's entries of a part of its list are below their tiles' largest maximum, `top`
+struct EntriesFar {
+    float top = -__builtin_inff(), share = 0.f, far = 0.f;
+    __device__ __forceinline__ void add(float q, float tile_top) {
+        const float to = fmaxf(top, tile_top);
+        far = far_from(far, share, top, to);
+        if (q != 0.f && tile_top != to) far += q * (to - tile_top);
+        share += q;
+        top = to;
+    }
+};
 
 // A block per row.
 template <bool TEACHER>
@@ -1098,7 +1195,15 @@ __global__ __launch_bounds__(256) void k_vocab_few_finish(const FewArgs a, float
         if (threadIdx.x == 0) loss[n] = 0.f, lse[n] = 0.f;
         return;
     }
-    float top = -__builtin_inff(), sum = 0.f, z = 0.f;
+    float top = -__builtin_inff(), sum = TEACHER ? -1.f : 0.f, z = 0.f;
+    EntriesFar entries;
+    if (TEACHER && w == 0) {
+        const int count = a.teacher.start[(size_t)n * a.teacher.marks + a.teacher.marks - 1];
+        for (int k = lane; k < count; k += 64) {
+            const size_t at = (size_t)n * a.teacher.K + k;
+            entries.add(a.teacher.shares[at], a.part_max[(size_t)n * a.tiles + a.teacher.words[at] / few_words(a.N)]);
+        }
+    }
     for (int t0 = threadIdx.x; t0 < a.tiles; t0 += 1024) {
         float m[4], s[4], zz[4];
 #pragma unroll
@@ -1106,39 +1211,83 @@ __global__ __launch_bounds__(256) void k_vocab_few_finish(const FewArgs a, float
             const size_t at = (size_t)n * a.tiles + min(t0 + 256 * u, a.tiles - 1);
             m[u] = a.part_max[at], s[u] = a.part_sum[at], zz[u] = a.part_z[at];
         }
-        float next = top;
+        if constexpr (TEACHER) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) next = fmaxf(next, m[u]);
-        sum = scaled_sum(sum, top, next);
-        top = next;
+            for (int u = 0; u < 4; ++u)
+                if (t0 + 256 * u < a.tiles) join_rest(top, sum, m[u], s[u]), z += zz[u];
+        } else {
+            float next = top;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (t0 + 256 * u < a.tiles) sum += scaled_sum(s[u], m[u], top), z += zz[u];
+            for (int u = 0; u < 4; ++u) next = fmaxf(next, m[u]);
+            sum = scaled_sum(sum, top, next);
+            top = next;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (t0 + 256 * u < a.tiles) sum += scaled_sum(s[u], m[u], top), z += zz[u];
+        }
     }
     const float wave_top = wave_max(top);
-    sum = wave_sum(scaled_sum(sum, top, wave_top));
+    if constexpr (TEACHER) {
+        // (of all lanes, whose exponentials are none, ones or more, one keeps its likeliest out)
+        const bool out = lane == __builtin_ctzll(__ballot(top == wave_top));
+        sum = wave_sum(out ? sum : scaled_sum(1.f + sum, top, wave_top));
+        if (w == 0) {
+            const float to = wave_max(entries.top);
+            z += far_from(entries.far, entries.share, entries.top, to);
+            entries.share = wave_sum(entries.share), entries.top = to;
+        }
+    } else {
+        sum = wave_sum(scaled_sum(sum, top, wave_top));
+    }
     z = wave_sum(z);
     if (lane == 0) s_max[w] = wave_top, s_sum[w] = sum, s_z[w] = z;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-    sum = 0.f, z = 0.f;
+    if constexpr (TEACHER) {
+        top = wave_top;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum += scaled_sum(s_sum[k], s_max[k], top), z += s_z[k];
-    if constexpr (TEACHER) loss_of_row(top, sum, z, a.teacher, n, loss[n], lse[n]);
-    else loss_of_row(top, sum, z, a.z_label[n], a.V, a.eps, loss[n], lse[n]);
+        for (int k = 1; k < 4; ++k) join_rest(top, sum, s_max[k], s_sum[k]), z += s_z[k];
+        loss_of_row(top, sum, far_from(z, entries.share, entries.top, top), a.teacher, n, loss[n], lse[n]);
+    } else {
+        top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+        sum = 0.f, z = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += scaled_sum(s_sum[k], s_max[k], top), z += s_z[k];
+        loss_of_row(top, sum, z, a.z_label[n], a.V, a.eps, loss[n], lse[n]);
+    }
 }
 
-// Joins the tiles of 64 rows: four waves take a quarter of the tiles each, lanes are rows.  Rows without a label get zeros.
+// Joins the tiles of 64 rows, of 2^tile_bits words each: four waves take a quarter of the tiles each, lanes are rows.  Rows without a label get zeros.
 template <bool TEACHER>
 __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restrict__ part_max, const float *__restrict__ part_sum,
                                                            const float *__restrict__ part_z, const float *__restrict__ z_label,
                                                            const int *__restrict__ place, int N, int V, int tiles, size_t pitch,
-                                                           float eps, const Teacher teacher, float *__restrict__ loss, float *__restrict__ lse) {
-    __shared__ float s_max[4][64], s_sum[4][64], s_z[4][64];
+                                                           float eps, const Teacher teacher, int tile_bits, float *__restrict__ loss,
+                                                           float *__restrict__ lse) {
+    __shared__ float s_max[4][64], s_sum[4][64], s_z[4][64], s_top[4][TEACHER ? 64 : 1], s_share[4][TEACHER ? 64 : 1];
     const int lane = lane_id(), w = wave_id(), n = blockIdx.x * 64 + lane, p = n < N ? place[n] : -1;
     const int share = (tiles + 3) / 4, t0 = w * share, t1 = min(tiles, t0 + share);
-    float top = -__builtin_inff(), sum = 0.f, z = 0.f;
+    float top = -__builtin_inff(), sum = TEACHER ? -1.f : 0.f, z = 0.f;
+    EntriesFar entries;
+    if (TEACHER && p >= 0) {                               // the waves share a row's entries too (what stands behind the last one is nothing)
+        constexpr int U = 8;
+        const int count = teacher.start[(size_t)n * teacher.marks + teacher.marks - 1];
+        for (int k0 = w; k0 < teacher.K; k0 += 4 * U) {
+            float q[U], m[U];
+            int word[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const size_t at = (size_t)n * teacher.K + min(k0 + 4 * u, teacher.K - 1);
+                word[u] = teacher.words[at];
+                q[u] = teacher.shares[at];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) m[u] = part_max[(size_t)(k0 + 4 * u < count ? word[u] >> tile_bits : 0) * pitch + p];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k0 + 4 * u < count) entries.add(q[u], m[u]);
+        }
+    }
     if (p >= 0) {
         for (int t = t0; t < t1; t += 8) {
             float m[8], s[8], zz[8];
@@ -1149,18 +1298,35 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
                 s[u] = part_sum[at];
                 zz[u] = TEACHER || eps > 0.f ? part_z[at] : 0.f;
             }
-            float next = top;
+            if constexpr (TEACHER) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) next = fmaxf(next, m[u]);
-            sum = scaled_sum(sum, top, next);
-            top = next;
+                for (int u = 0; u < 8; ++u)
+                    if (t + u >= t1) m[u] = -__builtin_inff(), s[u] = -1.f, zz[u] = 0.f;
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (t + u < t1) {
-                    sum += scaled_sum(s[u], m[u], top);
-                    z += zz[u];
-                }
+                for (int d = 1; d < 8; d *= 2)
+#pragma unroll
+                    for (int u = 0; u < 8; u += 2 * d) join_rest(m[u], s[u], m[u + d], s[u + d]), zz[u] += zz[u + d];
+                join_rest(top, sum, m[0], s[0]);
+                z += zz[0];
+            } else {
+                float next = top;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) next = fmaxf(next, m[u]);
+                sum = scaled_sum(sum, top, next);
+                top = next;
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (t + u < t1) {
+                        sum += scaled_sum(s[u], m[u], top);
+                        z += zz[u];
+                    }
+            }
         }
+    }
+    if constexpr (TEACHER) {
+        s_top[w][lane] = entries.top;
+        s_share[w][lane] = entries.share;
+        z += entries.far;
     }
     s_max[w][lane] = top;
     s_sum[w][lane] = sum;
@@ -1169,16 +1335,24 @@ __global__ __launch_bounds__(256) void k_vocab_loss_finish(const float *__restri
     if (w != 0 || n >= N) return;
     float l = 0.f, e = 0.f;
     if (p >= 0) {
-        float all = fmaxf(fmaxf(s_max[0][lane], s_max[1][lane]), fmaxf(s_max[2][lane], s_max[3][lane]));
-        sum = 0.f;
-        z = 0.f;
+        if constexpr (TEACHER) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            sum += scaled_sum(s_sum[k][lane], s_max[k][lane], all);
-            z += s_z[k][lane];
+            for (int k = 1; k < 4; ++k) join_rest(top, sum, s_max[k][lane], s_sum[k][lane]);
+            z = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z += far_from(s_z[k][lane], s_share[k][lane], s_top[k][lane], top);
+            loss_of_row(top, sum, z, teacher, n, l, e);
+        } else {
+            float all = fmaxf(fmaxf(s_max[0][lane], s_max[1][lane]), fmaxf(s_max[2][lane], s_max[3][lane]));
+            sum = 0.f;
+            z = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                sum += scaled_sum(s_sum[k][lane], s_max[k][lane], all);
+                z += s_z[k][lane];
+            }
+            loss_of_row(all, sum, z, z_label[p], V, eps, l, e);
         }
-        if constexpr (TEACHER) loss_of_row(all, sum, z, teacher, n, l, e);
-        else loss_of_row(all, sum, z, z_label[p], V, eps, l, e);
     }
     loss[n] = l;
     lse[n] = e;
@@ -1623,7 +1797,7 @@ static echo_status_t run_forward(const VocabRun &x, float eps, const Teacher &te
     }
     LaunchRecord r = launch_begin("vocab_loss_finish", x.st);
     k_vocab_loss_finish<TEACHER><<<(N + 63) / 64, 256, 0, x.st>>>(a.part_max, a.part_sum, a.part_z, a.z_label, x.at<int>(x.p.place), N, V, tiles, a.pitch,
-                                                                  eps, teacher, loss, lse);
+                                                                  eps, teacher, big ? 8 : 7, loss, lse);
     return launch_end(r);
 }
 
