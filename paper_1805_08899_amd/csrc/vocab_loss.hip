@@ -867,16 +867,27 @@ template <typename T> struct FewFragment {
         }
     }
 };
-template <int PLANES> __device__ __forceinline__ f32x4 few_multiply(const u32x4 (&a)[PLANES], const u32x4 (&b)[PLANES], f32x4 c) {
-    if constexpr (PLANES == 3) {                                               // the small terms first
-        c = mfma16(a[1], b[1], c);
-        c = mfma16(a[2], b[0], c);
-        c = mfma16(a[0], b[2], c);
-        c = mfma16(a[1], b[0], c);
-        c = mfma16(a[0], b[1], c);
+// A product of f32 rows is six of planes, five of them small.  APART: those have a sum of their own, which join() adds at the end: to the large one, every 32 k, they
+// are six roundings at its size instead of one (lse of 16 rows of D = 2048 off by 4.4e-7 of itself instead of 8e-8, 64 of 1024 by 2.8e-7 instead of 9e-8; a
+// plain fp32 product 8e-8, 9e-8; 0 to 0.5 % of the time).  Labels have one sum, so that their results stay as they were.
+template <int PLANES, bool APART> struct FewSum {
+    f32x4 large = {0.f, 0.f, 0.f, 0.f}, small = {0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void multiply(const u32x4 (&a)[PLANES], const u32x4 (&b)[PLANES]) {
+        f32x4 &c = APART ? small : large;
+        if constexpr (PLANES == 3) {                                           // the small terms first
+            c = mfma16(a[1], b[1], c);
+            c = mfma16(a[2], b[0], c);
+            c = mfma16(a[0], b[2], c);
+            c = mfma16(a[1], b[0], c);
+            c = mfma16(a[0], b[1], c);
+        }
+        large = mfma16(a[0], b[0], large);
     }
-    return mfma16(a[0], b[0], c);
-}
+    __device__ __forceinline__ f32x4 join() const {
+        if constexpr (APART && PLANES == 3) return large + small;
+        else return large;
+    }
+};
 
 // The logits of 16 NT rows and a wave's 16 words, joined over the block: s_*: WAVES x 16 NT floats
 template <int NT, int WAVES, bool TEACHER>
@@ -1029,7 +1040,7 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
         fh[d].load(rows, row_off, 32 * t + k_lane, a.D);
         loads_stay();
     };
-    f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
+    FewSum<PLANES, TEACHER> sum;
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d)
         if (d < steps) fetch(d, d);
@@ -1041,8 +1052,9 @@ __global__ __launch_bounds__(256, 2) void k_vocab_few_alone(const FewArgs a) {
             fw[d].planes(pw);
             fh[d].planes(ph);
             if (t0 + d + AHEAD < steps) fetch(d, t0 + d + AHEAD);
-            acc[0] = few_multiply<PLANES>(pw, ph, acc[0]);
+            sum.multiply(pw, ph);
         }
+    f32x4 acc[1] = {sum.join()};
     __shared__ __align__(16) float s_shares[TEACHER ? 4 * TeacherTile<16, 1>::BYTES / 4 : 1];
     few_join<1, 4, TEACHER>(a, acc, blockIdx.x, v0, s_max, s_sum, s_z, s_share, s_shares);
 }
@@ -1111,9 +1123,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
             }
         }
     };
-    f32x4 acc[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    FewSum<PLANES, TEACHER> sum[NT];
     fetch_rows(0);
     fetch_words(0, 0);
     fetch_words(1, 1);
@@ -1139,7 +1149,7 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
                 u32x4 ph[PLANES];
 #pragma unroll
                 for (int k = 0; k < PLANES; ++k) ph[k] = *reinterpret_cast<const u32x4 *>(from + (k * ROWS + 16 * j) * kFewPitch);
-                acc[j] = few_multiply<PLANES>(pw[s], ph, acc[j]);
+                sum[j].multiply(pw[s], ph);
             }
         }
         if (t + 1 < steps) put_rows(t + 1);
@@ -1149,6 +1159,9 @@ __global__ __launch_bounds__(512) void k_vocab_few_shared(const FewArgs all) {
         step(t, fw[0]);
         if (t + 1 < steps) step(t + 1, fw[1]);
     }
+    f32x4 acc[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j] = sum[j].join();
     static_assert(WAVES * TeacherTile<16, NT>::BYTES <= sizeof(s_h), "room for the shares");      // (behind the last barrier nobody reads the rows)
     float *s_shares = reinterpret_cast<float *>(s_h);
     if constexpr (BWD) few_dz<NT, TEACHER>(a, acc, n0, v0, s_shares);
