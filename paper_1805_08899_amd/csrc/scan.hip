@@ -1049,7 +1049,8 @@ static echo_status_t check_scan(const echo_scan_desc_t *d) {
     if (!d) return ECHO_ERR_NULL;
     if (d->dtype != ECHO_F32 && d->dtype != ECHO_BF16) return ECHO_ERR_DTYPE;
     if (d->B < 1 || d->T < 1 || d->H < 1 || d->B > ECHO_SCAN_MAX_ROWS || d->T > ECHO_SCAN_MAX_ROWS || d->H > ECHO_SCAN_MAX_H) return ECHO_ERR_SHAPE;
-    if ((d->reverse != 0 && d->reverse != 1) || (size_t)d->B * d->T * d->H > (size_t)1 << 40) return ECHO_ERR_SHAPE;
+    // (B T fits 64 bits, B T H may not)
+    if ((d->reverse != 0 && d->reverse != 1) || (size_t)d->B * d->T > ((size_t)1 << 40) / d->H) return ECHO_ERR_SHAPE;
     return ECHO_OK;
 }
 static size_t scan_chunks(const echo_scan_desc_t &d) { return ((size_t)d.T + ECHO_SCAN_CHUNK - 1) / ECHO_SCAN_CHUNK; }
