@@ -249,7 +249,7 @@ static echo_status_t check_draft(const echo_draft_desc_t *d) {
 
 // Several blocks to a sequence (and a second launch) pay where there are few sequences and many words; one block and kDraftGroups of them, us, f32:
 //   1 x 100003 words 20.0 / 11.3, 1 x 32000 9.7 / 9.7, 16 x 100003 23.9 / 14.7, 64 x 100003 24.9 / 17.9, 128 x 100003 26.9 / 28.4, 256 x 8000 11.4 / 25.7; 64 x 50021 bf16
-//   15.1 / 13.2
+//   15.1 / 13.2.  Between 64 and 128 sequences, where the two lines cross, nothing is measured: the border is the last number at which several were the better ones.
 constexpr int kDraftSplitB = 64, kDraftSplitV = 40000;
 static size_t draft_bytes(const echo_draft_desc_t &d) {
     return d.B <= kDraftSplitB && d.V >= kDraftSplitV ? (size_t)d.B * kDraftSegments * 8 : 0;

@@ -870,11 +870,13 @@ __global__ __launch_bounds__(kThreads<kChunkGroups>, 4) void k_scan_chain(const 
 // ---- chains that are a block's ---------------------------------------------------------------------------------------------
 // A short chain, or one of so many that they keep all compute units busy to the end, is better off with one block for all of its chunks: the state stays in LDS,
 // nothing is cleared and nobody looks at others' words.  Chain of blocks / blocks' chains, us, forward and backward:
-//   two chunks: 1 x 200 x 1024 bf16 8.7 / 7.8 and 10.3 / 10.2, 16 x 200 x 1024 bf16 11.8 / 9.8 and 13.7 / 12.9 (f32 16.0 / 13.4 and 21.8 / 23.3), 128 x 200 x 1024 bf16
-//     52 / 39 and 79 / 69
-//   three and four, 256 chains and a multiple: 32 x 300 x 1022 bf16 28.5 / 22 and 42.6 / 36.2, 64 x 300 x 512 f32 35.2 / 31.1 and 58.8 / 53.5; 128 x 500 x 1024 f32 183 / 170 and
-//     319 / 317; 16 x 500 x 1024 bf16 19.8 / 18.1 and 28.8 / 28.8; a few more than that: 33 x 500 x 1024 bf16 34 / 37 and 52 / 60; few: 8 x 500 x 1024 bf16 13.0 / 14.7 and 15.6 / 21.5
-//   more of them: 32 x 1000 x 1024 bf16 60 / 58 and 101 / 106; of unequal length 64 x 2000 x 512 f32 166 / 185 and 311 / 338
+//   two chunks: 1 x 200 x 1024 bf16 8.8 / 8.1 and 11.3 / 11.1, 16 x 200 x 1024 bf16 12.4 / 10.2 and 15.6 / 13.9 (f32 16.3 / 13.4 and 24.1 / 23.7), 128 x 200 x 1024 bf16
+//     58 / 47 and 96 / 82
+//   three and four, 512 chains and more, a multiple of 256 or little less: 32 x 300 x 1022 bf16 28.4 / 22.2 and 43.6 / 36.6, 64 x 300 x 512 f32 36.6 / 34.4 and 61.6 / 56.8,
+//     128 x 500 x 1024 f32 188 / 171 and 328 / 320; a few chains more than that: 33 x 500 x 1024 bf16 34 / 36 and 55 / 59
+//   three and four, 256 chains: 16 x 500 x 1024 bf16 20.8 / 19.2 and 30.7 / 31.3, f32 28.6 / 26.9 and 48.4 / 45.9: one of the four is slower, so they are left out; 128
+//     chains: 8 x 500 x 1024 bf16 12.5 / 14.5 and 16.7 / 22.2
+//   more chunks: 32 x 1000 x 1024 bf16 59 / 53 and 101 / 100; of unequal length 64 x 2000 x 512 f32 159 / 163 and 301 / 314
 // (The next chunk's gates requested while this one's maps are folded: 17 registers in memory with bf16 gates, 22 -> 30.5 us of 32 x 300 x 1022.)
 static bool walks(long long chains, int chunks) {
     if (chunks < 2 || chains > 1 << 22) return false;      // (a grid has fewer than 2^32 threads)

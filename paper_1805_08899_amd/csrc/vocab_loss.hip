@@ -353,7 +353,7 @@ struct LogitsArgs {
     int V, v0;                       // words of the vocabulary; this piece's first word
     float eps;                       // label smoothing
     Teacher teacher;                 // in the place of labels
-    // forward: [tiles][pitch] maximum, sum, sum of logits; the label's logit
+    // forward: [tiles][pitch] maximum, sum, sum of logits; the label's logit.  Against a teacher: maximum, rest, how far its words are below the maximum
     float *part_max, *part_sum, *part_z, *z_label;
     int first_tile;
     size_t pitch;
